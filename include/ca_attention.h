@@ -95,6 +95,21 @@ int ca_plan_upload(ca_plan_t *plan, void *hip_stream);
  * used on any stream. */
 int ca_plan(const ca_batch_desc *desc, ca_plan_t **out);
 
+/*
+ * ca_plan_window: a plan whose rows attend a sliding window of their context and its first tokens (layers with a window and
+ * sinks): row i of task t, at position p, sees the keys j of [0, min(kv_len[t], p + 1)) with p - j < window or j < sinks.
+ * window >= 1 counts the row's own position (1: the row itself alone, and the sinks); sinks >= 0.  Everything that takes a plan takes
+ * this one too: ca_forward and ca_backward run the windowed kernels, with the workspaces of ca_plan_workspace_bytes (which
+ * here includes the partial results of tiles with sinks; the forward needs none).  A row that sees nothing (its task's kv_len ends
+ * before its window and there are no sinks) gets O = 0 and LSE = -inf, dQ = 0, and adds nothing to dK and dV.  A window that hides
+ * nothing from any row gives the plan of ca_plan.  Results are bit-reproducible from run to run; the tiles of keys with sinks
+ * are summed in pieces whose number depends on the batch.
+ * With ca_merge_partials (shards with a sub-range of their context) window and sinks count within the "document" that the sub-range is.
+ * ca_plan_window_host: the same without a device, as ca_plan_host.
+ */
+int ca_plan_window(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out);
+int ca_plan_window_host(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out);
+
 /* Bytes of caller-provided device workspace ca_forward / ca_backward need (either pointer may be NULL). */
 int ca_plan_workspace_bytes(const ca_plan_t *plan, size_t *fwd_bytes, size_t *bwd_bytes);
 
@@ -315,6 +330,13 @@ int64_t ca_plan_combine_units(const ca_plan_t *plan, int32_t backward, int32_t *
  * 128, of 128 at 64; from the third field on every row sees a later key too; count 1, follow 0).  queue: [9], or NULL; units
  * queue[i] .. queue[i + 1] - 1 are those of XCD i, in the order in which its workgroups take them. */
 int64_t ca_plan_one_pass_units(const ca_plan_t *plan, int32_t *units, int32_t *queue);
+
+/* The schedule of a windowed plan (ca_plan_window; 0 for any other).  kind 0: its forward / dQ units, [n][8] = the 5 fields of fwd, the
+ * document position at which the unit's window tiles begin (the tiles with sinks before it come in addition; the packed KV row is
+ * the document's token 0 and keys are counted from there), -1, rows.  kind 1: its dK/dV units, [n][12] = the 10 fields of bwd (of a
+ * piece follow = -1 - part), and then the slot from which on rows do not all see the whole tile again, and a spare one.
+ * kind 2: [padded_rows] document position at which each slot's window begins (one behind its position where it is empty). */
+int64_t ca_plan_window_units(const ca_plan_t *plan, int32_t kind, int32_t *out);
 
 #ifdef __cplusplus
 }

@@ -41,10 +41,11 @@ class AttentionServer:
         o.backward(d_o)                          # q.grad, k.grad, v.grad
 
     `batch` is any object with the descriptor's fields (e.g. workloads.Batch).  Rows of q that belong to no task
-    have undefined output and zero gradient.  one_pass: see binding.alloc_workspace."""
+    have undefined output and zero gradient.  one_pass: see binding.alloc_workspace.  window, sinks: every row attends the last
+    `window` keys of its context, itself among them, and the context's first `sinks` (None: all of it); see binding.ca_plan."""
 
-    def __init__(self, batch, device="cuda", one_pass=None):
-        self.plan = B.ca_plan(batch)
+    def __init__(self, batch, device="cuda", one_pass=None, window=None, sinks=0):
+        self.plan = B.ca_plan(batch, window, sinks)
         self.ws = B.alloc_workspace(self.plan, device, one_pass)
         self.fwd_ws_bytes = self.plan.workspace_bytes_split()[0]
 

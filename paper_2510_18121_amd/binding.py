@@ -7,6 +7,7 @@ library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import numpy as np
@@ -52,6 +53,9 @@ def lib() -> ctypes.CDLL:
         vp, sz = ctypes.c_void_p, ctypes.c_size_t
         L.ca_plan_host.argtypes = [ctypes.POINTER(BatchDesc), ctypes.POINTER(vp)]
         L.ca_plan.argtypes = [ctypes.POINTER(BatchDesc), ctypes.POINTER(vp)]
+        for f in (L.ca_plan_window, L.ca_plan_window_host):
+            f.argtypes = [ctypes.POINTER(BatchDesc), ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(vp)]
+        L.ca_plan_window_units.argtypes = [vp, ctypes.c_int32, vp]
         L.ca_plan_upload.argtypes = [vp, vp]
         L.ca_plan_workspace_bytes.argtypes = [vp, ctypes.POINTER(sz), ctypes.POINTER(sz)]
         L.ca_plan_workspace_bytes_split.argtypes = [vp, ctypes.POINTER(sz), ctypes.POINTER(sz)]
@@ -68,7 +72,7 @@ def lib() -> ctypes.CDLL:
         L.ca_profile_read.argtypes = [vp, vp]
         L.ca_plan_info.argtypes = [vp, vp, ctypes.c_int]
         for f in (L.ca_plan_rows, L.ca_plan_fwd_units, L.ca_plan_bwd_units, L.ca_plan_fwd_pieces, L.ca_plan_bwd_pieces,
-                  L.ca_plan_combine_units, L.ca_plan_one_pass_units):
+                  L.ca_plan_combine_units, L.ca_plan_one_pass_units, L.ca_plan_window_units):
             f.restype = ctypes.c_int64
         L.ca_plan_fwd_pieces.argtypes = [vp, vp]
         L.ca_plan_bwd_pieces.argtypes = [vp, vp, vp]
@@ -170,6 +174,14 @@ class Plan:
         lib().ca_plan_bwd_units(self.handle, u.ctypes.data)
         return u
 
+    def window_units(self):
+        """Forward units, dK/dV units and the slots' windows of a windowed plan (arrays as in the header; empty for any other)."""
+        out = []
+        for kind, fields in ((0, 8), (1, 12), (2, 1)):
+            out.append(np.zeros((lib().ca_plan_window_units(self.handle, kind, None), fields), np.int32))
+            lib().ca_plan_window_units(self.handle, kind, out[-1].ctypes.data)
+        return out[0], out[1], out[2][:, 0]
+
     def one_pass_units(self):
         """Units of the backward in one pass (fields as in bwd_units), and where each XCD's queue of them begins."""
         n = lib().ca_plan_one_pass_units(self.handle, None, None)
@@ -210,22 +222,26 @@ class Plan:
             pass
 
 
-def ca_plan_host(batch) -> Plan:
-    """Validate `batch` and build its launch schedule on the host only (no GPU needed)."""
+def _planned(batch, window, sinks, plain, windowed) -> Plan:
     keep = []
     d = make_desc(batch, keep)
     h = ctypes.c_void_p()
-    _check(lib().ca_plan_host(ctypes.byref(d), ctypes.byref(h)))
+    if window is None:
+        _check(plain(ctypes.byref(d), ctypes.byref(h)))
+    else:
+        _check(windowed(ctypes.byref(d), operator.index(window), operator.index(sinks), ctypes.byref(h)))
     return Plan(h.value, batch)
 
 
-def ca_plan(batch) -> Plan:
+def ca_plan_host(batch, window=None, sinks=0) -> Plan:
+    """Validate `batch` and build its launch schedule on the host only (no GPU needed).  With a window a row sees, of the keys up to
+    its own position p, those with p - j < window or j < sinks (ca_plan_window of the header); without one, `sinks` has no effect."""
+    return _planned(batch, window, sinks, lib().ca_plan_host, lib().ca_plan_window_host)
+
+
+def ca_plan(batch, window=None, sinks=0) -> Plan:
     """ca_plan_host + upload of the schedule to the current device."""
-    keep = []
-    d = make_desc(batch, keep)
-    h = ctypes.c_void_p()
-    _check(lib().ca_plan(ctypes.byref(d), ctypes.byref(h)))
-    return Plan(h.value, batch)
+    return _planned(batch, window, sinks, lib().ca_plan, lib().ca_plan_window)
 
 
 def _stream_ptr(stream):

@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "ca_internal.h"
+#include "ca_launch.h"
 
 namespace ca {
 // parts / split: (there is) device memory for the partial results of the piece lists; otherwise the whole units are run
@@ -74,6 +75,7 @@ static void free_device(ca_plan_t *p) {
   p->d_fwd_units = p->d_fwd_pieces = nullptr;
   p->d_bwd_units = p->d_bwd_pieces = p->d_fused_units = nullptr;
   p->d_fwd_combine = p->d_bwd_combine = nullptr;
+  p->d_slot_lo = nullptr, p->d_window_units = nullptr;
   if (cur >= 0 && cur != p->device) (void)hipSetDevice(cur);
   p->device = -1;
 }
@@ -139,6 +141,7 @@ int ca_plan_upload(ca_plan_t *p, void *hip_stream) {
     auto add = [&](const auto &src) { arrays.push_back({src.data(), src.size() * sizeof(src[0]), 0}); };
     add(p->slot_row), add(p->slot_pos), add(p->block_rpk), add(p->pos_kv), add(p->fwd_units), add(p->bwd_units);
     add(p->fwd_pieces), add(p->bwd_pieces), add(p->fwd_combine), add(p->bwd_combine), add(p->joint_order), add(p->fused_units);
+    add(p->slot_lo), add(p->window_units);
     for (const bool large : {false, true}) {
       for (Array &a : arrays)
         if ((a.bytes > SMALL_ARRAY) == large) a.at = bytes, bytes = (bytes + a.bytes + 255) / 256 * 256;
@@ -172,14 +175,13 @@ int ca_plan_upload(ca_plan_t *p, void *hip_stream) {
   place(p->d_slot_row, 0), place(p->d_slot_pos, 1), place(p->d_block_rpk, 2), place(p->d_pos_kv, 3);
   place(p->d_fwd_units, 4), place(p->d_bwd_units, 5), place(p->d_fwd_pieces, 6), place(p->d_bwd_pieces, 7);
   place(p->d_fwd_combine, 8), place(p->d_bwd_combine, 9), place(p->d_joint_order, 10), place(p->d_fused_units, 11);
+  place(p->d_slot_lo, 12), place(p->d_window_units, 13);
   // the vectors and `blob` stay alive in the plan, so the asynchronous copies read valid memory
   return CA_OK;
 }
 
-int ca_plan(const ca_batch_desc *desc, ca_plan_t **out) {
-  int rc = ca_plan_host(desc, out);
-  if (rc != CA_OK) return rc;
-  rc = ca_plan_upload(*out, nullptr);
+static int upload_and_wait(ca_plan_t **out) {
+  int rc = ca_plan_upload(*out, nullptr);
   if (rc == CA_OK) {  // callers launch on streams of their own: the schedule must have landed before they do
     const hipError_t e = hipStreamSynchronize(nullptr);
     if (e != hipSuccess) rc = ca::hip_fail("plan upload", e);
@@ -189,6 +191,16 @@ int ca_plan(const ca_batch_desc *desc, ca_plan_t **out) {
     *out = nullptr;
   }
   return rc;
+}
+
+int ca_plan(const ca_batch_desc *desc, ca_plan_t **out) {
+  const int rc = ca_plan_host(desc, out);
+  return rc != CA_OK ? rc : upload_and_wait(out);
+}
+
+int ca_plan_window(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out) {
+  const int rc = ca_plan_window_host(desc, window, sinks, out);
+  return rc != CA_OK ? rc : upload_and_wait(out);
 }
 
 int ca_profile_enable(ca_plan_t *p, int on) {
@@ -270,7 +282,7 @@ int ca_forward(const ca_plan_t *p, const void *q, const void *k, const void *v, 
     return x->ws_fwd_split > 0 && ws && ws_bytes >= x->ws_fwd_split && reinterpret_cast<uintptr_t>(ws) % 256 == 0;
   };
   const ca_plan_t *const use = p->within_static && !fits(p) ? p->within_static.get() : p;
-  hipError_t e = launch_fwd(use, q, k, v, o, lse, fits(use) ? ws : nullptr, st);
+  hipError_t e = p->window > 0 ? launch_fwd_window(p, q, k, v, o, lse, st) : launch_fwd(use, q, k, v, o, lse, fits(use) ? ws : nullptr, st);
   if (e != hipSuccess) return hip_fail("forward launch", e);
   if (p->profile) {
     (void)hipEventRecord(static_cast<hipEvent_t>(mp->ev[1]), st);
@@ -296,8 +308,10 @@ int ca_backward(const ca_plan_t *p, const void *q, const void *k, const void *v,
   const ca_plan_t *const use = p->within_static && ws_bytes < p->ws_bwd_split ? p->within_static.get() : p;
   const bool split = use->ws_bwd_split > use->ws_bwd && ws_bytes >= use->ws_bwd_split;
   const bool fused = p->fused && ws_bytes >= p->ws_bwd_fused;
-  hipError_t e = launch_bwd(fused ? p : use, q, k, v, o, d_o, lse, dq, dk, dv, ws, split, fused, static_cast<hipStream_t>(hip_stream),
-                            p->profile ? reinterpret_cast<hipEvent_t *>(&mp->ev[2]) : nullptr);
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  hipEvent_t *const ev = p->profile ? reinterpret_cast<hipEvent_t *>(&mp->ev[2]) : nullptr;
+  hipError_t e = p->window > 0 ? launch_bwd_window(p, q, k, v, o, d_o, lse, dq, dk, dv, ws, st, ev)
+                               : launch_bwd(fused ? p : use, q, k, v, o, d_o, lse, dq, dk, dv, ws, split, fused, st, ev);
   if (e != hipSuccess) return hip_fail("backward launch", e);
   if (p->profile) mp->ev_bwd = true;
   return CA_OK;

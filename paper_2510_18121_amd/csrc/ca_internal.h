@@ -18,6 +18,11 @@ constexpr int FWD_BN = 64;   // keys per forward inner step
 constexpr int BWD_BN = 128;  // keys owned by one backward work unit (4 waves x 32)
 constexpr int BWD_BQ = 64;   // query rows per backward inner step
 
+// A windowed plan (attention with a sliding window and sinks): a row at document position p sees the keys j <= min(p, kv_len - 1)
+// with j > p - window or j < sinks.  slot_pos holds the last of them, slot_lo where the row's window begins (one behind slot_pos
+// where it is empty); key0 of a forward unit is where the unit's window tiles begin, positions and n_keys are absolute.  All units
+// are head-packed (rows of few positions and many heads waste least on the window's edges), and slots are padded wherever windows no longer overlap.
+
 // One workgroup of the forward / dQ kernels, or two (halves; always in the joint backward launch): 8 row groups of 32 slots, one or
 // two to a wave.  A full tile of a document is 256 slots of one query head (hp = 1).  The slots a document has left over
 // after its full tiles are covered by head-packed units instead: 256 / hp slots of hp consecutive query heads of one KV
@@ -55,6 +60,12 @@ struct BwdUnit {  // one (KV tile, KV head)
   // (block, head) tiles per query block: the heads of the KV group, or fewer where a document of at most 32 rows has
   // the rows of 2 or 4 heads packed into each 64-row tile (the heads of a group add into the same dK and dV)
   int32_t heads;
+};
+// A unit of a windowed plan.  Its query blocks from slot_edge on (slot_full <= slot_edge) hold rows whose windows begin behind the
+// tile's first key: they need a mask too.  Those of a tile with sinks go on to the document's last row.
+struct WindowUnit : BwdUnit {
+  int32_t slot_edge;
+  int32_t spare;
 };
 // A piece of a unit's query blocks (see CombineUnit) runs alone, and its `follow` is -1 - (block of partial results).
 
@@ -136,6 +147,13 @@ struct ca_plan {
   size_t ws_fwd = 0, ws_bwd = 0, ws_off_l2 = 0, ws_off_qs = 0, ws_off_dos = 0;
   size_t ws_off_stats_kv = 0;  // the row statistics once more: [block][head][half of 32 rows of the dK/dV tile][log2e*LSE, -Delta][32]
   bool q_covered = false, kv_covered = false;  // every packed Q row / KV row belongs to some unit
+  // windowed plans
+  int64_t window = 0;  // 0: none
+  int32_t sinks = 0;
+  std::vector<int32_t> slot_lo;
+  std::vector<ca::WindowUnit> window_units;  // in place of bwd_units; long ones cut into pieces whose parts are part of ws_bwd
+  const int32_t *d_slot_lo = nullptr;
+  const ca::WindowUnit *d_window_units = nullptr;
   // device copies
   int device = -1;
   void *d_blob = nullptr;  // one allocation that holds all of the arrays below
@@ -153,5 +171,5 @@ struct ca_plan {
 
 namespace ca {
 void set_error(const std::string &msg);
-int build_plan(const ca_batch_desc *desc, ca_plan_t **out);  // host only
+int build_plan(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out);  // host only; window 0: none
 }  // namespace ca

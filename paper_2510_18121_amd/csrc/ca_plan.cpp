@@ -16,6 +16,7 @@
 #include <sstream>
 
 #include "ca_internal.h"
+#include "ca_plan_window.h"
 
 namespace ca {
 
@@ -562,18 +563,6 @@ bool schedule(ca_plan_t *p, bool beyond_static) {
   for (size_t blk = 0; blk < p->block_rpk.size(); ++blk)
     if (const int rpk = p->block_rpk[blk])
       for (int i = 0; i < BWD_BQ; ++i) p->pos_kv[blk * BWD_BQ + i] = p->slot_pos[blk * BWD_BQ + i % rpk];
-  auto base_workspace = [&]() {
-    // workspace of backward, all in slot order: per (head, slot) fp32 -Delta and log2(e)*LSE, then bf16 copies of Q
-    // and dO as [block of 64 slots][head][64][head_dim] (the dK/dV kernel re-reads their 64-slot tiles once per 128-key
-    // tile: in this layout a tile is one contiguous run and needs no row indices)
-    const size_t per = (size_t(padded) * hq * sizeof(float) + 255) / 256 * 256;
-    const size_t copy = (size_t(padded) * hq * p->d * 2 + 255) / 256 * 256;
-    p->ws_off_l2 = per;
-    p->ws_off_qs = 2 * per;
-    p->ws_off_dos = 2 * per + copy;
-    p->ws_off_stats_kv = 2 * per + 2 * copy;
-    return 4 * per + 2 * copy;
-  };
   // Partial results are bounded: at most this much more than whole units need, and, unless beyond_static, no more than what the
   // library's static workspace has left over (at 8 query heads of 128 it holds 15.8K rows, so from 8K rows on too little to cut
   // with: forward + backward of 9K rows, 8/1 heads, 1.75 ms with what is left and 0.85 ms with 256 MiB).
@@ -648,7 +637,7 @@ bool schedule(ca_plan_t *p, bool beyond_static) {
       }
     };
     lay_out(chains, btiles, p->bwd_units, {}, p->bwd_workgroups);
-    p->ws_bwd = base_workspace();
+    p->ws_bwd = backward_layout(p);
     // the list in which long units that run alone are cut along their query blocks
     cut_budget = p->ws_bwd <= CA_STATIC_WS_BYTES && !beyond_static ? CA_STATIC_WS_BYTES - p->ws_bwd : MAX_CUT_BYTES;
     limits = {cut_budget, MAX_CUT_BYTES};
@@ -939,15 +928,39 @@ std::unique_ptr<ca_plan_t> described(const ca_batch_desc *desc) {
 }
 }  // namespace
 
-int build_plan(const ca_batch_desc *desc, ca_plan_t **out) {
+size_t backward_layout(ca_plan_t *p) {
+  // workspace of backward, all in slot order: per (head, slot) fp32 -Delta and log2(e)*LSE, then bf16 copies of Q
+  // and dO as [block of 64 slots][head][64][head_dim] (the dK/dV kernel re-reads their 64-slot tiles once per 128-key
+  // tile: in this layout a tile is one contiguous run and needs no row indices)
+  const size_t padded = p->slot_row.size();
+  const size_t per = (padded * p->hq * sizeof(float) + 255) / 256 * 256;
+  const size_t copy = (padded * p->hq * p->d * 2 + 255) / 256 * 256;
+  p->ws_off_l2 = per;
+  p->ws_off_qs = 2 * per;
+  p->ws_off_dos = 2 * per + copy;
+  p->ws_off_stats_kv = 2 * per + 2 * copy;
+  return 4 * per + 2 * copy;
+}
+
+int build_plan(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out) {
   if (!out) {
     set_error("output plan pointer is null");
     return CA_ERR_INVALID_ARG;
   }
   *out = nullptr;
   try {
+    CA_REQUIRE(window >= 0 && sinks >= 0, CA_ERR_INVALID_ARG, "negative window or sinks");
     validate(desc);
     auto p = described(desc);
+    // (a window that hides nothing from any row is none)
+    int64_t last = -1;
+    for (int t = 0; t < desc->n_tasks; ++t) last = std::max(last, desc->task_q_pos[t] + desc->task_q_len[t] - 1);
+    if (window > 0 && last >= window) {
+      p->window = window, p->sinks = int32_t(std::min<int64_t>(sinks, int64_t(1) << 30));
+      CA_REQUIRE(schedule_window(p.get()), CA_ERR_UNSUPPORTED, "too many padded query rows");
+      *out = p.release();
+      return CA_OK;
+    }
     // Where cutting units beyond the static workspace looks better by a tenth, or would save a backward launch worth it (the dQ parts
     // take the place of the dK/dV parts inside, which needs two), or leaves room for two long forward pieces per CU, both plans are
     // made, and kept if the whole pass is better: the larger for callers that bring the workspace, the smaller inside it for all others.  (Forward + backward, 8/2 heads,
@@ -988,7 +1001,16 @@ static int64_t leading_fields(const std::vector<T> &list, int32_t *out, size_t n
 
 extern "C" {
 
-int ca_plan_host(const ca_batch_desc *desc, ca_plan_t **out) { return ca::build_plan(desc, out); }
+int ca_plan_host(const ca_batch_desc *desc, ca_plan_t **out) { return ca::build_plan(desc, 0, 0, out); }
+
+int ca_plan_window_host(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out) {
+  if (window < 1 && out) {
+    *out = nullptr;
+    ca::set_error("window must be at least 1");
+    return CA_ERR_INVALID_ARG;
+  }
+  return ca::build_plan(desc, window, sinks, out);
+}
 
 const char *ca_last_error(void) { return ca::last_error(); }
 
@@ -1019,7 +1041,7 @@ int ca_plan_info(const ca_plan_t *p, int64_t *out, int n) {
   int64_t full_tiles = 0;
   for (auto &u : p->fwd_units) full_tiles += u.hp == 1 && u.head == 0;
   const int64_t v[19] = {ca::FWD_BM, full_tiles, int64_t(p->fwd_units.size()),
-                         ca::BWD_BN, int64_t(p->bwd_units.size()), ca::FWD_BN, int64_t(p->slot_row.size()),
+                         ca::BWD_BN, int64_t(p->window > 0 ? p->window_units.size() : p->bwd_units.size()), ca::FWD_BN, int64_t(p->slot_row.size()),
                          p->fwd_steps, p->bwd_steps, ca::BWD_BQ, p->slot_align, p->heads_packed, p->bwd_workgroups,
                          p->joint, p->fwd_form.halves, p->fwd_piece_form.halves, p->fwd_form.turns, p->fwd_piece_form.turns, p->fused};
   for (int i = 0; i < n && i < 19 && out; ++i) out[i] = v[i];
@@ -1038,8 +1060,18 @@ int64_t ca_plan_fwd_units(const ca_plan_t *p, int32_t *units) {
   return leading_fields(p->fwd_units, units, ca::FWD_UNIT_INTS);
 }
 
+int64_t ca_plan_window_units(const ca_plan_t *p, int32_t kind, int32_t *out) {
+  if (!p || p->window == 0) return 0;
+  if (kind == 0) return leading_fields(p->fwd_units, out, sizeof(ca::FwdUnit) / 4);
+  if (kind == 1) return leading_fields(p->window_units, out, sizeof(ca::WindowUnit) / 4);
+  if (kind != 2) return 0;
+  if (out) std::copy(p->slot_lo.begin(), p->slot_lo.end(), out);
+  return int64_t(p->slot_lo.size());
+}
+
 int64_t ca_plan_bwd_units(const ca_plan_t *p, int32_t *units) {
   if (!p) return 0;
+  if (p->window > 0) return leading_fields(p->window_units, units, sizeof(ca::BwdUnit) / 4);
   return leading_fields(p->bwd_units, units, sizeof(ca::BwdUnit) / 4);
 }
 

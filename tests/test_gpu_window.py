@@ -1,0 +1,182 @@
+"""Attention with a sliding window and sinks on the GPU, against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import window_util as U
+from paper_2510_18121_amd import binding as B
+from paper_2510_18121_amd import workloads as W
+from paper_2510_18121_amd.autograd import AttentionServer
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def run(b, window, sinks, tensors, backward=True, mark=None):
+    q, k, v, d_o = tensors
+    plan = B.ca_plan(b, window=window, sinks=sinks)
+    o = torch.full_like(q, mark if mark is not None else 7.0)
+    lse = torch.full((b.n_q_heads, b.total_q), 7.0, device=DEV)
+    ws = torch.full((max(*plan.workspace_bytes(), 256),), 0xFF, dtype=torch.uint8, device=DEV)  # NaN wherever something is read first
+    B.ca_forward(plan, q, k, v, o, lse, ws)
+    out = {"o": o, "lse": lse}
+    if backward:
+        out |= {"dq": torch.full_like(q, 7.0), "dk": torch.full_like(k, 7.0), "dv": torch.full_like(v, 7.0)}
+        B.ca_backward(plan, q, k, v, o, d_o, lse, out["dq"], out["dk"], out["dv"], ws)
+    return out
+
+
+def check(b, window, sinks, got, tensors):
+    q, k, v, d_o = tensors
+    want, far = U.reference(b, window, sinks, q, k, v, d_o, got["o"])
+    U.check(got, want, far, ("o", "dq", "dk", "dv"))
+    lse = got["lse"].double().cpu()
+    none = torch.isinf(want["lse"])
+    assert (lse[none] == -np.inf).all()
+    off = (lse - want["lse"]).abs()[~none]  # fp32 sums of products: 2^-20 of a large one
+    assert (off <= 1e-4 + 2.0 ** -20 * want["lse"].abs()[~none]).all()
+    rows = none[0]
+    assert (got["o"].cpu()[rows] == 0).all() and (got["dq"].cpu()[rows] == 0).all()
+
+
+SHAPES = {
+    "documents": dict(lens=[300, 1, 777], tasks=[(0, 0, 300), (1, 0, 1), (2, 0, 777)]),
+    "shards_far_apart": dict(lens=[2500, 40], tasks=[(0, 2300, 17), (0, 3, 100), (1, 10, 30), (0, 1200, 300)]),
+    "same_positions_twice": dict(lens=[500], tasks=[(0, 100, 200), (0, 150, 300)]),
+    "clipped": dict(lens=[600], tasks=[(0, 0, 300), (0, 300, 300)], kv_lens={1: 200}),
+    "single_rows": dict(lens=[1500], tasks=[(0, 1499, 1), (0, 0, 1), (0, 77, 1)]),
+}
+
+
+@pytest.mark.parametrize("heads,d", [((4, 2), 64), ((4, 1), 128), ((3, 3), 128), ((8, 1), 64)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (17, 0), (63, 130), (64, 4), (129, 0), (400, 1)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_against_the_definition(shape, window, sinks, heads, d):
+    s = SHAPES[shape]
+    b = U.batch(s["lens"], s["tasks"], *heads, d, s.get("kv_lens"), seed=3)
+    tensors = W.make_tensors(b, DEV)
+    check(b, window, sinks, run(b, window, sinks, tensors), tensors)
+
+
+def test_windows_of_many_tiles_and_cut_sink_tiles():
+    """4000 rows, windows of 1024 keys (whole tiles without a mask), a sink tile of 252 steps in pieces."""
+    b = U.batch([4003], [(0, 0, 4003)], 8, 2, 128, seed=4)
+    tensors = W.make_tensors(b, DEV)
+    assert B.ca_plan_host(b, window=1024, sinks=4).pieces()["bwd_combine"].size > 0
+    check(b, 1024, 4, run(b, 1024, 4, tensors), tensors)
+
+
+@pytest.mark.parametrize("factor", [8.0, 60.0])
+def test_scores_that_outgrow_the_first_keys(factor):
+    """Early keys are small and later ones large: the reference of the exponentials is outgrown and rows are computed again."""
+    b = U.batch([700], [(0, 0, 700)], 4, 2, 64, seed=5)
+    q, k, v, d_o = W.make_tensors(b, DEV)
+    k = (k.float() * torch.linspace(0, factor, 700, device=DEV)[:, None, None]).to(torch.bfloat16)
+    got = run(b, 200, 2, (q, k, v, d_o))
+    check(b, 200, 2, got, (q, k, v, d_o))
+
+
+def test_rows_of_no_task_and_keys_that_nobody_sees():
+    b = U.batch([600, 100], [(0, 400, 64), (1, 0, 100)], 4, 2, 64, seed=6)
+    b.total_q += 13  # rows behind the last task
+    q, k, v, d_o = W.make_tensors(b, DEV)
+    got = run(b, 100, 0, (q, k, v, d_o), mark=5.0)
+    assert (got["o"][-13:] == 5.0).all() and (got["lse"][:, -13:] == 7.0).all() and (got["dq"][-13:] == 0).all()
+    k0 = int(b.doc_kv_start[0])
+    for n in ("dk", "dv"):
+        assert (got[n][k0:k0 + 301] == 0).all() and (got[n][k0 + 464:k0 + 600] == 0).all()
+        assert (got[n][k0 + 301:k0 + 464].abs().sum((1, 2)) > 0).all()
+
+
+def test_a_window_over_everything_is_plain_attention_bit_for_bit():
+    b = W.config(1)
+    tensors = W.make_tensors(b, DEV)
+    got, want = run(b, 1 << 33, 3, tensors), run(b, None, 0, tensors)
+    assert all(torch.equal(got[n], want[n]) for n in want)
+
+
+def test_runs_repeat_bit_for_bit_and_documents_do_not_depend_on_their_shards():
+    b = U.batch([900], [(0, 0, 900)], 8, 2, 128, seed=7)
+    tensors = W.make_tensors(b, DEV)
+    a, c = run(b, 130, 4, tensors), run(b, 130, 4, tensors)
+    assert all(torch.equal(a[n], c[n]) for n in a)
+    parts = W.custom([900], [(0, 0, 333), (0, 333, 1), (0, 334, 566)], 8, 2, 128, seed=7)
+    d = run(parts, 130, 4, tensors)
+    assert torch.equal(a["o"], d["o"]) and torch.equal(a["dq"], d["dq"]) and torch.equal(a["dk"], d["dk"])
+
+
+def test_differentiable_op_and_gradients_against_differences():
+    b = U.batch([150], [(0, 0, 150)], 2, 1, 64, seed=8)
+    q, k, v, d_o = (x.detach().clone() for x in W.make_tensors(b, DEV))
+    for x in (q, k, v):
+        x.requires_grad_()
+    server = AttentionServer(b, DEV, window=20, sinks=2)
+    o = server(q, k, v)
+    grads = torch.autograd.grad(o, (q, k, v), d_o)
+    want, far = U.reference(b, 20, 2, q, k, v, d_o, o.detach())
+    U.check(dict(zip(("dq", "dk", "dv"), grads)), want, far, ("dq", "dk", "dv"))
+    # the definition's gradient itself, by central differences of its loss in 64 bits along one direction
+    x = [t.detach().double().cpu() for t in (q, k, v)]
+    gen = torch.Generator().manual_seed(0)
+    step = [torch.randn(t.shape, generator=gen, dtype=torch.float64) for t in x]
+    loss = lambda e: (U.reference(b, 20, 2, *(t + e * u for t, u in zip(x, step)))[0]["o"] * d_o.double().cpu()).sum()  # noqa: E731
+    exact = U.reference(b, 20, 2, *x, d_o)[0]
+    slope = sum((exact[n] * u).sum() for n, u in zip(("dq", "dk", "dv"), step))
+    assert abs((loss(1e-5) - loss(-1e-5)) / 2e-5 - slope) <= 1e-6 * abs(slope) + 1e-6
+
+
+def test_replayed_from_a_graph_beside_an_eager_graph_of_the_same_leaves():
+    b = U.batch([800], [(0, 0, 800)], 8, 2, 64, seed=9)
+    q, k, v, d_o = W.make_tensors(b, DEV)
+    want = run(b, 100, 4, (q, k, v, d_o))
+    plan = B.ca_plan(b, window=100, sinks=4)
+    ws = B.alloc_workspace(plan, DEV)
+    got = {n: torch.zeros_like(x) for n, x in want.items()}
+
+    def step():
+        B.ca_forward(plan, q, k, v, got["o"], got["lse"], ws)
+        B.ca_backward(plan, q, k, v, got["o"], d_o, got["lse"], got["dq"], got["dk"], got["dv"], ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for x in got.values():
+            x.zero_()
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[n], want[n]) for n in want)
+        assert torch.equal(run(b, 100, 4, (q, k, v, d_o))["dq"], want["dq"])
+
+
+def test_too_small_a_workspace_is_refused():
+    b = U.batch([800], [(0, 0, 800)], 8, 2, 64)
+    q, k, v, d_o = W.make_tensors(b, DEV)
+    plan = B.ca_plan(b, window=100, sinks=4)
+    need = plan.workspace_bytes()[1]
+    ws = torch.empty(need - 1, dtype=torch.uint8, device=DEV)
+    lse = torch.zeros(8, 800, device=DEV)
+    with pytest.raises(B.CaError) as e:
+        B.ca_backward(plan, q, k, v, q, d_o, lse, torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), ws)
+    assert e.value.code == B.CA_ERR_WORKSPACE
+
+
+def test_kernel_times_are_read():
+    b = U.batch([800], [(0, 0, 800)], 8, 2, 64)
+    tensors = W.make_tensors(b, DEV)
+    want = run(b, 100, 0, tensors)
+    q, k, v, d_o = tensors
+    plan = B.ca_plan(b, window=100)
+    plan.profile_enable()
+    ws = B.alloc_workspace(plan, DEV)
+    got = {n: torch.zeros_like(x) for n, x in want.items()}
+    B.ca_forward(plan, q, k, v, got["o"], got["lse"], ws)
+    B.ca_backward(plan, q, k, v, got["o"], d_o, got["lse"], got["dq"], got["dk"], got["dv"], ws)
+    assert all(t > 0 for t in plan.profile_read().values())
+    assert all(torch.equal(got[n], want[n]) for n in want)
