@@ -13,7 +13,7 @@
  * All tensor pointers are DEVICE pointers owned by the caller; all descriptor arrays are HOST
  * pointers.  No entry point throws; every one returns CA_OK (0) or a negative ca_status, and ca_last_error()
  * then holds a human-readable detail for the calling thread.  The launch calls (ca_forward, ca_backward,
- * ca_merge_partials, ca_sum_partial_dq, ca_mfma_stream) never synchronise the device; ca_plan waits for its own
+ * ca_merge_partials, ca_sum_partial_dq, ca_cache_*, ca_mfma_stream) never synchronise the device; ca_plan waits for its own
  * upload and ca_profile_read for the events it reads.  A plan is read-only for the launch calls and may serve several
  * host threads and streams at once, each launch with a workspace of its own (while profiling is enabled on it, one
  * thread and one stream at a time: the timing events belong to the plan).
@@ -207,6 +207,70 @@ int ca_merge_partials(const int32_t *part_rows, int64_t n_rows, int32_t n_parts,
  */
 int ca_sum_partial_dq(const int32_t *part_rows, int64_t n_rows, int32_t n_parts, const void *dq_part,
                       int64_t total_q_part, void *dq, int32_t n_q_heads, int32_t head_dim, void *hip_stream);
+
+/*
+ * A paged cache of keys and values in 8 bits, for answering with a model: its contexts are held in pages of CA_CACHE_PAGE_TOKENS tokens
+ * and attended by single new tokens or by chunks of a prompt.
+ * A page holds, for each KV head, the keys as e4m3 codes [64][head_dim], the values as e4m3 codes [head_dim][64] (token fastest), and one
+ * fp32 scale each; a code stands for code * scale.  ca_cache is a description in host memory; what it points to is device memory
+ * of the caller's, k and v 16-byte aligned:
+ *   k       : [n_pages][n_kv_heads][64][head_dim]     k_scale, v_scale : [n_pages][n_kv_heads]
+ *   v       : [n_pages][n_kv_heads][head_dim][64]
+ */
+#define CA_CACHE_PAGE_TOKENS 64
+typedef struct {
+  int32_t n_pages, n_kv_heads, head_dim; /* head_dim 64 or 128; n_kv_heads at most 1024 */
+  void *k, *v;
+  float *k_scale, *v_scale;
+} ca_cache;
+
+/*
+ * The sequences of a call.  The three arrays are DEVICE memory, read when the kernels run, so that a captured graph follows them.
+ * Sequence s has the rows q_start[s] .. q_start[s + 1] - 1 of the packed tensors (K and V to append, or queries); with n of them they
+ * sit at its positions kv_len[s] - n .. kv_len[s] - 1: kv_len counts the cached tokens, those of this call among them.  Token j of s
+ * is token j % 64 of page page_table[s][j / 64].  A page id outside [0, n_pages) is no page: nothing is written for its tokens,
+ * and nobody sees them.  Lengths beyond the table and rows beyond total_rows count as far as these go; rows of no sequence are left
+ * as they are.  At most 4096 sequences.
+ */
+typedef struct {
+  int32_t n_seqs, table_width;
+  int64_t total_rows;
+  const int32_t *q_start;    /* [n_seqs + 1], not descending */
+  const int32_t *kv_len;     /* [n_seqs] */
+  const int32_t *page_table; /* [n_seqs][table_width] */
+} ca_cache_batch;
+
+/*
+ * ca_cache_append: quantises the rows of k and v (device bf16 [total_rows][n_kv_heads][head_dim]) into the pages of their sequences.
+ * The scale of a (page, head) becomes the smallest power of two, at least 2^-126, that is no less than (largest finite magnitude of
+ * the new tokens) / 448 and, unless the page's token 0 is among the new ones (what the page held before is forgotten then), no less
+ * than the scale it has.  New codes are value / scale to the nearest, ties to even (Inf and NaN become NaN); where the scale has grown the
+ * page's other codes (all 64 tokens) are rounded again, from code * old / new.  Between two powers of two that is exact but for
+ * codes that leave the normal range of e4m3.  A page belongs to one sequence of the call: pages that are shared are copied first.
+ * One launch on hip_stream; allocates nothing, never synchronises.
+ */
+int ca_cache_append(const ca_cache *cache, const ca_cache_batch *batch, const void *k, const void *v, void *hip_stream);
+
+/*
+ * ca_cache_attend: O = softmax(softmax_scale Q K^T) V over the cached tokens of each row's sequence: the row at position p sees the
+ * tokens j <= p (itself among them: append first), with a window (>= 1; 0: none) only those with p - j < window or j < sinks.
+ * q, o: device bf16 [total_rows][n_q_heads][head_dim]; lse: device fp32 [n_q_heads][total_rows], or NULL.  softmax_scale <= 0 selects
+ * 1/sqrt(head_dim).  A row that sees nothing gets O = 0 and LSE = -inf.  Tokens that no row of a tile of rows sees may hold anything
+ * (pages that have left every window may be freed and their table entries set to -1); tokens that only some rows see are finite.
+ * ws: device workspace of ca_cache_attend_workspace_bytes, 256-byte aligned, written; calls that may overlap in time need one each.
+ * Two launches on hip_stream; allocates nothing, never synchronises, bit-reproducible.  How the work is split, and with it the last bits of
+ * a row's result, depends on the whole batch.
+ */
+int ca_cache_attend(const ca_cache *cache, const ca_cache_batch *batch, int32_t n_q_heads, float softmax_scale, int64_t window,
+                    int64_t sinks, const void *q, void *o, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+int ca_cache_attend_workspace_bytes(const ca_cache *cache, int32_t n_q_heads, size_t *bytes);
+
+/*
+ * ca_cache_copy_pages: copies page src[i] to page dst[i] (DEVICE int32 [n]; all heads, keys, values and scales), for i < n: the shared last
+ * page of a forked sequence, or the pages that a compaction moves.  No page is written twice, and none that is written is read by
+ * another pair.  Pairs with an id outside [0, n_pages) are skipped.  One launch on hip_stream; allocates nothing, never synchronises.
+ */
+int ca_cache_copy_pages(const ca_cache *cache, const int32_t *src, const int32_t *dst, int64_t n, void *hip_stream);
 
 /*
  * Per-kernel timing for profilers and cost models (Section 4.2's profiler benchmarks core attention over

@@ -42,6 +42,13 @@ class BatchDesc(ctypes.Structure):
     ]
 
 
+class CacheBatch(ctypes.Structure):
+    """ca_cache_batch of include/ca_attention.h."""
+
+    _fields_ = [("n_seqs", ctypes.c_int32), ("table_width", ctypes.c_int32), ("total_rows", ctypes.c_int64),
+                ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
 def lib() -> ctypes.CDLL:
     """The loaded C-ABI library; raises if it has not been built (python -m paper_2510_18121_amd.build)."""
     global _lib
@@ -85,6 +92,10 @@ def lib() -> ctypes.CDLL:
         i32, i64 = ctypes.c_int32, ctypes.c_int64
         L.ca_merge_partials.argtypes = [vp, i64, i32, vp, vp, i64, vp, vp, vp, vp, i32, i32, vp]
         L.ca_sum_partial_dq.argtypes = [vp, i64, i32, vp, i64, vp, i32, i32, vp]
+        L.ca_cache_append.argtypes = [vp] * 5
+        L.ca_cache_attend.argtypes = [vp, vp, i32, ctypes.c_float, i64, i64, vp, vp, vp, vp, sz, vp]
+        L.ca_cache_attend_workspace_bytes.argtypes = [vp, i32, ctypes.POINTER(sz)]
+        L.ca_cache_copy_pages.argtypes = [vp, vp, vp, i64, vp]
         L.ca_mfma_stream.argtypes = L.ca_mfma_stream16.argtypes = [vp, i64, i32, i32, vp, vp]
         L.ca_xcd_map.argtypes = [i32, i32, vp, vp]
         L.ca_atomic_stream.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp]
@@ -378,6 +389,77 @@ def ca_sum_partial_dq(part_rows, dq_part, dq, stream=None):
     _expect(dq_part, (tq, hq, d), torch.bfloat16, "dq_part")
     _expect(dq, (n_rows, hq, d), torch.bfloat16, "dq")
     _check(lib().ca_sum_partial_dq(_p(part_rows), n_rows, n_parts, _p(dq_part), tq, _p(dq), hq, d, _stream_ptr(stream)))
+
+
+def _cache_batch(cache, rows, q_start, kv_len, page_table) -> CacheBatch:
+    import torch
+    n = kv_len.shape[0]
+    if page_table.dim() != 2:
+        raise ValueError(f"page_table: expected [{n}, pages], got {tuple(page_table.shape)}")
+    for t, shape, name in ((q_start, (n + 1,), "q_start"), (kv_len, (n,), "kv_len"), (page_table, (n, page_table.shape[1]), "page_table")):
+        _expect(t, shape, torch.int32, name)
+        if t.device != cache.device:
+            raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
+    return CacheBatch(n, page_table.shape[1], rows, _p(q_start), _p(kv_len), _p(page_table))
+
+
+def _expect_on(cache, t, shape, dtype, name):
+    _expect(t, shape, dtype, name)
+    if t.device != cache.device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
+
+
+def _current(cache):
+    """The cache's memory is on the current device (the streams of another would not order the work with its own)."""
+    import torch
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, the current device is {torch.cuda.current_device()}")
+
+
+def ca_cache_append(cache, k, v, q_start, kv_len, page_table, stream=None):
+    """Quantise the rows of k and v (bf16 [rows, n_kv_heads, head_dim]) into the pages of their sequences (cache: cache.KVCache; the
+    arrays: device int32, see the header).  On torch's current stream, or `stream`."""
+    import torch
+    for t, name in ((k, "k"), (v, "v")):
+        _expect_on(cache, t, (k.shape[0], cache.n_kv_heads, cache.head_dim), torch.bfloat16, name)
+    b = _cache_batch(cache, k.shape[0], q_start, kv_len, page_table)
+    _current(cache)
+    _check(lib().ca_cache_append(ctypes.byref(cache.desc), ctypes.byref(b), _p(k), _p(v), _stream_ptr(stream)))
+
+
+def ca_cache_attend(cache, q, o, lse, q_start, kv_len, page_table, ws, window=None, sinks=0, softmax_scale=0.0, stream=None):
+    """Attention of the rows of q (bf16 [rows, n_q_heads, head_dim]) over the cached tokens of their sequences.  Writes o (like q) and,
+    unless it is None, lse (fp32 [n_q_heads, rows]); ws: alloc_cache_workspace."""
+    import torch
+    rows, hq, _ = q.shape
+    _expect_on(cache, q, (rows, hq, cache.head_dim), torch.bfloat16, "q")
+    _expect_on(cache, o, q.shape, torch.bfloat16, "o")
+    if lse is not None:
+        _expect_on(cache, lse, (hq, rows), torch.float32, "lse")
+    if window is not None and operator.index(window) < 1:
+        raise ValueError(f"window {window}: at least 1, or None")
+    b = _cache_batch(cache, rows, q_start, kv_len, page_table)
+    _current(cache)
+    _check(lib().ca_cache_attend(ctypes.byref(cache.desc), ctypes.byref(b), hq, float(softmax_scale), 0 if window is None else operator.index(window),
+                                 operator.index(sinks), _p(q), _p(o), _p(lse), _p(ws), ws.numel() * ws.element_size() if ws is not None else 0,
+                                 _stream_ptr(stream)))
+
+
+def ca_cache_copy_pages(cache, src, dst, stream=None):
+    """Copy page src[i] of the cache to page dst[i] (device int32 [n]; no page is written twice or both written and read)."""
+    import torch
+    for t, name in ((src, "src"), (dst, "dst")):
+        _expect_on(cache, t, (src.shape[0],), torch.int32, name)
+    _current(cache)
+    _check(lib().ca_cache_copy_pages(ctypes.byref(cache.desc), _p(src), _p(dst), src.shape[0], _stream_ptr(stream)))
+
+
+def alloc_cache_workspace(cache, n_q_heads, device=None):
+    """A torch uint8 buffer big enough for ca_cache_attend on that cache.  Calls that may overlap in time need one each."""
+    import torch
+    n = ctypes.c_size_t()
+    _check(lib().ca_cache_attend_workspace_bytes(ctypes.byref(cache.desc), operator.index(n_q_heads), ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=cache.device if device is None else device)
 
 
 def ca_mfma_stream(operands, n_mfma_per_wave, sums, side_work=0, stream=None, shape=32):

@@ -1,0 +1,714 @@
+// A paged cache of keys and values in 8 bits, and the attention that reads it (serving: single tokens and chunks of prompts).
+//
+// A page holds 64 tokens.  Of a page and KV head: the keys as e4m3 codes [64][D], the values as e4m3 codes [D][64], and one fp32
+// scale each; a code stands for code * scale.  With that layout every operand of the two products is a run of 16 bytes per lane
+// straight from global memory, with no transposition and no trip through LDS:
+//   S^T = K Q^T (v_mfma_f32_16x16x32_bf16, 16 keys x 16 rows): row i of tile t of a page is key 16 (i / 4) + 4 t + i % 4, so that lane
+//   (r, j) of the results holds keys 16 j .. 16 j + 15 of query row r, in order, over the four tiles;
+//   O^T += V^T P^T: the probabilities of two tiles are the B operand as they stand, and the lane's A operand is 8 consecutive
+//   tokens of a V^T row.
+// e4m3 is exact in bf16; the scales go into the exponent's factor (K) and into the probabilities (V).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <climits>
+#include <sstream>
+
+#include "ca_device.h"
+#include "ca_internal.h"
+#include "ca_launch.h"
+
+namespace ca {
+
+constexpr int PAGE = CA_CACHE_PAGE_TOKENS;
+static_assert(PAGE == 64);
+constexpr int MAX_SEQS = 4096;  // their prefix sums lie in LDS
+constexpr float NO_MAX = -3.402823466e38f;
+
+// ------------------------------------------------------------------------------------------------ sequences
+// The batch as the kernels see it.  What the device arrays say is clamped to the tensors' sizes: no value reads or writes beyond them.
+struct SeqArgs {
+  const int32_t *q_start, *kv_len, *table;
+  int n_seqs, width, total, n_pages;
+};
+struct Seq {
+  int row0, n, len;  // rows row0 .. row0 + n - 1, at positions len - n .. len - 1
+};
+__device__ __forceinline__ Seq seq_of(const SeqArgs &a, int s) {
+  Seq q;
+  q.row0 = min(max(a.q_start[s], 0), a.total);
+  q.n = min(max(a.q_start[s + 1], q.row0), a.total) - q.row0;
+  q.len = min(max(a.kv_len[s], 0), a.width * PAGE);
+  return q;
+}
+
+// pre[i] = sum of units(0) .. units(i - 1), for all threads of the workgroup; returns the whole sum.  (Sums stop growing at MOST_UNITS:
+// only sequences that overlap, against their description, come so far, and then nothing overflows.)
+constexpr int MOST_UNITS = (1 << 30) - 1;
+__device__ __forceinline__ int sum_units(int a, int b) { return min(a + b, MOST_UNITS); }
+template <int T, class F>
+__device__ __forceinline__ int block_prefix(int *pre, int *wave_sums, int n, F units) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int carry = 0;
+  for (int base = 0; base < n; base += T) {
+    const int i = base + int(threadIdx.x);
+    int x = i < n ? units(i) : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(x, o);
+      if (lane >= o) x = sum_units(x, y);
+    }
+    if (lane == 63) wave_sums[wave] = x;
+    __syncthreads();
+    int before = carry;
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) {
+      before = sum_units(before, w < wave ? wave_sums[w] : 0);
+      carry = sum_units(carry, wave_sums[w]);
+    }
+    if (i < n) pre[i + 1] = sum_units(before, x);
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) pre[0] = 0;
+  __syncthreads();
+  return carry;
+}
+// the entry whose run of units holds unit u < pre[n]
+__device__ __forceinline__ int find_unit(const int *pre, int n, int u) {
+  int lo = 0, hi = n;  // pre[lo] <= u < pre[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (pre[mid] <= u) lo = mid;
+    else hi = mid;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+struct AttendArgs {
+  SeqArgs s;
+  const uint8_t *k, *v;
+  const float *k_scale, *v_scale;
+  const bf16_t *q;
+  bf16_t *o;
+  float *lse;
+  float *parts;  // [worker][2][KV head][R rows][D] and then [R][2] {running maximum, sum}
+  int4 *heads;   // [worker][KV head]: {parts of the tile that begins in this worker and is cut, its sequence, its tile, -}
+  int hq, hkv, window, sinks;
+  float c;  // softmax_scale * log2(e)
+};
+
+// Rows of a sequence and KV head, token by token and then by head of the group, make up tiles of R = 16 NR; a unit of work is a page
+// of a tile.  The units of all sequences, in order, are dealt to the workers in equal runs, whatever the sequences' lengths
+// are; a run that ends inside a tile of at most CUT pages is moved to the tile's nearer end, longer tiles are cut.
+constexpr int CUT = 24;
+__device__ __forceinline__ int tile_pages(int len, int R, int G, int window, int sinks) {
+  const int pages = (len + PAGE - 1) / PAGE;
+  if (window >= len) return max(1, pages);
+  const int tokens = (R + G - 2) / G + 1;  // at most, of a tile
+  return max(1, min(pages, (sinks + PAGE - 1) / PAGE + (window + tokens - 2) / PAGE + 2));
+}
+
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b) {
+  typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+  const v2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+  const v2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+  return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+}
+
+template <int D, int NR, int W>
+struct AttendShape {
+  static constexpr int R = 16 * NR, CW = NR == 1 ? D : 32, ROW = CW + 4;
+  static constexpr int MERGE = (W * R * ROW + W * R * 2) * 4;
+  static constexpr size_t smem(int n_seqs) { return size_t(n_seqs + 1 + 3) / 4 * 16 + 64 + MERGE; }
+};
+
+template <int D, int NR, int W>
+__global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kernel(const AttendArgs a) {
+  using S = AttendShape<D, NR, W>;
+  constexpr int R = S::R, NH = D / 64, NB = D / 16;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  int *const pre = reinterpret_cast<int *>(smem), *const wave_sums = pre + (a.s.n_seqs + 4) / 4 * 4;
+  float *const merge = reinterpret_cast<float *>(wave_sums + 16), *const merge_ml = merge + W * R * S::ROW;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j4 = lane >> 4, li = lane & 15;
+  const int G = a.hq / a.hkv, hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv, n_workers = gridDim.x / a.hkv;
+
+  const int total = __builtin_amdgcn_readfirstlane(block_prefix<64 * W>(pre, wave_sums, a.s.n_seqs, [&](int s) {
+    const Seq q = seq_of(a.s, s);
+    return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, a.window, a.sinks);
+  }));
+  const int run = max(W, (total + n_workers - 1) / n_workers);
+  auto bound = [&](int w) {
+    const int u = min(w, (total + run - 1) / run) * run;
+    if (u >= total || u == 0) return min(u, total);
+    const int s = find_unit(pre, a.s.n_seqs, u), n = tile_pages(seq_of(a.s, s).len, R, G, a.window, a.sinks);
+    const int into = (u - pre[s]) % n;
+    return n > CUT ? u : 2 * into < n ? u - into : u - into + n;
+  };
+  const int begin = __builtin_amdgcn_readfirstlane(bound(worker)), end = __builtin_amdgcn_readfirstlane(bound(worker + 1));
+  int4 head = {0, 0, 0, 0};
+
+  for (int u = begin, s = begin < end ? find_unit(pre, a.s.n_seqs, begin) : 0; u < end;) {
+    while (pre[s + 1] <= u) ++s;
+    s = __builtin_amdgcn_readfirstlane(s);
+    const Seq q = seq_of(a.s, s);
+    const int per_tile = tile_pages(q.len, R, G, a.window, a.sinks);
+    const int tile = __builtin_amdgcn_readfirstlane((u - pre[s]) / per_tile), first = __builtin_amdgcn_readfirstlane((u - pre[s]) % per_tile);
+    const int n = min(end - u, per_tile - first);
+    u += n;
+    // the rows
+    const int last_row = min((tile + 1) * R, q.n * G) - 1, pos0 = q.len - q.n;
+    const int p0 = pos0 + tile * R / G, p1 = pos0 + last_row / G;  // of the tile's first and last row
+    const int from = max(0, p0 - a.window + 1);                    // the first key of a window that some row has
+    const int n_sink = min((a.sinks + PAGE - 1) / PAGE, from / PAGE);
+    int hi[NR], lo[NR];
+    bf16x8 qf[2 * NH][NR];
+#pragma unroll
+    for (int rg = 0; rg < NR; ++rg) {
+      const int r = tile * R + 16 * rg + li, ok = r <= last_row, i = ok ? r / G : 0, h = hk * G + (ok ? r - i * G : 0);
+      hi[rg] = ok ? pos0 + i : -1, lo[rg] = max(0, pos0 + i - a.window + 1);
+      const bf16_t *const qp = a.q + (size_t(q.row0 + i) * a.hq + h) * D + 16 * j4;
+#pragma unroll
+      for (int f = 0; f < 2 * NH; ++f) qf[f][rg] = *reinterpret_cast<const bf16x8 *>(qp + 64 * (f >> 1) + 8 * (f & 1));
+    }
+    f32x4 acc[NB][NR];
+    float m[NR], l[NR];
+#pragma unroll
+    for (int rg = 0; rg < NR; ++rg) {
+      m[rg] = NO_MAX, l[rg] = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b][rg] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // pages first + wave, first + wave + W, ..: their ids and scales, 64 at a time, one per lane
+    const int n_mine = (n - wave + W - 1) / W;
+    for (int base = 0; base < n_mine; base += 64) {
+      int id = -1, at = 0;
+      float ks = 0.f, vs = 0.f;
+      if (base + lane < n_mine) {
+        const int i = first + wave + W * (base + lane);
+        at = i < n_sink ? i : from / PAGE + i - n_sink;
+        if (at * PAGE <= p1) id = a.s.table[size_t(s) * a.s.width + at];
+        if (id >= a.s.n_pages) id = -1;
+        if (id >= 0) ks = a.k_scale[size_t(id) * a.hkv + hk] * a.c, vs = a.v_scale[size_t(id) * a.hkv + hk];
+      }
+      uint64_t left = __ballot(id >= 0);
+      const uint32_t k_lane = uint32_t(16 * (li >> 2) + (li & 3)) * D + 16 * j4, v_lane = uint32_t(li) * PAGE + 16 * j4;
+      u32x4 kr[4 * NH], vr[NB];
+      auto load_k = [&](int i) {
+        const uint8_t *const p = a.k + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
+#pragma unroll
+        for (int f = 0; f < 4 * NH; ++f) kr[f] = *reinterpret_cast<const u32x4 *>(p + k_lane + 4 * (f / NH) * D + 64 * (f % NH));
+      };
+      if (left) load_k(__builtin_ctzll(left));
+      while (left) {
+        const int i = __builtin_ctzll(left);
+        left &= left - 1;
+        const uint8_t *const vp = a.v + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) vr[b] = *reinterpret_cast<const u32x4 *>(vp + v_lane + 16 * PAGE * b);
+        const int key0 = __builtin_amdgcn_readlane(at, i) * PAGE;
+        const float ksi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), i));
+        const float vsi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), i));
+        f32x4 x[4][NR];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int f = 0; f < NH; ++f) {
+            const u32x4 w = kr[t * NH + f];
+            const bf16x8 k0 = codes_to_bf16(w[0], w[1]), k1 = codes_to_bf16(w[2], w[3]);
+#pragma unroll
+            for (int rg = 0; rg < NR; ++rg) {
+              x[t][rg] = mfma16(k0, qf[2 * f][rg], f == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x[t][rg]);
+              x[t][rg] = mfma16(k1, qf[2 * f + 1][rg], x[t][rg]);
+            }
+          }
+        if (left) load_k(__builtin_ctzll(left));  // of the next page
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int rg = 0; rg < NR; ++rg)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[t][rg][e] *= ksi;
+        // some row does not see some key: lane (r, j) holds keys key0 + 16 j + 4 t + e
+        if (key0 + PAGE - 1 > p0 || (key0 < p1 - a.window + 1 && key0 + PAGE > a.sinks)) {
+          const int key = key0 + 16 * j4;
+#pragma unroll
+          for (int rg = 0; rg < NR; ++rg)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int j = key + 4 * t + e;
+                x[t][rg][e] = j <= hi[rg] && (j >= lo[rg] || j < a.sinks) ? x[t][rg][e] : -INFINITY;
+              }
+          // values of tokens that no row sees count nothing, whatever stands there
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t keep = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int j = key + 4 * w + e;
+              keep |= j <= p1 && (j >= from || j < a.sinks) ? 0xFFu << (8 * e) : 0u;
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) vr[b][w] &= keep;
+          }
+        }
+        bf16x8 pb[2][NR];
+#pragma unroll
+        for (int rg = 0; rg < NR; ++rg) {
+          float top = x[0][rg][0];
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, x[t][rg][e]);
+          // the reference moves when some row's maximum has grown by more than 2^8 (see the forward kernel)
+          if (__any(top > m[rg] + 8.f)) {
+            const float grown = fmaxf(m[rg], quad_max(top)), f = m[rg] == NO_MAX ? 0.f : fast_exp2(m[rg] - grown);
+            m[rg] = grown, l[rg] *= f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) acc[b][rg] *= f;
+          }
+          uint32_t w[2][4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            float p[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = fast_exp2(x[t][rg][e] - m[rg]);
+            l[rg] += (p[0] + p[1]) + (p[2] + p[3]);
+            w[t >> 1][2 * (t & 1)] = pack_bf16(p[0] * vsi, p[1] * vsi), w[t >> 1][2 * (t & 1) + 1] = pack_bf16(p[2] * vsi, p[3] * vsi);
+          }
+          pb[0][rg] = __builtin_bit_cast(bf16x8, u32x4{w[0][0], w[0][1], w[0][2], w[0][3]});
+          pb[1][rg] = __builtin_bit_cast(bf16x8, u32x4{w[1][0], w[1][1], w[1][2], w[1][3]});
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const bf16x8 v0 = codes_to_bf16(vr[b][0], vr[b][1]), v1 = codes_to_bf16(vr[b][2], vr[b][3]);
+#pragma unroll
+          for (int rg = 0; rg < NR; ++rg) {
+            acc[b][rg] = mfma16(v0, pb[0][rg], acc[b][rg]);
+            acc[b][rg] = mfma16(v1, pb[1][rg], acc[b][rg]);
+          }
+        }
+      }
+    }
+    // The waves' sums meet in LDS, CW columns at a time.  A tile that this worker has from its first page to its last is done; of
+    // any other the sums go to the workspace.
+#pragma unroll
+    for (int rg = 0; rg < NR; ++rg) {
+      const float sum = quad_sum(l[rg]);
+      if (j4 == 0) merge_ml[(wave * R + 16 * rg + li) * 2] = m[rg], merge_ml[(wave * R + 16 * rg + li) * 2 + 1] = sum;
+    }
+    __syncthreads();
+    const bool whole = n == per_tile;
+    const int slot = first == 0 ? 1 : 0;
+    float *const part = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2));
+    if (!whole && slot == 1) head = int4{(u - n + per_tile - 1) / run - worker + 1, s, tile, 0};
+    float factor[NR];
+#pragma unroll
+    for (int rg = 0; rg < NR; ++rg) {
+      float top = NO_MAX;
+#pragma unroll
+      for (int w = 0; w < W; ++w) top = fmaxf(top, merge_ml[(w * R + 16 * rg + li) * 2]);
+      factor[rg] = m[rg] == NO_MAX ? 0.f : fast_exp2(m[rg] - top);
+    }
+    for (int c0 = 0; c0 < D; c0 += S::CW) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        if (S::CW == D || (b >= c0 / 16 && b < c0 / 16 + S::CW / 16))
+#pragma unroll
+          for (int rg = 0; rg < NR; ++rg)
+            *reinterpret_cast<f32x4 *>(&merge[(wave * R + 16 * rg + li) * S::ROW + 16 * b - c0 + 4 * j4]) = acc[b][rg] * factor[rg];
+      __syncthreads();
+      for (int i = threadIdx.x; i < R * S::CW / 4; i += 64 * W) {
+        const int r = i / (S::CW / 4), col = 4 * (i % (S::CW / 4)), at = tile * R + r;
+        f32x4 y = *reinterpret_cast<const f32x4 *>(&merge[r * S::ROW + col]);
+#pragma unroll
+        for (int w = 1; w < W; ++w) y += *reinterpret_cast<const f32x4 *>(&merge[(w * R + r) * S::ROW + col]);
+        if (at > last_row) continue;
+        float top = NO_MAX, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = fmaxf(top, merge_ml[(w * R + r) * 2]);
+#pragma unroll
+        for (int w = 0; w < W; ++w) sum += merge_ml[(w * R + r) * 2 + 1] * fast_exp2(merge_ml[(w * R + r) * 2] - top);
+        if (!whole) {
+          *reinterpret_cast<f32x4 *>(part + r * D + c0 + col) = y;
+          if (c0 + col == 0) part[R * D + 2 * r] = top, part[R * D + 2 * r + 1] = sum;
+          continue;
+        }
+        const int token = at / G, h = hk * G + at - token * G;
+        const float inv = sum == 0.f ? 0.f : 1.0f / sum;  // (a row that sees nothing: O = 0, LSE = -inf)
+        *reinterpret_cast<u32x2 *>(a.o + (size_t(q.row0 + token) * a.hq + h) * D + c0 + col) =
+            u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
+        if (c0 + col == 0 && a.lse) a.lse[size_t(h) * a.s.total + q.row0 + token] = 0.6931471805599453f * (top + fast_log2(sum));
+      }
+      __syncthreads();
+    }
+  }
+  if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
+}
+
+// Adds up the parts of the tiles that were cut: one wave per row, two parts at a time; the order is fixed.
+template <int D, int NR>
+__global__ __launch_bounds__(256) void ca_cache_combine_kernel(const AttendArgs a) {
+  constexpr int R = 16 * NR, LANES = D / 4, AT_A_TIME = 64 / LANES;
+  const int hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv;
+  const int4 head = a.heads[worker * a.hkv + hk];
+  if (head.x < 2) return;
+  const int G = a.hq / a.hkv, lane = threadIdx.x & 63, r = 4 * blockIdx.y + (threadIdx.x >> 6);
+  const Seq q = seq_of(a.s, head.y);
+  const int at = head.z * R + r;
+  if (at >= q.n * G) return;
+  const size_t stride = size_t(2 * a.hkv) * (R * (D + 2));
+  const float *const first = a.parts + size_t((worker * 2 + 1) * a.hkv + hk) * (R * (D + 2));
+  const float *const others = first + stride - size_t(a.hkv) * (R * (D + 2));
+  auto part = [&](int i) { return i == 0 ? first : others + size_t(i - 1) * stride; };
+  float top = NO_MAX;
+  for (int i = lane; i < head.x; i += 64) top = fmaxf(top, part(i)[R * D + 2 * r]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  f32x4 y = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+  const int mine = lane / LANES, col = 4 * (lane % LANES);
+#pragma unroll 8
+  for (int i = mine; i < head.x; i += AT_A_TIME) {
+    const float *const p = part(i);
+    const float w = fast_exp2(p[R * D + 2 * r] - top);
+    sum += w * p[R * D + 2 * r + 1];
+    y += w * *reinterpret_cast<const f32x4 *>(p + r * D + col);
+  }
+#pragma unroll
+  for (int o = LANES; o < 64; o <<= 1) {
+    sum += __shfl_xor(sum, o);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], o);
+  }
+  if (mine != 0) return;
+  const int token = at / G, h = hk * G + at - token * G;
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  *reinterpret_cast<u32x2 *>(a.o + (size_t(q.row0 + token) * a.hq + h) * D + col) =
+      u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
+  if (col == 0 && a.lse) a.lse[size_t(h) * a.s.total + q.row0 + token] = 0.6931471805599453f * (top + fast_log2(sum));
+}
+
+// ------------------------------------------------------------------------------------------------ append
+struct AppendArgs {
+  SeqArgs s;
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+  const bf16_t *new_k, *new_v;
+  int hkv;
+};
+
+// The smallest power of two that is at least top / 448, the largest e4m3 value (448 = 1.75 * 2^8), and at least 2^-126.
+__device__ __forceinline__ float scale_for(float top) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, top);
+  const int e = int(u >> 23) - 8 + ((u & 0x7FFFFF) > 0x600000);  // the exponent field of the scale
+  return __builtin_bit_cast(float, uint32_t(max(e, 1)) << 23);
+}
+// The smallest power of two that is at least x (of a positive normal number).
+__device__ __forceinline__ float next_power(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  return __builtin_bit_cast(float, (u & 0x7FFFFF) ? ((u >> 23) + 1) << 23 : u);
+}
+__device__ __forceinline__ float inverse_power(float s) {  // of a power of two from 2^-126 to 2^126
+  return __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, s));
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
+// four values to four codes, nearest, ties to even (no finite value here is beyond 448; Inf and NaN become NaN)
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true));
+}
+__device__ __forceinline__ uint32_t scaled_codes(uint32_t w, float f) {
+  return to_codes(__builtin_amdgcn_cvt_f32_fp8(int(w), 0) * f, __builtin_amdgcn_cvt_f32_fp8(int(w), 1) * f,
+                  __builtin_amdgcn_cvt_f32_fp8(int(w), 2) * f, __builtin_amdgcn_cvt_f32_fp8(int(w), 3) * f);
+}
+// the larger of the finite magnitudes of a word's two values and `top` (bits of a bf16)
+__device__ __forceinline__ uint32_t top_of(uint32_t top, uint32_t w) {
+  const uint32_t a = w & 0x7FFF, b = (w >> 16) & 0x7FFF;
+  return max(top, max(a < 0x7F80 ? a : 0u, b < 0x7F80 ? b : 0u));
+}
+__device__ __forceinline__ float wave_top(uint32_t top) { return __builtin_bit_cast(float, uint32_t(wave_max(int(top))) << 16); }
+
+// One wave per (page that gets new tokens, KV head): the new tokens of the page in registers, their largest magnitude, the scale, the codes.
+// Where the page holds tokens already and its scale grows, all that it holds is rounded again, from old / new of the scales:
+// exact but for codes that leave the normal range.
+template <int D>
+__global__ __launch_bounds__(256) void ca_cache_append_kernel(const AppendArgs a) {
+  constexpr int LPT = D / 8, TPI = 64 / LPT, NI = PAGE / TPI;    // K: lanes per token, tokens per load, loads per page
+  constexpr int VL = D / 2, VT = 64 / VL, NV = PAGE / VT;        // V: a lane has two columns of NV tokens (of all 64, or of 32)
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  int *const pre = reinterpret_cast<int *>(smem), *const wave_sums = pre + (a.s.n_seqs + 4) / 4 * 4;
+  auto first_pos = [](const Seq &q) { return max(0, q.len - q.n); };
+  const int total = block_prefix<256>(pre, wave_sums, a.s.n_seqs, [&](int s) {
+    const Seq q = seq_of(a.s, s);
+    return q.n > 0 && q.len > 0 ? (q.len - 1) / PAGE - first_pos(q) / PAGE + 1 : 0;
+  });
+  const int unit = int(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int touch = unit / a.hkv, h = unit % a.hkv, lane = threadIdx.x & 63;
+  if (touch >= total) return;
+  const int s = find_unit(pre, a.s.n_seqs, touch);
+  const Seq q = seq_of(a.s, s);
+  const int index = first_pos(q) / PAGE + touch - pre[s];
+  const int page = a.s.table[size_t(s) * a.s.width + index];
+  if (page < 0 || page >= a.s.n_pages) return;
+  const int begin = max(first_pos(q) - index * PAGE, 0), end = min(q.len - index * PAGE, PAGE);  // the page's tokens that are new
+  const int row0 = q.row0 + index * PAGE - (q.len - q.n);                                        // the row of the page's token 0
+  const size_t at = size_t(page) * a.hkv + h;
+  uint8_t *const kp = a.k + at * (PAGE * D), *const vp = a.v + at * (PAGE * D);
+
+  auto scales = [&](uint32_t top, float *scale, float &f, float &again) {  // 1 / the new scale, and old / new
+    const float need = scale_for(wave_top(top)), old = begin > 0 ? *scale : 0.f;
+    const float now = begin > 0 && old > 0.f ? fmaxf(need, next_power(old)) : need;
+    again = begin > 0 && old > 0.f ? old * inverse_power(now) : 1.f;
+    f = inverse_power(now);
+    if (lane == 0) *scale = now;
+  };
+  {  // K: lane (token lane / LPT of a load, 8 columns)
+    u32x4 x[NI];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int t = TPI * i + lane / LPT;
+      x[i] = u32x4{0, 0, 0, 0};
+      if (t >= begin && t < end) x[i] = *reinterpret_cast<const u32x4 *>(a.new_k + (size_t(row0 + t) * a.hkv + h) * D + 8 * (lane % LPT));
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = top_of(top, x[i][w]);
+    float f, again;
+    scales(top, a.k_scale + at, f, again);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int t = TPI * i + lane / LPT;
+      u32x2 *const dst = reinterpret_cast<u32x2 *>(kp + t * D + 8 * (lane % LPT));
+      if (t >= begin && t < end) {
+        *dst = u32x2{to_codes(bf16_lo(x[i][0]) * f, bf16_hi(x[i][0]) * f, bf16_lo(x[i][1]) * f, bf16_hi(x[i][1]) * f),
+                     to_codes(bf16_lo(x[i][2]) * f, bf16_hi(x[i][2]) * f, bf16_lo(x[i][3]) * f, bf16_hi(x[i][3]) * f)};
+      } else if (again != 1.f) {
+        const u32x2 w = *dst;
+        *dst = u32x2{scaled_codes(w[0], again), scaled_codes(w[1], again)};
+      }
+    }
+  }
+  {  // V: lane (columns 2 (lane % VL) and the next, tokens NV (lane / VL) ..)
+    uint32_t x[NV], top = 0;
+    const int t0 = NV * (lane / VL), col = 2 * (lane % VL);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int t = t0 + i;
+      x[i] = 0;
+      if (t >= begin && t < end) x[i] = *reinterpret_cast<const uint32_t *>(a.new_v + (size_t(row0 + t) * a.hkv + h) * D + col);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) top = top_of(top, x[i]);
+    float f, again;
+    scales(top, a.v_scale + at, f, again);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      uint8_t *const dst = vp + (col + c) * PAGE + t0;
+#pragma unroll
+      for (int i = 0; i < NV; i += 4) {
+        const int t = t0 + i;
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (c == 0 ? bf16_lo(x[i + e]) : bf16_hi(x[i + e])) * f;
+        const uint32_t codes = to_codes(y[0], y[1], y[2], y[3]);
+        uint32_t *const word = reinterpret_cast<uint32_t *>(dst + i);
+        if (t >= begin && t + 4 <= end) {
+          *word = codes;
+        } else if (again != 1.f) {
+          const uint32_t held = scaled_codes(*word, again);
+          uint32_t mine = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mine |= t + e >= begin && t + e < end ? 0xFFu << (8 * e) : 0u;
+          *word = (codes & mine) | (held & ~mine);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t + e >= begin && t + e < end) dst[i + e] = uint8_t(codes >> (8 * e));
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ copies
+// 16 KiB of a page's keys, then of its values, per workgroup.
+constexpr int COPY_BYTES = 16384;
+__global__ __launch_bounds__(256) void ca_cache_copy_kernel(uint8_t *__restrict__ k, uint8_t *__restrict__ v, float *__restrict__ k_scale,
+                                                            float *__restrict__ v_scale, const int32_t *__restrict__ src,
+                                                            const int32_t *__restrict__ dst, int n_pages, int hkv, int page_bytes,
+                                                            int chunks) {
+  const int pair = blockIdx.x / (2 * chunks), rest = blockIdx.x % (2 * chunks), at = rest % chunks * COPY_BYTES;
+  const int from = src[pair], to = dst[pair];
+  if (from < 0 || from >= n_pages || to < 0 || to >= n_pages || from == to) return;
+  uint8_t *const p = rest < chunks ? k : v;
+  const u32x4 *const x = reinterpret_cast<const u32x4 *>(p + size_t(from) * page_bytes + at);
+  u32x4 *const y = reinterpret_cast<u32x4 *>(p + size_t(to) * page_bytes + at);
+  const int n = min(COPY_BYTES, page_bytes - at) / 16;
+  u32x4 r[COPY_BYTES / 4096];
+#pragma unroll
+  for (int i = 0; i < COPY_BYTES / 4096; ++i)
+    if (256 * i + int(threadIdx.x) < n) r[i] = x[256 * i + threadIdx.x];
+#pragma unroll
+  for (int i = 0; i < COPY_BYTES / 4096; ++i)
+    if (256 * i + int(threadIdx.x) < n) y[256 * i + threadIdx.x] = r[i];
+  if (at == 0) {
+    float *const scale = rest < chunks ? k_scale : v_scale;
+    for (int h = threadIdx.x; h < hkv; h += 256) scale[size_t(to) * hkv + h] = scale[size_t(from) * hkv + h];
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ calls
+static int fail(int code, const std::string &msg) {
+  set_error(msg);
+  return code;
+}
+static int check_cache(const ca_cache *c) {
+  if (!c) return fail(CA_ERR_INVALID_ARG, "cache is null");
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(CA_ERR_UNSUPPORTED, "head_dim not supported (64 or 128)");
+  if (c->n_pages < 0 || c->n_kv_heads < 1) return fail(CA_ERR_INVALID_ARG, "cache: n_pages must not be negative, n_kv_heads at least 1");
+  if (c->n_kv_heads > 1024) return fail(CA_ERR_UNSUPPORTED, "cache: more than 1024 KV heads");
+  if (c->n_pages > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return fail(CA_ERR_INVALID_ARG, "cache: k, v, k_scale or v_scale is null");
+  if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16 != 0) return fail(CA_ERR_INVALID_ARG, "cache: k or v is not 16-byte aligned");
+  return CA_OK;
+}
+static int check_batch(const ca_cache_batch *b) {
+  if (!b) return fail(CA_ERR_INVALID_ARG, "batch is null");
+  if (b->n_seqs < 0 || b->table_width < 0 || b->total_rows < 0) return fail(CA_ERR_INVALID_ARG, "batch: negative size");
+  if (b->n_seqs > MAX_SEQS) return fail(CA_ERR_UNSUPPORTED, "batch: more than 4096 sequences");
+  if (b->table_width > (1 << 23)) return fail(CA_ERR_UNSUPPORTED, "batch: table_width beyond 2^23 pages");
+  if (b->total_rows >= (int64_t(1) << 30)) return fail(CA_ERR_UNSUPPORTED, "batch: total_rows beyond 2^30");
+  if (b->n_seqs > 0 && (!b->q_start || !b->kv_len || (b->table_width > 0 && !b->page_table)))
+    return fail(CA_ERR_INVALID_ARG, "batch: q_start, kv_len or page_table is null");
+  return CA_OK;
+}
+static SeqArgs seq_args(const ca_cache *c, const ca_cache_batch *b) {
+  return {b->q_start, b->kv_len, b->page_table, b->n_seqs, b->table_width, int(b->total_rows), c->n_pages};
+}
+static int launched(const char *what, hipError_t e) {
+  if (e == hipSuccess) e = hipGetLastError();
+  if (e == hipSuccess) return CA_OK;
+  return fail(CA_ERR_HIP, std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")");
+}
+
+// Workers per KV head: about one workgroup of eight waves, or two of four, for each CU.
+template <int NR>
+constexpr int WAVES = NR == 1 ? 8 : 4;
+static int n_workers(int hkv, int waves) { return std::max(1, N_CU * 8 / waves / hkv); }
+template <int D, int NR>
+static size_t attend_bytes(int hkv) {
+  const size_t workers = size_t(n_workers(hkv, WAVES<NR>));
+  return workers * hkv * sizeof(int4) + workers * 2 * hkv * (16 * NR * (D + 2)) * 4;
+}
+static size_t attend_bytes(const ca_cache *c) {
+  const int hkv = c->n_kv_heads;
+  return c->head_dim == 128 ? std::max({attend_bytes<128, 1>(hkv), attend_bytes<128, 2>(hkv), attend_bytes<128, 4>(hkv)})
+                            : std::max({attend_bytes<64, 1>(hkv), attend_bytes<64, 2>(hkv), attend_bytes<64, 4>(hkv)});
+}
+
+template <int D, int NR>
+static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
+  constexpr int W = WAVES<NR>;
+  using S = AttendShape<D, NR, W>;
+  const int workers = n_workers(a.hkv, W);
+  a.heads = static_cast<int4 *>(ws);
+  a.parts = reinterpret_cast<float *>(a.heads + size_t(workers) * a.hkv);
+  auto kern = ca_cache_attend_kernel<D, NR, W>;
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  static std::atomic<bool> done[16];
+  if (e == hipSuccess) e = set_smem(kern, int(S::smem(MAX_SEQS)), device, done);
+  if (e != hipSuccess) return launched("cache attention", e);
+  hipLaunchKernelGGL(kern, dim3(unsigned(workers * a.hkv)), dim3(64 * W), S::smem(a.s.n_seqs), st, a);
+  const int most = 16 * NR;
+  hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(workers * a.hkv), unsigned(most / 4)), dim3(256), 0, st, a);
+  return launched("cache attention", hipSuccess);
+}
+
+}  // namespace ca
+
+extern "C" {
+
+int ca_cache_attend_workspace_bytes(const ca_cache *c, int32_t n_q_heads, size_t *bytes) {
+  using namespace ca;
+  if (const int rc = check_cache(c); rc != CA_OK) return rc;
+  if (!bytes) return fail(CA_ERR_INVALID_ARG, "output is null");
+  if (n_q_heads < 1 || n_q_heads % c->n_kv_heads != 0) return fail(CA_ERR_UNSUPPORTED, "n_q_heads is not a multiple of n_kv_heads");
+  *bytes = attend_bytes(c);
+  return CA_OK;
+}
+
+int ca_cache_attend(const ca_cache *c, const ca_cache_batch *b, int32_t n_q_heads, float softmax_scale, int64_t window, int64_t sinks,
+                    const void *q, void *o, float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+  using namespace ca;
+  if (const int rc = check_cache(c); rc != CA_OK) return rc;
+  if (const int rc = check_batch(b); rc != CA_OK) return rc;
+  if (n_q_heads < 1 || n_q_heads % c->n_kv_heads != 0) return fail(CA_ERR_UNSUPPORTED, "n_q_heads is not a multiple of n_kv_heads");
+  if (window < 0 || sinks < 0) return fail(CA_ERR_INVALID_ARG, "negative window or sinks");
+  if (b->n_seqs == 0 || b->total_rows == 0) return CA_OK;
+  if (!q || !o) return fail(CA_ERR_INVALID_ARG, "q or o is null");
+  const size_t need = attend_bytes(c);
+  if (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % 256 != 0) {
+    std::ostringstream os;
+    os << "workspace of " << (ws ? ws_bytes : 0) << " bytes given, " << need << " needed, 256-byte aligned";
+    return fail(CA_ERR_WORKSPACE, os.str());
+  }
+  const int64_t g = n_q_heads / c->n_kv_heads;
+  if ((b->total_rows * g / 16 + b->n_seqs) * std::max(1, b->table_width) >= int64_t(1) << 30)
+    return fail(CA_ERR_UNSUPPORTED, "batch: rows times pages beyond 2^30");
+  AttendArgs a = {};
+  a.s = seq_args(c, b);
+  a.k = static_cast<const uint8_t *>(c->k), a.v = static_cast<const uint8_t *>(c->v), a.k_scale = c->k_scale, a.v_scale = c->v_scale;
+  a.q = static_cast<const bf16_t *>(q), a.o = static_cast<bf16_t *>(o), a.lse = lse;
+  a.hq = n_q_heads, a.hkv = c->n_kv_heads;
+  a.window = window == 0 ? 1 << 30 : int(std::min<int64_t>(window, 1 << 30));
+  a.sinks = window == 0 ? 0 : int(std::min<int64_t>(sinks, 1 << 30));
+  a.c = (softmax_scale > 0.f ? softmax_scale : c->head_dim == 128 ? 0.08838834764831845f : 0.125f) * 1.4426950408889634f;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  // Rows per tile from the average sequence: what fits 16 rows reads each page once as it is; more rows per tile convert and read a page
+  // less often.
+  const int64_t rows = b->total_rows * g / b->n_seqs;
+  if (c->head_dim == 128) return rows <= 16 ? launch_attend<128, 1>(a, ws, st) : rows <= 32 ? launch_attend<128, 2>(a, ws, st) : launch_attend<128, 4>(a, ws, st);
+  return rows <= 16 ? launch_attend<64, 1>(a, ws, st) : rows <= 32 ? launch_attend<64, 2>(a, ws, st) : launch_attend<64, 4>(a, ws, st);
+}
+
+int ca_cache_append(const ca_cache *c, const ca_cache_batch *b, const void *k, const void *v, void *hip_stream) {
+  using namespace ca;
+  if (const int rc = check_cache(c); rc != CA_OK) return rc;
+  if (const int rc = check_batch(b); rc != CA_OK) return rc;
+  if (b->n_seqs == 0 || b->total_rows == 0 || b->table_width == 0) return CA_OK;
+  if (!k || !v) return fail(CA_ERR_INVALID_ARG, "k or v is null");
+  const AppendArgs a = {seq_args(c, b), static_cast<uint8_t *>(c->k), static_cast<uint8_t *>(c->v), c->k_scale, c->v_scale,
+                        static_cast<const bf16_t *>(k), static_cast<const bf16_t *>(v), c->n_kv_heads};
+  // pages that n rows of a sequence can touch: at most (n - 1) / 64 + 2, and no more than n
+  const int64_t touches = std::min<int64_t>(b->total_rows, b->total_rows / PAGE + 2 * int64_t(b->n_seqs));
+  const int64_t groups = (touches * c->n_kv_heads + 3) / 4;
+  if (groups >= int64_t(1) << 31) return fail(CA_ERR_UNSUPPORTED, "batch: rows times KV heads too many");
+  const size_t smem = size_t(b->n_seqs + 4) / 4 * 16 + 64;
+  hipLaunchKernelGGL(c->head_dim == 128 ? ca_cache_append_kernel<128> : ca_cache_append_kernel<64>, dim3(unsigned(groups)), dim3(256), smem,
+                     static_cast<hipStream_t>(hip_stream), a);
+  return launched("cache append", hipSuccess);
+}
+
+int ca_cache_copy_pages(const ca_cache *c, const int32_t *src, const int32_t *dst, int64_t n, void *hip_stream) {
+  using namespace ca;
+  if (const int rc = check_cache(c); rc != CA_OK) return rc;
+  if (n < 0) return fail(CA_ERR_INVALID_ARG, "negative number of pages");
+  if (n == 0) return CA_OK;
+  if (!src || !dst) return fail(CA_ERR_INVALID_ARG, "src or dst is null");
+  const int64_t page_bytes = int64_t(c->n_kv_heads) * PAGE * c->head_dim, chunks = (page_bytes + COPY_BYTES - 1) / COPY_BYTES;
+  if (2 * chunks * n >= int64_t(1) << 31) return fail(CA_ERR_UNSUPPORTED, "too many pages");
+  hipLaunchKernelGGL(ca_cache_copy_kernel, dim3(unsigned(2 * chunks * n)), dim3(256), 0, static_cast<hipStream_t>(hip_stream),
+                     static_cast<uint8_t *>(c->k), static_cast<uint8_t *>(c->v), c->k_scale, c->v_scale, src, dst, c->n_pages, c->n_kv_heads,
+                     int(page_bytes), int(chunks));
+  return launched("cache copy", hipSuccess);
+}
+
+}  // extern "C"
