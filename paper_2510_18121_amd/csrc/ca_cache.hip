@@ -43,36 +43,55 @@ __device__ __forceinline__ Seq seq_of(const SeqArgs &a, int s) {
   return q;
 }
 
-// pre[i] = sum of units(0) .. units(i - 1), for all threads of the workgroup; returns the whole sum.  (Sums stop growing at MOST_UNITS:
-// only sequences that overlap, against their description, come so far, and then nothing overflows.)
+// What the workgroup keeps of the sequences in LDS: pre[i] = sum of the units of sequences 0 .. i - 1, and the sequences themselves, so
+// that finding a unit and its sequence costs no trip to memory.  (Sums stop growing at MOST_UNITS: only sequences that overlap,
+// against their description, come so far, and then nothing overflows.)
 constexpr int MOST_UNITS = (1 << 30) - 1;
 __device__ __forceinline__ int sum_units(int a, int b) { return min(a + b, MOST_UNITS); }
+struct SeqTable {
+  int *wave_sums, *pre, *row0, *n, *len;
+  __device__ __forceinline__ Seq at(int s) const {
+    return {__builtin_amdgcn_readfirstlane(row0[s]), __builtin_amdgcn_readfirstlane(n[s]), __builtin_amdgcn_readfirstlane(len[s])};
+  }
+};
+constexpr size_t seq_table_bytes(int n_seqs) { return 64 + size_t(n_seqs + 4) / 4 * 16 * 4; }
+__device__ __forceinline__ SeqTable seq_table(void *lds, int n_seqs) {
+  const int stride = (n_seqs + 4) / 4 * 4;
+  int *const p = static_cast<int *>(lds);
+  return {p, p + 16, p + 16 + stride, p + 16 + 2 * stride, p + 16 + 3 * stride};
+}
+// fills the table for all threads of the workgroup; returns the sum of all units
 template <int T, class F>
-__device__ __forceinline__ int block_prefix(int *pre, int *wave_sums, int n, F units) {
+__device__ __forceinline__ int fill_table(const SeqTable &tab, const SeqArgs &a, F units) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int carry = 0;
-  for (int base = 0; base < n; base += T) {
+  for (int base = 0; base < a.n_seqs; base += T) {
     const int i = base + int(threadIdx.x);
-    int x = i < n ? units(i) : 0;
+    int x = 0;
+    if (i < a.n_seqs) {
+      const Seq q = seq_of(a, i);
+      tab.row0[i] = q.row0, tab.n[i] = q.n, tab.len[i] = q.len;
+      x = units(q);
+    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int y = __shfl_up(x, o);
       if (lane >= o) x = sum_units(x, y);
     }
-    if (lane == 63) wave_sums[wave] = x;
+    if (lane == 63) tab.wave_sums[wave] = x;
     __syncthreads();
     int before = carry;
 #pragma unroll
     for (int w = 0; w < T / 64; ++w) {
-      before = sum_units(before, w < wave ? wave_sums[w] : 0);
-      carry = sum_units(carry, wave_sums[w]);
+      const int sum = tab.wave_sums[w];
+      before = sum_units(before, w < wave ? sum : 0);
+      carry = sum_units(carry, sum);
     }
-    if (i < n) pre[i + 1] = sum_units(before, x);
+    if (i < a.n_seqs) tab.pre[i + 1] = sum_units(before, x);
+    if (i == 0) tab.pre[0] = 0;
     __syncthreads();
   }
-  if (threadIdx.x == 0) pre[0] = 0;
-  __syncthreads();
-  return carry;
+  return __builtin_amdgcn_readfirstlane(carry);
 }
 // the entry whose run of units holds unit u < pre[n]
 __device__ __forceinline__ int find_unit(const int *pre, int n, int u) {
@@ -121,7 +140,7 @@ template <int D, int NR, int W>
 struct AttendShape {
   static constexpr int R = 16 * NR, CW = NR == 1 ? D : 32, ROW = CW + 4;
   static constexpr int MERGE = (W * R * ROW + W * R * 2) * 4;
-  static constexpr size_t smem(int n_seqs) { return size_t(n_seqs + 1 + 3) / 4 * 16 + 64 + MERGE; }
+  static constexpr size_t smem(int n_seqs) { return seq_table_bytes(n_seqs) + MERGE; }
 };
 
 template <int D, int NR, int W>
@@ -129,33 +148,30 @@ __global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kerne
   using S = AttendShape<D, NR, W>;
   constexpr int R = S::R, NH = D / 64, NB = D / 16;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  int *const pre = reinterpret_cast<int *>(smem), *const wave_sums = pre + (a.s.n_seqs + 4) / 4 * 4;
-  float *const merge = reinterpret_cast<float *>(wave_sums + 16), *const merge_ml = merge + W * R * S::ROW;
+  const SeqTable tab = seq_table(smem, a.s.n_seqs);
+  float *const merge = reinterpret_cast<float *>(smem + seq_table_bytes(a.s.n_seqs)), *const merge_ml = merge + W * R * S::ROW;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j4 = lane >> 4, li = lane & 15;
   const int G = a.hq / a.hkv, hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv, n_workers = gridDim.x / a.hkv;
 
-  const int total = __builtin_amdgcn_readfirstlane(block_prefix<64 * W>(pre, wave_sums, a.s.n_seqs, [&](int s) {
-    const Seq q = seq_of(a.s, s);
-    return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, a.window, a.sinks);
-  }));
+  const int total = fill_table<64 * W>(tab, a.s, [&](const Seq &q) { return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, a.window, a.sinks); });
   const int run = max(W, (total + n_workers - 1) / n_workers);
   auto bound = [&](int w) {
     const int u = min(w, (total + run - 1) / run) * run;
     if (u >= total || u == 0) return min(u, total);
-    const int s = find_unit(pre, a.s.n_seqs, u), n = tile_pages(seq_of(a.s, s).len, R, G, a.window, a.sinks);
-    const int into = (u - pre[s]) % n;
+    const int s = find_unit(tab.pre, a.s.n_seqs, u), n = tile_pages(tab.at(s).len, R, G, a.window, a.sinks);
+    const int into = (u - tab.pre[s]) % n;
     return n > CUT ? u : 2 * into < n ? u - into : u - into + n;
   };
   const int begin = __builtin_amdgcn_readfirstlane(bound(worker)), end = __builtin_amdgcn_readfirstlane(bound(worker + 1));
   int4 head = {0, 0, 0, 0};
 
-  for (int u = begin, s = begin < end ? find_unit(pre, a.s.n_seqs, begin) : 0; u < end;) {
-    while (pre[s + 1] <= u) ++s;
+  for (int u = begin, s = begin < end ? find_unit(tab.pre, a.s.n_seqs, begin) : 0; u < end;) {
+    while (tab.pre[s + 1] <= u) ++s;
     s = __builtin_amdgcn_readfirstlane(s);
-    const Seq q = seq_of(a.s, s);
+    const Seq q = tab.at(s);
     const int per_tile = tile_pages(q.len, R, G, a.window, a.sinks);
-    const int tile = __builtin_amdgcn_readfirstlane((u - pre[s]) / per_tile), first = __builtin_amdgcn_readfirstlane((u - pre[s]) % per_tile);
+    const int tile = __builtin_amdgcn_readfirstlane((u - tab.pre[s]) / per_tile), first = __builtin_amdgcn_readfirstlane((u - tab.pre[s]) % per_tile);
     const int n = min(end - u, per_tile - first);
     u += n;
     // the rows
@@ -434,105 +450,143 @@ __device__ __forceinline__ uint32_t top_of(uint32_t top, uint32_t w) {
 }
 __device__ __forceinline__ float wave_top(uint32_t top) { return __builtin_bit_cast(float, uint32_t(wave_max(int(top))) << 16); }
 
-// One wave per (page that gets new tokens, KV head): the new tokens of the page in registers, their largest magnitude, the scale, the codes.
-// Where the page holds tokens already and its scale grows, all that it holds is rounded again, from old / new of the scales:
-// exact but for codes that leave the normal range.
+// One wave per (page that gets new tokens, KV head, K or V): the largest magnitude of the new tokens, the scale, the codes.  A page that
+// is all new (of a prompt) passes through registers once; of any other the new tokens are read twice, a few at a time, the second time
+// from the caches.  Where such a page's scale grows, all that it holds is rounded again, from old / new of the scales: exact but for codes
+// that leave the normal range.
+// K: D / 8 lanes per token, 8 columns each.  V: a lane has two columns; at head_dim 64 the wave's halves take tokens of their own.
 template <int D>
 __global__ __launch_bounds__(256) void ca_cache_append_kernel(const AppendArgs a) {
-  constexpr int LPT = D / 8, TPI = 64 / LPT, NI = PAGE / TPI;    // K: lanes per token, tokens per load, loads per page
-  constexpr int VL = D / 2, VT = 64 / VL, NV = PAGE / VT;        // V: a lane has two columns of NV tokens (of all 64, or of 32)
+  constexpr int LPT = D / 8, TPI = 64 / LPT, NI = PAGE / TPI;  // K: lanes per token, tokens per load, loads per page
+  constexpr int VL = D / 2, VT = 64 / VL, NV = PAGE / VT;      // V: lanes per token, halves, tokens per half of a whole page
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  int *const pre = reinterpret_cast<int *>(smem), *const wave_sums = pre + (a.s.n_seqs + 4) / 4 * 4;
+  const SeqTable tab = seq_table(smem, a.s.n_seqs);
   auto first_pos = [](const Seq &q) { return max(0, q.len - q.n); };
-  const int total = block_prefix<256>(pre, wave_sums, a.s.n_seqs, [&](int s) {
-    const Seq q = seq_of(a.s, s);
-    return q.n > 0 && q.len > 0 ? (q.len - 1) / PAGE - first_pos(q) / PAGE + 1 : 0;
-  });
+  const int total = fill_table<256>(tab, a.s, [&](const Seq &q) { return q.n > 0 && q.len > 0 ? (q.len - 1) / PAGE - first_pos(q) / PAGE + 1 : 0; });
   const int unit = int(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int touch = unit / a.hkv, h = unit % a.hkv, lane = threadIdx.x & 63;
+  const int touch = unit / (2 * a.hkv), h = unit / 2 % a.hkv, lane = threadIdx.x & 63;
   if (touch >= total) return;
-  const int s = find_unit(pre, a.s.n_seqs, touch);
-  const Seq q = seq_of(a.s, s);
-  const int index = first_pos(q) / PAGE + touch - pre[s];
+  const int s = find_unit(tab.pre, a.s.n_seqs, touch);
+  const Seq q = tab.at(s);
+  const int index = __builtin_amdgcn_readfirstlane(first_pos(q) / PAGE + touch - tab.pre[s]);
   const int page = a.s.table[size_t(s) * a.s.width + index];
   if (page < 0 || page >= a.s.n_pages) return;
   const int begin = max(first_pos(q) - index * PAGE, 0), end = min(q.len - index * PAGE, PAGE);  // the page's tokens that are new
-  const int row0 = q.row0 + index * PAGE - (q.len - q.n);                                        // the row of the page's token 0
-  const size_t at = size_t(page) * a.hkv + h;
-  uint8_t *const kp = a.k + at * (PAGE * D), *const vp = a.v + at * (PAGE * D);
-
-  auto scales = [&](uint32_t top, float *scale, float &f, float &again) {  // 1 / the new scale, and old / new
-    const float need = scale_for(wave_top(top)), old = begin > 0 ? *scale : 0.f;
-    const float now = begin > 0 && old > 0.f ? fmaxf(need, next_power(old)) : need;
-    again = begin > 0 && old > 0.f ? old * inverse_power(now) : 1.f;
-    f = inverse_power(now);
+  const int64_t row0 = int64_t(q.row0) + index * PAGE - (q.len - q.n);                           // the row of the page's token 0
+  const size_t at = size_t(page) * a.hkv + h, row = size_t(a.hkv) * D;
+  // 1 / the new scale and old / new; stores the new scale
+  auto scales = [&](uint32_t top, float old, float *scale, float &f, float &again) {
+    const float need = scale_for(wave_top(top)), now = old > 0.f ? fmaxf(need, next_power(old)) : need;
+    f = inverse_power(now), again = old > 0.f ? old * f : 1.f;
     if (lane == 0) *scale = now;
   };
-  {  // K: lane (token lane / LPT of a load, 8 columns)
-    u32x4 x[NI];
+  float f, again;
+
+  if (unit % 2 == 0) {
+    const bf16_t *const src = a.new_k + row0 * int64_t(row) + size_t(h) * D + 8 * (lane % LPT);
+    uint8_t *const dst = a.k + at * (PAGE * D) + 8 * (lane % LPT);
+    auto codes = [&](const u32x4 &x) {
+      return u32x2{to_codes(bf16_lo(x[0]) * f, bf16_hi(x[0]) * f, bf16_lo(x[1]) * f, bf16_hi(x[1]) * f),
+                   to_codes(bf16_lo(x[2]) * f, bf16_hi(x[2]) * f, bf16_lo(x[3]) * f, bf16_hi(x[3]) * f)};
+    };
     uint32_t top = 0;
+    if (end - begin == PAGE) {
+      u32x4 x[NI];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int t = TPI * i + lane / LPT;
-      x[i] = u32x4{0, 0, 0, 0};
-      if (t >= begin && t < end) x[i] = *reinterpret_cast<const u32x4 *>(a.new_k + (size_t(row0 + t) * a.hkv + h) * D + 8 * (lane % LPT));
+      for (int i = 0; i < NI; ++i) x[i] = *reinterpret_cast<const u32x4 *>(src + (TPI * i + lane / LPT) * row);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = top_of(top, x[i][w]);
+      scales(top, 0.f, a.k_scale + at, f, again);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) *reinterpret_cast<u32x2 *>(dst + (TPI * i + lane / LPT) * D) = codes(x[i]);
+      return;
     }
+    const float old = begin > 0 ? a.k_scale[at] : 0.f;
+    for (int t0 = begin; t0 < end; t0 += 4 * TPI) {
+      u32x4 x[4];
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+      for (int i = 0; i < 4; ++i) {
+        const int t = t0 + TPI * i + lane / LPT;
+        x[i] = u32x4{0, 0, 0, 0};
+        if (t < end) x[i] = *reinterpret_cast<const u32x4 *>(src + t * row);
+      }
 #pragma unroll
-      for (int w = 0; w < 4; ++w) top = top_of(top, x[i][w]);
-    float f, again;
-    scales(top, a.k_scale + at, f, again);
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int t = TPI * i + lane / LPT;
-      u32x2 *const dst = reinterpret_cast<u32x2 *>(kp + t * D + 8 * (lane % LPT));
-      if (t >= begin && t < end) {
-        *dst = u32x2{to_codes(bf16_lo(x[i][0]) * f, bf16_hi(x[i][0]) * f, bf16_lo(x[i][1]) * f, bf16_hi(x[i][1]) * f),
-                     to_codes(bf16_lo(x[i][2]) * f, bf16_hi(x[i][2]) * f, bf16_lo(x[i][3]) * f, bf16_hi(x[i][3]) * f)};
-      } else if (again != 1.f) {
-        const u32x2 w = *dst;
-        *dst = u32x2{scaled_codes(w[0], again), scaled_codes(w[1], again)};
+        for (int w = 0; w < 4; ++w) top = top_of(top, x[i][w]);
+    }
+    scales(top, old, a.k_scale + at, f, again);
+    if (again != 1.f) {
+#pragma unroll 4
+      for (int t = lane / LPT; t < PAGE; t += TPI) {
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(dst + t * D);
+        if (t < begin || t >= end) *reinterpret_cast<u32x2 *>(dst + t * D) = u32x2{scaled_codes(w[0], again), scaled_codes(w[1], again)};
       }
     }
+#pragma unroll 4
+    for (int t = begin + lane / LPT; t < end; t += TPI) *reinterpret_cast<u32x2 *>(dst + t * D) = codes(*reinterpret_cast<const u32x4 *>(src + t * row));
+    return;
   }
-  {  // V: lane (columns 2 (lane % VL) and the next, tokens NV (lane / VL) ..)
-    uint32_t x[NV], top = 0;
-    const int t0 = NV * (lane / VL), col = 2 * (lane % VL);
+
+  const bf16_t *const src = a.new_v + row0 * int64_t(row) + size_t(h) * D + 2 * (lane % VL);
+  uint8_t *const dst = a.v + at * (PAGE * D) + 2 * (lane % VL) * PAGE;
+  auto codes = [&](int c, const uint32_t *x) {  // of column c of four tokens
+    return c == 0 ? to_codes(bf16_lo(x[0]) * f, bf16_lo(x[1]) * f, bf16_lo(x[2]) * f, bf16_lo(x[3]) * f)
+                  : to_codes(bf16_hi(x[0]) * f, bf16_hi(x[1]) * f, bf16_hi(x[2]) * f, bf16_hi(x[3]) * f);
+  };
+  uint32_t top = 0;
+  if (end - begin == PAGE) {
+    const int t0 = NV * (lane / VL);
+    uint32_t x[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int t = t0 + i;
-      x[i] = 0;
-      if (t >= begin && t < end) x[i] = *reinterpret_cast<const uint32_t *>(a.new_v + (size_t(row0 + t) * a.hkv + h) * D + col);
-    }
+    for (int i = 0; i < NV; ++i) x[i] = *reinterpret_cast<const uint32_t *>(src + (t0 + i) * row);
 #pragma unroll
     for (int i = 0; i < NV; ++i) top = top_of(top, x[i]);
-    float f, again;
-    scales(top, a.v_scale + at, f, again);
+    scales(top, 0.f, a.v_scale + at, f, again);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < NV; i += 16)
+        *reinterpret_cast<u32x4 *>(dst + c * PAGE + t0 + i) = u32x4{codes(c, x + i), codes(c, x + i + 4), codes(c, x + i + 8), codes(c, x + i + 12)};
+    return;
+  }
+  const float old = begin > 0 ? a.v_scale[at] : 0.f;
+  for (int t0 = begin; t0 < end; t0 += 8 * VT) {
+    uint32_t x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int t = t0 + VT * i + lane / VL;
+      x[i] = 0;
+      if (t < end) x[i] = *reinterpret_cast<const uint32_t *>(src + t * row);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = top_of(top, x[i]);
+  }
+  scales(top, old, a.v_scale + at, f, again);
+  // words of four tokens: all of the page's where it is rounded again, those with new tokens otherwise
+  const bool all = again != 1.f;
+#pragma unroll 2
+  for (int t = (all ? 0 : begin & ~3) + 4 * (lane / VL); t < (all ? PAGE : end); t += 4 * VT) {
+    uint32_t x[4], mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool is_new = t + e >= begin && t + e < end;
+      x[e] = 0;
+      if (is_new) x[e] = *reinterpret_cast<const uint32_t *>(src + (t + e) * row);
+      mine |= is_new ? 0xFFu << (8 * e) : 0u;
+    }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      uint8_t *const dst = vp + (col + c) * PAGE + t0;
+      uint32_t *const word = reinterpret_cast<uint32_t *>(dst + c * PAGE + t);
+      const uint32_t w = codes(c, x);
+      if (mine == 0xFFFFFFFFu || all) {
+        *word = (w & mine) | (mine == 0xFFFFFFFFu ? 0u : scaled_codes(*word, again) & ~mine);
+      } else {
 #pragma unroll
-      for (int i = 0; i < NV; i += 4) {
-        const int t = t0 + i;
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = (c == 0 ? bf16_lo(x[i + e]) : bf16_hi(x[i + e])) * f;
-        const uint32_t codes = to_codes(y[0], y[1], y[2], y[3]);
-        uint32_t *const word = reinterpret_cast<uint32_t *>(dst + i);
-        if (t >= begin && t + 4 <= end) {
-          *word = codes;
-        } else if (again != 1.f) {
-          const uint32_t held = scaled_codes(*word, again);
-          uint32_t mine = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mine |= t + e >= begin && t + e < end ? 0xFFu << (8 * e) : 0u;
-          *word = (codes & mine) | (held & ~mine);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (t + e >= begin && t + e < end) dst[i + e] = uint8_t(codes >> (8 * e));
-        }
+        for (int e = 0; e < 4; ++e)
+          if ((mine >> (8 * e)) & 1) dst[c * PAGE + t + e] = uint8_t(w >> (8 * e));
       }
     }
   }
@@ -689,11 +743,16 @@ int ca_cache_append(const ca_cache *c, const ca_cache_batch *b, const void *k, c
                         static_cast<const bf16_t *>(k), static_cast<const bf16_t *>(v), c->n_kv_heads};
   // pages that n rows of a sequence can touch: at most (n - 1) / 64 + 2, and no more than n
   const int64_t touches = std::min<int64_t>(b->total_rows, b->total_rows / PAGE + 2 * int64_t(b->n_seqs));
-  const int64_t groups = (touches * c->n_kv_heads + 3) / 4;
+  const int64_t groups = (touches * 2 * c->n_kv_heads + 3) / 4;
   if (groups >= int64_t(1) << 31) return fail(CA_ERR_UNSUPPORTED, "batch: rows times KV heads too many");
-  const size_t smem = size_t(b->n_seqs + 4) / 4 * 16 + 64;
-  hipLaunchKernelGGL(c->head_dim == 128 ? ca_cache_append_kernel<128> : ca_cache_append_kernel<64>, dim3(unsigned(groups)), dim3(256), smem,
-                     static_cast<hipStream_t>(hip_stream), a);
+  const size_t smem = seq_table_bytes(b->n_seqs);
+  auto kern = c->head_dim == 128 ? ca_cache_append_kernel<128> : ca_cache_append_kernel<64>;
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  static std::atomic<bool> done[2][16];
+  if (e == hipSuccess) e = set_smem(kern, int(seq_table_bytes(MAX_SEQS)), device, done[c->head_dim == 128]);
+  if (e != hipSuccess) return launched("cache append", e);
+  hipLaunchKernelGGL(kern, dim3(unsigned(groups)), dim3(256), smem, static_cast<hipStream_t>(hip_stream), a);
   return launched("cache append", hipSuccess);
 }
 
