@@ -25,6 +25,7 @@ constexpr int PAGE = CA_CACHE_PAGE_TOKENS;
 static_assert(PAGE == 64);
 constexpr int MAX_SEQS = 4096;  // their prefix sums lie in LDS
 constexpr float NO_MAX = -3.402823466e38f;
+constexpr float LEAST_SCALE = 1.17549435e-38f;  // (a hidden score is -infinity, and that times a scale of 0 would be NaN)
 
 // ------------------------------------------------------------------------------------------------ sequences
 // The batch as the kernels see it.  What the device arrays say is clamped to the tensors' sizes: no value reads or writes beyond them.
@@ -136,15 +137,62 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b) {
   return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
+// The workers' shares of the units: worker w has units bound(w) .. bound(w + 1) - 1.
+struct WorkSplit {
+  SeqTable tab;
+  int n_seqs, total, run, R, G, window, sinks;
+  __device__ __forceinline__ int bound(int w) const {
+    const int u = min(w, (total + run - 1) / run) * run;
+    if (u >= total || u == 0) return min(u, total);
+    const int s = find_unit(tab.pre, n_seqs, u), n = tile_pages(tab.at(s).len, R, G, window, sinks);
+    const int into = __builtin_amdgcn_readfirstlane(u - tab.pre[s]) % n;
+    return n > CUT ? u : 2 * into < n ? u - into : u - into + n;
+  }
+};
+template <int T>
+__device__ __forceinline__ WorkSplit split_work(const SeqTable &tab, const AttendArgs &a, int R, int G, int n_workers, int least) {
+  const int total = fill_table<T>(tab, a.s, [&](const Seq &q) { return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, a.window, a.sinks); });
+  return {tab, a.s.n_seqs, total, max(least, (total + n_workers - 1) / n_workers), R, G, a.window, a.sinks};
+}
+
+// Scores x of a page (of row group rg; -infinity where a key is not seen) to the operand of P V; ks and vs: the page's scales, ks with
+// the softmax's factor in base 2.  The reference m moves when some row's maximum has grown by more than 2^8 (see the forward kernel).
+template <int NB, int NR>
+__device__ __forceinline__ void softmax_page(const f32x4 (&x)[4][NR], int rg, float ks, float vs, float &m, float &l, f32x4 (&acc)[NB][NR],
+                                             bf16x8 (&pb)[2][NR]) {
+  float top = x[0][rg][0];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = fmaxf(top, x[t][rg][e]);
+  top *= ks;
+  if (__any(top > m + 8.f)) {
+    const float grown = fmaxf(m, quad_max(top)), f = m == NO_MAX ? 0.f : fast_exp2(m - grown);
+    m = grown, l *= f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b][rg] *= f;
+  }
+  uint32_t w[2][4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    float p[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = fast_exp2(fmaf(x[t][rg][e], ks, -m));
+    l += (p[0] + p[1]) + (p[2] + p[3]);
+    w[t >> 1][2 * (t & 1)] = pack_bf16(p[0] * vs, p[1] * vs), w[t >> 1][2 * (t & 1) + 1] = pack_bf16(p[2] * vs, p[3] * vs);
+  }
+  pb[0][rg] = __builtin_bit_cast(bf16x8, u32x4{w[0][0], w[0][1], w[0][2], w[0][3]});
+  pb[1][rg] = __builtin_bit_cast(bf16x8, u32x4{w[1][0], w[1][1], w[1][2], w[1][3]});
+}
+
 template <int D, int NR, int W>
 struct AttendShape {
   static constexpr int R = 16 * NR, CW = NR == 1 ? D : 32, ROW = CW + 4;
   static constexpr int MERGE = (W * R * ROW + W * R * 2) * 4;
-  static constexpr size_t smem(int n_seqs) { return seq_table_bytes(n_seqs) + MERGE; }
 };
 
 template <int D, int NR, int W>
-__global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * W, 2) void ca_cache_attend_kernel(const AttendArgs a) {
   using S = AttendShape<D, NR, W>;
   constexpr int R = S::R, NH = D / 64, NB = D / 16;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -154,16 +202,8 @@ __global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kerne
   const int j4 = lane >> 4, li = lane & 15;
   const int G = a.hq / a.hkv, hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv, n_workers = gridDim.x / a.hkv;
 
-  const int total = fill_table<64 * W>(tab, a.s, [&](const Seq &q) { return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, a.window, a.sinks); });
-  const int run = max(W, (total + n_workers - 1) / n_workers);
-  auto bound = [&](int w) {
-    const int u = min(w, (total + run - 1) / run) * run;
-    if (u >= total || u == 0) return min(u, total);
-    const int s = find_unit(tab.pre, a.s.n_seqs, u), n = tile_pages(tab.at(s).len, R, G, a.window, a.sinks);
-    const int into = (u - tab.pre[s]) % n;
-    return n > CUT ? u : 2 * into < n ? u - into : u - into + n;
-  };
-  const int begin = __builtin_amdgcn_readfirstlane(bound(worker)), end = __builtin_amdgcn_readfirstlane(bound(worker + 1));
+  const WorkSplit split = split_work<64 * W>(tab, a, R, G, n_workers, W);
+  const int begin = split.bound(worker), end = split.bound(worker + 1);
   int4 head = {0, 0, 0, 0};
 
   for (int u = begin, s = begin < end ? find_unit(tab.pre, a.s.n_seqs, begin) : 0; u < end;) {
@@ -207,7 +247,7 @@ __global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kerne
         at = i < n_sink ? i : from / PAGE + i - n_sink;
         if (at * PAGE <= p1) id = a.s.table[size_t(s) * a.s.width + at];
         if (id >= a.s.n_pages) id = -1;
-        if (id >= 0) ks = a.k_scale[size_t(id) * a.hkv + hk] * a.c, vs = a.v_scale[size_t(id) * a.hkv + hk];
+        if (id >= 0) ks = fmaxf(a.k_scale[size_t(id) * a.hkv + hk] * a.c, LEAST_SCALE), vs = a.v_scale[size_t(id) * a.hkv + hk];
       }
       uint64_t left = __ballot(id >= 0);
       const uint32_t k_lane = uint32_t(16 * (li >> 2) + (li & 3)) * D + 16 * j4, v_lane = uint32_t(li) * PAGE + 16 * j4;
@@ -241,12 +281,6 @@ __global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kerne
             }
           }
         if (left) load_k(__builtin_ctzll(left));  // of the next page
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int rg = 0; rg < NR; ++rg)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[t][rg][e] *= ksi;
         // some row does not see some key: lane (r, j) holds keys key0 + 16 j + 4 t + e
         if (key0 + PAGE - 1 > p0 || (key0 < p1 - a.window + 1 && key0 + PAGE > a.sinks)) {
           const int key = key0 + 16 * j4;
@@ -274,31 +308,7 @@ __global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kerne
         }
         bf16x8 pb[2][NR];
 #pragma unroll
-        for (int rg = 0; rg < NR; ++rg) {
-          float top = x[0][rg][0];
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = fmaxf(top, x[t][rg][e]);
-          // the reference moves when some row's maximum has grown by more than 2^8 (see the forward kernel)
-          if (__any(top > m[rg] + 8.f)) {
-            const float grown = fmaxf(m[rg], quad_max(top)), f = m[rg] == NO_MAX ? 0.f : fast_exp2(m[rg] - grown);
-            m[rg] = grown, l[rg] *= f;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) acc[b][rg] *= f;
-          }
-          uint32_t w[2][4];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            float p[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = fast_exp2(x[t][rg][e] - m[rg]);
-            l[rg] += (p[0] + p[1]) + (p[2] + p[3]);
-            w[t >> 1][2 * (t & 1)] = pack_bf16(p[0] * vsi, p[1] * vsi), w[t >> 1][2 * (t & 1) + 1] = pack_bf16(p[2] * vsi, p[3] * vsi);
-          }
-          pb[0][rg] = __builtin_bit_cast(bf16x8, u32x4{w[0][0], w[0][1], w[0][2], w[0][3]});
-          pb[1][rg] = __builtin_bit_cast(bf16x8, u32x4{w[1][0], w[1][1], w[1][2], w[1][3]});
-        }
+        for (int rg = 0; rg < NR; ++rg) softmax_page<NB>(x, rg, ksi, vsi, m[rg], l[rg], acc, pb);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           const bf16x8 v0 = codes_to_bf16(vr[b][0], vr[b][1]), v1 = codes_to_bf16(vr[b][2], vr[b][3]);
@@ -321,7 +331,7 @@ __global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kerne
     const bool whole = n == per_tile;
     const int slot = first == 0 ? 1 : 0;
     float *const part = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2));
-    if (!whole && slot == 1) head = int4{(u - n + per_tile - 1) / run - worker + 1, s, tile, 0};
+    if (!whole && slot == 1) head = int4{(u - n + per_tile - 1) / split.run - worker + 1, s, tile, 0};
     float factor[NR];
 #pragma unroll
     for (int rg = 0; rg < NR; ++rg) {
@@ -362,6 +372,201 @@ __global__ __launch_bounds__(64 * W, NR == 4 ? 1 : 2) void ca_cache_attend_kerne
       }
       __syncthreads();
     }
+  }
+  if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
+}
+
+// ------------------------------------------------------------------------------------------------ attention of chunks
+// Tiles of 128 rows, 32 to a wave.  The waves share a page: each converts a quarter of it to bf16 and puts it into LDS, so that a code is
+// converted once per 128 rows, and all read its fragments from there.  The page after the next is on its way to registers, the
+// next one is written to the other stage while this one is multiplied; one barrier per page.  K's rows stand in the order of
+// the four tiles' rows, V^T's chunks of 8 keys in the order of its fragments, both swizzled as the other kernels' tiles are.
+template <int D>
+struct ChunkSmem {
+  static constexpr int V_OFF = PAGE * 2 * D, STAGE = 2 * PAGE * 2 * D;
+  static constexpr int TOTAL = 2 * STAGE;
+  static_assert(4 * PATCH_BYTES <= TOTAL, "patches fit in the stages");
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs a) {
+  using S = ChunkSmem<D>;
+  constexpr int R = 128, NK = D / 32, NB = D / 16, ROWB = 2 * D, NL = D / 64;  // NL: loads of K, and of V, of a wave per page
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(CA_LDS char *)smem;
+  const SeqTable tab = seq_table(smem + S::TOTAL, a.s.n_seqs);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j4 = lane >> 4, li = lane & 15;
+  const int G = a.hq / a.hkv, hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv, n_workers = gridDim.x / a.hkv;
+  const WorkSplit split = split_work<256>(tab, a, R, G, n_workers, 4);
+  const int begin = split.bound(worker), end = split.bound(worker + 1);
+  int4 head = {0, 0, 0, 0};
+  // where the wave's codes come from in a page, and where they go: K row i of tile `wave` is key 16 (i / 4) + 4 wave + i % 4
+  uint32_t k_src[NL], k_dst[NL], v_src[NL], v_dst[NL];
+#pragma unroll
+  for (int n = 0; n < NL; ++n) {
+    constexpr int KL = D / 16;  // lanes per row of K
+    const int i = 64 / KL * n + lane / KL, piece = lane % KL, d = D / 4 * wave + 16 * n + lane / 4, j = lane % 4;
+    k_src[n] = uint32_t(16 * (i >> 2) + 4 * wave + (i & 3)) * D + 16 * piece;
+    k_dst[n] = lds0 + (16 * wave + i) * ROWB + 16 * ((2 * piece) ^ tile_sw<D>(i));  // (the second half of the codes: ^ 16)
+    v_src[n] = uint32_t(d) * PAGE + 16 * j;
+    v_dst[n] = lds0 + S::V_OFF + d * (2 * PAGE) + 16 * (j ^ tile_sw<64>(d));        // (... ^ 64)
+  }
+  const uint32_t koff = lds0 + li * ROWB + 16 * (j4 ^ tile_sw<D>(li)), voff = lds0 + S::V_OFF + li * (2 * PAGE) + 16 * (j4 ^ tile_sw<64>(li));
+
+  for (int u = begin, s = begin < end ? find_unit(tab.pre, a.s.n_seqs, begin) : 0; u < end;) {
+    while (tab.pre[s + 1] <= u) ++s;
+    s = __builtin_amdgcn_readfirstlane(s);
+    const Seq q = tab.at(s);
+    const int per_tile = tile_pages(q.len, R, G, a.window, a.sinks);
+    const int tile = __builtin_amdgcn_readfirstlane((u - tab.pre[s]) / per_tile), first = __builtin_amdgcn_readfirstlane((u - tab.pre[s]) % per_tile);
+    const int n = min(end - u, per_tile - first);
+    u += n;
+    // the rows: of the tile, and of the wave (w..)
+    const int last_row = min((tile + 1) * R, q.n * G) - 1, pos0 = q.len - q.n, row_w = tile * R + 32 * wave;
+    const int p0 = pos0 + tile * R / G, p1 = pos0 + last_row / G;
+    const int from = max(0, p0 - a.window + 1), n_sink = min((a.sinks + PAGE - 1) / PAGE, from / PAGE);
+    const int p0w = pos0 + row_w / G, p1w = row_w <= last_row ? pos0 + min(row_w + 31, last_row) / G : -1;
+    const int from_w = max(0, p0w - a.window + 1);
+    int hi[2], lo[2];
+    bf16x8 qf[NK][2];
+#pragma unroll
+    for (int rg = 0; rg < 2; ++rg) {
+      const int r = row_w + 16 * rg + li, ok = r <= last_row, i = ok ? r / G : 0, h = hk * G + (ok ? r - i * G : 0);
+      hi[rg] = ok ? pos0 + i : -1, lo[rg] = max(0, pos0 + i - a.window + 1);
+      const bf16_t *const qp = a.q + (size_t(q.row0 + i) * a.hq + h) * D + 8 * j4;
+#pragma unroll
+      for (int f = 0; f < NK; ++f) qf[f][rg] = *reinterpret_cast<const bf16x8 *>(qp + 32 * f);
+    }
+    f32x4 acc[NB][2];
+    float m[2], l[2];
+#pragma unroll
+    for (int rg = 0; rg < 2; ++rg) {
+      m[rg] = NO_MAX, l[rg] = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b][rg] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int base = 0; base < n; base += 64) {  // 64 pages at a time: their ids and scales, one per lane
+      int id = -1, at = 0;
+      float ks = 0.f, vs = 0.f;
+      if (base + lane < n) {
+        const int i = first + base + lane;
+        at = i < n_sink ? i : from / PAGE + i - n_sink;
+        if (at * PAGE <= p1) id = a.s.table[size_t(s) * a.s.width + at];
+        if (id >= a.s.n_pages) id = -1;
+        if (id >= 0) ks = fmaxf(a.k_scale[size_t(id) * a.hkv + hk] * a.c, LEAST_SCALE), vs = a.v_scale[size_t(id) * a.hkv + hk];
+      }
+      uint64_t left = __ballot(id >= 0);
+      u32x4 kr[NL], vr[NL];
+      auto pop = [&]() __attribute__((always_inline)) {
+        if (!left) return -1;
+        const int i = __builtin_ctzll(left);
+        left &= left - 1;
+        return i;
+      };
+      auto load = [&](int i) __attribute__((always_inline)) {
+        const size_t p = (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
+#pragma unroll
+        for (int x = 0; x < NL; ++x) kr[x] = *reinterpret_cast<const u32x4 *>(a.k + p + k_src[x]), vr[x] = *reinterpret_cast<const u32x4 *>(a.v + p + v_src[x]);
+      };
+      auto put = [&](uint32_t stage, int i) __attribute__((always_inline)) {
+        const int key0 = __builtin_amdgcn_readlane(at, i) * PAGE;
+        if (key0 + PAGE - 1 > p1 || (key0 < from && key0 + PAGE > a.sinks)) {  // values of tokens that no row sees count nothing, whatever stands there
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t keep = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int j = key0 + 16 * (lane % 4) + 4 * w + e;
+              keep |= j <= p1 && (j >= from || j < a.sinks) ? 0xFFu << (8 * e) : 0u;
+            }
+#pragma unroll
+            for (int x = 0; x < NL; ++x) vr[x][w] &= keep;
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < NL; ++x) {
+          *(CA_LDS bf16x8 *)(stage + k_dst[x]) = codes_to_bf16(kr[x][0], kr[x][1]);
+          *(CA_LDS bf16x8 *)(stage + (k_dst[x] ^ 16)) = codes_to_bf16(kr[x][2], kr[x][3]);
+          *(CA_LDS bf16x8 *)(stage + v_dst[x]) = codes_to_bf16(vr[x][0], vr[x][1]);
+          *(CA_LDS bf16x8 *)(stage + (v_dst[x] ^ 64)) = codes_to_bf16(vr[x][2], vr[x][3]);
+        }
+      };
+      int cur = pop(), next = pop();
+      if (cur >= 0) load(cur), put(0, cur);
+      if (next >= 0) load(next);
+      uint32_t stage = 0;
+      barrier_nofence();
+      while (cur >= 0) {
+        const int after = pop();
+        if (next >= 0) {
+          put(S::STAGE - stage, next);
+          if (after >= 0) load(after);
+        }
+        const int key0 = __builtin_amdgcn_readlane(at, cur) * PAGE;
+        if (key0 <= p1w && (key0 + PAGE > from_w || key0 < a.sinks)) {
+          const float ksi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), cur));
+          const float vsi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), cur));
+          f32x4 x[4][2];
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int f = 0; f < NK; ++f) {
+              const bf16x8 k = lds_read8_at(stage + (koff ^ (64 * f)) + 16 * t * ROWB);
+#pragma unroll
+              for (int rg = 0; rg < 2; ++rg) x[t][rg] = mfma16(k, qf[f][rg], f == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x[t][rg]);
+            }
+          // some row does not see some key: lane (r, j) holds keys key0 + 16 j + 4 t + e
+          if (key0 + PAGE - 1 > p0w || (key0 < p1w - a.window + 1 && key0 + PAGE > a.sinks)) {
+            const int key = key0 + 16 * j4;
+#pragma unroll
+            for (int rg = 0; rg < 2; ++rg)
+#pragma unroll
+              for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int j = key + 4 * t + e;
+                  x[t][rg][e] = j <= hi[rg] && (j >= lo[rg] || j < a.sinks) ? x[t][rg][e] : -INFINITY;
+                }
+          }
+          bf16x8 pb[2][2];
+#pragma unroll
+          for (int rg = 0; rg < 2; ++rg) softmax_page<NB>(x, rg, ksi, vsi, m[rg], l[rg], acc, pb);
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+              const bf16x8 v = lds_read8_at(stage + (voff ^ (64 * kk)) + 16 * b * (2 * PAGE));
+#pragma unroll
+              for (int rg = 0; rg < 2; ++rg) acc[b][rg] = mfma16(v, pb[kk][rg], acc[b][rg]);
+            }
+        }
+        cur = next, next = after, stage = S::STAGE - stage;
+        barrier_nofence();
+      }
+    }
+    const float sum[2] = {quad_sum(l[0]), quad_sum(l[1])};
+    if (n == per_tile) {
+      const float f0 = sum[0] == 0.f ? 0.f : 1.0f / sum[0], f1 = sum[1] == 0.f ? 0.f : 1.0f / sum[1];
+      store_tile16_as_lines<0>(lds0 + wave * PATCH_BYTES, acc, f0, f1, lane, [&](int p) __attribute__((always_inline)) -> bf16_t * {
+        const int r = row_w + p, i = r / G;
+        return r <= last_row ? a.o + (size_t(q.row0 + i) * a.hq + hk * G + r - i * G) * D : nullptr;
+      });
+      const int r = row_w + lane, i = r / G;
+      if (lane < 32 && r <= last_row && a.lse)
+        a.lse[size_t(hk * G + r - i * G) * a.s.total + q.row0 + i] = 0.6931471805599453f * ((lane < 16 ? m[0] : m[1]) + fast_log2(lane < 16 ? sum[0] : sum[1]));
+    } else {
+      const int slot = first == 0 ? 1 : 0;
+      if (slot == 1) head = int4{(u - n + per_tile - 1) / split.run - worker + 1, s, tile, 0};
+      float *const part = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2)) + 32 * wave * D;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int rg = 0; rg < 2; ++rg) *reinterpret_cast<f32x4 *>(part + (16 * rg + li) * D + 16 * b + 4 * j4) = acc[b][rg];
+      float *const ml = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2)) + R * D + 64 * wave;
+      if (lane < 32) ml[2 * lane] = lane < 16 ? m[0] : m[1], ml[2 * lane + 1] = lane < 16 ? sum[0] : sum[1];
+    }
+    __syncthreads();  // the patches lie in the stages
   }
   if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
 }
@@ -653,6 +858,7 @@ static int launched(const char *what, hipError_t e) {
 }
 
 // Workers per KV head: about one workgroup of eight waves, or two of four, for each CU.
+// (NR: 16-row groups of a tile; 8: chunks)
 template <int NR>
 constexpr int WAVES = NR == 1 ? 8 : 4;
 static int n_workers(int hkv, int waves) { return std::max(1, N_CU * 8 / waves / hkv); }
@@ -663,24 +869,26 @@ static size_t attend_bytes(int hkv) {
 }
 static size_t attend_bytes(const ca_cache *c) {
   const int hkv = c->n_kv_heads;
-  return c->head_dim == 128 ? std::max({attend_bytes<128, 1>(hkv), attend_bytes<128, 2>(hkv), attend_bytes<128, 4>(hkv)})
-                            : std::max({attend_bytes<64, 1>(hkv), attend_bytes<64, 2>(hkv), attend_bytes<64, 4>(hkv)});
+  return c->head_dim == 128 ? std::max({attend_bytes<128, 1>(hkv), attend_bytes<128, 2>(hkv), attend_bytes<128, 8>(hkv)})
+                            : std::max({attend_bytes<64, 1>(hkv), attend_bytes<64, 2>(hkv), attend_bytes<64, 8>(hkv)});
 }
 
 template <int D, int NR>
 static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
   constexpr int W = WAVES<NR>;
-  using S = AttendShape<D, NR, W>;
   const int workers = n_workers(a.hkv, W);
   a.heads = static_cast<int4 *>(ws);
   a.parts = reinterpret_cast<float *>(a.heads + size_t(workers) * a.hkv);
-  auto kern = ca_cache_attend_kernel<D, NR, W>;
+  void (*kern)(AttendArgs);
+  size_t bytes;  // of LDS, but for the table of sequences
+  if constexpr (NR == 8) kern = ca_cache_chunk_kernel<D>, bytes = ChunkSmem<D>::TOTAL;
+  else kern = ca_cache_attend_kernel<D, NR, W>, bytes = AttendShape<D, NR, W>::MERGE;
   int device = 0;
   hipError_t e = hipGetDevice(&device);
   static std::atomic<bool> done[16];
-  if (e == hipSuccess) e = set_smem(kern, int(S::smem(MAX_SEQS)), device, done);
+  if (e == hipSuccess) e = set_smem(kern, int(bytes + seq_table_bytes(MAX_SEQS)), device, done);
   if (e != hipSuccess) return launched("cache attention", e);
-  hipLaunchKernelGGL(kern, dim3(unsigned(workers * a.hkv)), dim3(64 * W), S::smem(a.s.n_seqs), st, a);
+  hipLaunchKernelGGL(kern, dim3(unsigned(workers * a.hkv)), dim3(64 * W), bytes + seq_table_bytes(a.s.n_seqs), st, a);
   const int most = 16 * NR;
   hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(workers * a.hkv), unsigned(most / 4)), dim3(256), 0, st, a);
   return launched("cache attention", hipSuccess);
@@ -726,11 +934,11 @@ int ca_cache_attend(const ca_cache *c, const ca_cache_batch *b, int32_t n_q_head
   a.sinks = window == 0 ? 0 : int(std::min<int64_t>(sinks, 1 << 30));
   a.c = (softmax_scale > 0.f ? softmax_scale : c->head_dim == 128 ? 0.08838834764831845f : 0.125f) * 1.4426950408889634f;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  // Rows per tile from the average sequence: what fits 16 rows reads each page once as it is; more rows per tile convert and read a page
-  // less often.
+  // Rows per tile from the average sequence: up to 32 rows a page is converted by the wave that reads it; with more it is converted once
+  // per 128 rows, through LDS.
   const int64_t rows = b->total_rows * g / b->n_seqs;
-  if (c->head_dim == 128) return rows <= 16 ? launch_attend<128, 1>(a, ws, st) : rows <= 32 ? launch_attend<128, 2>(a, ws, st) : launch_attend<128, 4>(a, ws, st);
-  return rows <= 16 ? launch_attend<64, 1>(a, ws, st) : rows <= 32 ? launch_attend<64, 2>(a, ws, st) : launch_attend<64, 4>(a, ws, st);
+  if (c->head_dim == 128) return rows <= 16 ? launch_attend<128, 1>(a, ws, st) : rows <= 32 ? launch_attend<128, 2>(a, ws, st) : launch_attend<128, 8>(a, ws, st);
+  return rows <= 16 ? launch_attend<64, 1>(a, ws, st) : rows <= 32 ? launch_attend<64, 2>(a, ws, st) : launch_attend<64, 8>(a, ws, st);
 }
 
 int ca_cache_append(const ca_cache *c, const ca_cache_batch *b, const void *k, const void *v, void *hip_stream) {
