@@ -25,6 +25,7 @@ constexpr int PAGE = CA_CACHE_PAGE_TOKENS;
 static_assert(PAGE == 64);
 constexpr int MAX_SEQS = 4096;  // their prefix sums lie in LDS
 constexpr float NO_MAX = -3.402823466e38f;
+constexpr float OUTGROWN = 0x1p20f;
 constexpr float LEAST_SCALE = 1.17549435e-38f;  // (a hidden score is -infinity, and that times a scale of 0 would be NaN)
 
 // ------------------------------------------------------------------------------------------------ sequences
@@ -114,7 +115,7 @@ struct AttendArgs {
   bf16_t *o;
   float *lse;
   float *parts;  // [worker][2][KV head][R rows][D] and then [R][2] {running maximum, sum}
-  int4 *heads;   // [worker][KV head]: {parts of the tile that begins in this worker and is cut, its sequence, its tile, -}
+  int4 *heads;   // [worker][KV head], of the tile that begins in this worker and is cut: {parts, first row of its sequence, first and last row}
   int hq, hkv, window, sinks;
   float c;  // softmax_scale * log2(e)
 };
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(64 * W, 2) void ca_cache_attend_kernel(const Attend
     const bool whole = n == per_tile;
     const int slot = first == 0 ? 1 : 0;
     float *const part = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2));
-    if (!whole && slot == 1) head = int4{(u - n + per_tile - 1) / split.run - worker + 1, s, tile, 0};
+    if (!whole && slot == 1) head = int4{(u - n + per_tile - 1) / split.run - worker + 1, q.row0, tile * R, last_row};
     float factor[NR];
 #pragma unroll
     for (int rg = 0; rg < NR; ++rg) {
@@ -448,13 +449,16 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
     }
     for (int base = 0; base < n; base += 64) {  // 64 pages at a time: their ids and scales, one per lane
       int id = -1, at = 0;
-      float ks = 0.f, vs = 0.f;
+      float ks = 0.f, vs = 1.f, lv = 0.f, iv = 1.f;
       if (base + lane < n) {
         const int i = first + base + lane;
         at = i < n_sink ? i : from / PAGE + i - n_sink;
         if (at * PAGE <= p1) id = a.s.table[size_t(s) * a.s.width + at];
         if (id >= a.s.n_pages) id = -1;
         if (id >= 0) ks = fmaxf(a.k_scale[size_t(id) * a.hkv + hk] * a.c, LEAST_SCALE), vs = a.v_scale[size_t(id) * a.hkv + hk];
+        // The scale of V goes into the exponent: exp2(x - m + lv) = P vs, and their sum times iv is that of P.  Not where that could
+        // leave the normal range.
+        if (vs > 0x1p-40f && vs < 0x1p40f) lv = fast_log2(vs), iv = fast_exp2(-lv);
       }
       uint64_t left = __ballot(id >= 0);
       u32x4 kr[NL], vr[NL];
@@ -505,41 +509,106 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
         }
         const int key0 = __builtin_amdgcn_readlane(at, cur) * PAGE;
         if (key0 <= p1w && (key0 + PAGE > from_w || key0 < a.sinks)) {
-          const float ksi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), cur));
-          const float vsi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), cur));
-          f32x4 x[4][2];
+          auto of_page = [&](float x) __attribute__((always_inline)) {
+            return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), cur));
+          };
+          const float ksi = of_page(ks), vsi = of_page(vs), lvi = of_page(lv), ivi = of_page(iv);
+          const bool hidden = key0 + PAGE - 1 > p0w || (key0 < p1w - a.window + 1 && key0 + PAGE > a.sinks);  // some row does not see some key
+          // Fragments come from LDS AHEAD fragments before the MFMAs that use them: per half of 32 keys 2 NK of K and NB of V^T.  The
+          // exponentials of the first tile go between the score MFMAs of the second; fences keep that order.
+          constexpr int NF = 2 * NK + NB, AHEAD = 4;
+          {
+            bf16x8 fr[AHEAD];
+            auto fetch = [&](int i) __attribute__((always_inline)) -> bf16x8 {
+              const int kk = i / NF, f = i % NF;
+              return f < 2 * NK ? lds_read8_at(stage + (koff ^ (64 * (f % NK))) + 16 * (2 * kk + f / NK) * ROWB)
+                                : lds_read8_at(stage + (voff ^ (64 * kk)) + 16 * (f - 2 * NK) * (2 * PAGE));
+            };
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int f = 0; f < NK; ++f) {
-              const bf16x8 k = lds_read8_at(stage + (koff ^ (64 * f)) + 16 * t * ROWB);
-#pragma unroll
-              for (int rg = 0; rg < 2; ++rg) x[t][rg] = mfma16(k, qf[f][rg], f == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x[t][rg]);
-            }
-          // some row does not see some key: lane (r, j) holds keys key0 + 16 j + 4 t + e
-          if (key0 + PAGE - 1 > p0w || (key0 < p1w - a.window + 1 && key0 + PAGE > a.sinks)) {
-            const int key = key0 + 16 * j4;
-#pragma unroll
-            for (int rg = 0; rg < 2; ++rg)
-#pragma unroll
-              for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int j = key + 4 * t + e;
-                  x[t][rg][e] = j <= hi[rg] && (j >= lo[rg] || j < a.sinks) ? x[t][rg][e] : -INFINITY;
-                }
-          }
-          bf16x8 pb[2][2];
-#pragma unroll
-          for (int rg = 0; rg < 2; ++rg) softmax_page<NB>(x, rg, ksi, vsi, m[rg], l[rg], acc, pb);
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
+            for (int i = 0; i < AHEAD; ++i) fr[i] = fetch(i);
+            int now = 0;  // the fragment in use
+            auto advance = [&]() __attribute__((always_inline)) {
+              if (now + AHEAD < 2 * NF) fr[now % AHEAD] = fetch(now + AHEAD);
+              ++now;
+              __builtin_amdgcn_sched_barrier(0);
+            };
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
-              const bf16x8 v = lds_read8_at(stage + (voff ^ (64 * kk)) + 16 * b * (2 * PAGE));
+              f32x4 x[2][2];
+              uint32_t w[2][4];
+              float sum[2] = {0.f, 0.f};
+              // probabilities times the scale of V of tile t and row group rg, relative to the reference as it stands
+              auto expo = [&](int t, int rg) __attribute__((always_inline)) {
+                float p[4];
 #pragma unroll
-              for (int rg = 0; rg < 2; ++rg) acc[b][rg] = mfma16(v, pb[kk][rg], acc[b][rg]);
+                for (int e = 0; e < 4; ++e) p[e] = fast_exp2(fmaf(x[t][rg][e], ksi, lvi - m[rg]));
+                sum[rg] += (p[0] + p[1]) + (p[2] + p[3]);
+                w[rg][2 * t] = pack_bf16(p[0], p[1]), w[rg][2 * t + 1] = pack_bf16(p[2], p[3]);
+              };
+              auto mask = [&](int t) __attribute__((always_inline)) {  // lane (r, j) holds keys key0 + 16 j + 8 kk + 4 t + e
+                if (!hidden) return;
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg) {
+                  const int base = key0 + 16 * j4 + 8 * kk + 4 * t, vis = hi[rg] - base, begins = lo[rg] - base, sink_end = a.sinks - base;
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) x[t][rg][e] = e <= vis && (e >= begins || e < sink_end) ? x[t][rg][e] : -INFINITY;
+                }
+              };
+#pragma unroll
+              for (int f = 0; f < 2 * NK; ++f) {
+                const int t = f / NK;
+                if (f == NK) mask(0);
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg) x[t][rg] = mfma16(fr[now % AHEAD], qf[f % NK][rg], f % NK == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : x[t][rg]);
+                if (t == 1) {
+#pragma unroll
+                  for (int rg = 2 * (f - NK) / NK; rg < 2 * (f - NK + 1) / NK; ++rg) expo(0, rg);
+                }
+                advance();
+              }
+              mask(1);
+#pragma unroll
+              for (int rg = 0; rg < 2; ++rg) {
+                expo(1, rg);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+              // The reference is moved when it has been outgrown by far (or there is none yet): probabilities relative to a stale one are
+              // merely larger numbers.
+              if (__any(!(sum[0] * ivi < OUTGROWN && sum[1] * ivi < OUTGROWN))) {
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg) {
+                  float top = x[0][rg][0];
+#pragma unroll
+                  for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, x[t][rg][e]);
+                  const float grown = fmaxf(m[rg], quad_max(top * ksi)), f = m[rg] == NO_MAX ? 0.f : fast_exp2(m[rg] - grown);
+                  m[rg] = grown, l[rg] *= f, sum[rg] = 0.f;
+#pragma unroll
+                  for (int b = 0; b < NB; ++b) acc[b][rg] *= f;
+                  expo(0, rg), expo(1, rg);
+                }
+              }
+              bf16x8 pb[2];
+#pragma unroll
+              for (int rg = 0; rg < 2; ++rg) {
+                l[rg] = fmaf(sum[rg], ivi, l[rg]);
+                pb[rg] = __builtin_bit_cast(bf16x8, u32x4{w[rg][0], w[rg][1], w[rg][2], w[rg][3]});
+              }
+              if (lvi == 0.f && vsi != 1.f) {  // a scale of V that the exponent does not take
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg)
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) pb[rg][i] = bf16_t(float(pb[rg][i]) * vsi);
+              }
+#pragma unroll
+              for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                for (int rg = 0; rg < 2; ++rg) acc[b][rg] = mfma16(fr[now % AHEAD], pb[rg], acc[b][rg]);
+                advance();
+              }
             }
+          }
         }
         cur = next, next = after, stage = S::STAGE - stage;
         barrier_nofence();
@@ -557,7 +626,7 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
         a.lse[size_t(hk * G + r - i * G) * a.s.total + q.row0 + i] = 0.6931471805599453f * ((lane < 16 ? m[0] : m[1]) + fast_log2(lane < 16 ? sum[0] : sum[1]));
     } else {
       const int slot = first == 0 ? 1 : 0;
-      if (slot == 1) head = int4{(u - n + per_tile - 1) / split.run - worker + 1, s, tile, 0};
+      if (slot == 1) head = int4{(u - n + per_tile - 1) / split.run - worker + 1, q.row0, tile * R, last_row};
       float *const part = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2)) + 32 * wave * D;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -571,47 +640,58 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
   if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
 }
 
-// Adds up the parts of the tiles that were cut: one wave per row, two parts at a time; the order is fixed.
+// Adds up the parts of the tiles that were cut, in their order: a wave takes RW rows, and two (four) parts of each at a time.
 template <int D, int NR>
 __global__ __launch_bounds__(256) void ca_cache_combine_kernel(const AttendArgs a) {
-  constexpr int R = 16 * NR, LANES = D / 4, AT_A_TIME = 64 / LANES;
+  constexpr int R = 16 * NR, LANES = D / 4, AT_A_TIME = 64 / LANES, RW = NR == 8 ? 4 : 1;
   const int hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv;
-  const int4 head = a.heads[worker * a.hkv + hk];
-  if (head.x < 2) return;
-  const int G = a.hq / a.hkv, lane = threadIdx.x & 63, r = 4 * blockIdx.y + (threadIdx.x >> 6);
-  const Seq q = seq_of(a.s, head.y);
-  const int at = head.z * R + r;
-  if (at >= q.n * G) return;
+  const int4 head = a.heads[worker * a.hkv + hk];  // {parts, first row of the sequence, first row of the tile, last row of the tile}
+  const int G = a.hq / a.hkv, lane = threadIdx.x & 63, r0 = RW * (4 * blockIdx.y + (threadIdx.x >> 6));
+  if (head.x < 2 || head.z + r0 > head.w) return;
   const size_t stride = size_t(2 * a.hkv) * (R * (D + 2));
   const float *const first = a.parts + size_t((worker * 2 + 1) * a.hkv + hk) * (R * (D + 2));
   const float *const others = first + stride - size_t(a.hkv) * (R * (D + 2));
   auto part = [&](int i) { return i == 0 ? first : others + size_t(i - 1) * stride; };
-  float top = NO_MAX;
-  for (int i = lane; i < head.x; i += 64) top = fmaxf(top, part(i)[R * D + 2 * r]);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f;
   const int mine = lane / LANES, col = 4 * (lane % LANES);
-#pragma unroll 8
+  f32x4 y[RW];
+  float top[RW], sum[RW];
+#pragma unroll
+  for (int x = 0; x < RW; ++x) top[x] = NO_MAX, sum[x] = 0.f, y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = lane; i < head.x; i += 64) {
+#pragma unroll
+    for (int x = 0; x < RW; ++x)
+      if (head.z + r0 + x <= head.w) top[x] = fmaxf(top[x], part(i)[R * D + 2 * (r0 + x)]);
+  }
+#pragma unroll
+  for (int x = 0; x < RW; ++x)
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top[x] = fmaxf(top[x], __shfl_xor(top[x], o));
+#pragma unroll RW == 1 ? 8 : 2
   for (int i = mine; i < head.x; i += AT_A_TIME) {
     const float *const p = part(i);
-    const float w = fast_exp2(p[R * D + 2 * r] - top);
-    sum += w * p[R * D + 2 * r + 1];
-    y += w * *reinterpret_cast<const f32x4 *>(p + r * D + col);
+#pragma unroll
+    for (int x = 0; x < RW; ++x) {
+      if (head.z + r0 + x > head.w) continue;
+      const float w = fast_exp2(p[R * D + 2 * (r0 + x)] - top[x]);
+      sum[x] += w * p[R * D + 2 * (r0 + x) + 1];
+      y[x] += w * *reinterpret_cast<const f32x4 *>(p + (r0 + x) * D + col);
+    }
   }
 #pragma unroll
-  for (int o = LANES; o < 64; o <<= 1) {
-    sum += __shfl_xor(sum, o);
+  for (int x = 0; x < RW; ++x) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], o);
+    for (int o = LANES; o < 64; o <<= 1) {
+      sum[x] += __shfl_xor(sum[x], o);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[x][e] += __shfl_xor(y[x][e], o);
+    }
+    const int at = head.z + r0 + x, token = at / G, h = hk * G + at - token * G;
+    if (mine != 0 || at > head.w) continue;
+    const float inv = sum[x] == 0.f ? 0.f : 1.0f / sum[x];
+    *reinterpret_cast<u32x2 *>(a.o + (size_t(head.y + token) * a.hq + h) * D + col) =
+        u32x2{pack_bf16(y[x][0] * inv, y[x][1] * inv), pack_bf16(y[x][2] * inv, y[x][3] * inv)};
+    if (col == 0 && a.lse) a.lse[size_t(h) * a.s.total + head.y + token] = 0.6931471805599453f * (top[x] + fast_log2(sum[x]));
   }
-  if (mine != 0) return;
-  const int token = at / G, h = hk * G + at - token * G;
-  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-  *reinterpret_cast<u32x2 *>(a.o + (size_t(q.row0 + token) * a.hq + h) * D + col) =
-      u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
-  if (col == 0 && a.lse) a.lse[size_t(h) * a.s.total + q.row0 + token] = 0.6931471805599453f * (top + fast_log2(sum));
 }
 
 // ------------------------------------------------------------------------------------------------ append
@@ -889,8 +969,7 @@ static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
   if (e == hipSuccess) e = set_smem(kern, int(bytes + seq_table_bytes(MAX_SEQS)), device, done);
   if (e != hipSuccess) return launched("cache attention", e);
   hipLaunchKernelGGL(kern, dim3(unsigned(workers * a.hkv)), dim3(64 * W), bytes + seq_table_bytes(a.s.n_seqs), st, a);
-  const int most = 16 * NR;
-  hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(workers * a.hkv), unsigned(most / 4)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(workers * a.hkv), NR == 8 ? 8 : 4 * NR), dim3(256), 0, st, a);
   return launched("cache attention", hipSuccess);
 }
 
