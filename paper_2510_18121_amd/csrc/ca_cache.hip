@@ -413,7 +413,7 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
     v_src[n] = uint32_t(d) * PAGE + 16 * j;
     v_dst[n] = lds0 + S::V_OFF + d * (2 * PAGE) + 16 * (j ^ tile_sw<64>(d));        // (... ^ 64)
   }
-  const uint32_t koff = lds0 + li * ROWB + 16 * (j4 ^ tile_sw<D>(li)), voff = lds0 + S::V_OFF + li * (2 * PAGE) + 16 * (j4 ^ tile_sw<64>(li));
+  uint32_t koff = lds0 + li * ROWB + 16 * (j4 ^ tile_sw<D>(li)), voff = lds0 + S::V_OFF + li * (2 * PAGE) + 16 * (j4 ^ tile_sw<64>(li)), stage = 0;
 
   for (int u = begin, s = begin < end ? find_unit(tab.pre, a.s.n_seqs, begin) : 0; u < end;) {
     while (tab.pre[s + 1] <= u) ++s;
@@ -499,14 +499,10 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
       int cur = pop(), next = pop();
       if (cur >= 0) load(cur), put(0, cur);
       if (next >= 0) load(next);
-      uint32_t stage = 0;
+      koff -= stage, voff -= stage, stage = 0;
       barrier_nofence();
       while (cur >= 0) {
         const int after = pop();
-        if (next >= 0) {
-          put(S::STAGE - stage, next);
-          if (after >= 0) load(after);
-        }
         const int key0 = __builtin_amdgcn_readlane(at, cur) * PAGE;
         if (key0 <= p1w && (key0 + PAGE > from_w || key0 < a.sinks)) {
           auto of_page = [&](float x) __attribute__((always_inline)) {
@@ -521,8 +517,8 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
             bf16x8 fr[AHEAD];
             auto fetch = [&](int i) __attribute__((always_inline)) -> bf16x8 {
               const int kk = i / NF, f = i % NF;
-              return f < 2 * NK ? lds_read8_at(stage + (koff ^ (64 * (f % NK))) + 16 * (2 * kk + f / NK) * ROWB)
-                                : lds_read8_at(stage + (voff ^ (64 * kk)) + 16 * (f - 2 * NK) * (2 * PAGE));
+              return f < 2 * NK ? lds_read8_at((koff ^ (64 * (f % NK))) + 16 * (2 * kk + f / NK) * ROWB)
+                                : lds_read8_at((voff ^ (64 * kk)) + 16 * (f - 2 * NK) * (2 * PAGE));
             };
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) fr[i] = fetch(i);
@@ -547,6 +543,7 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
               };
               auto mask = [&](int t) __attribute__((always_inline)) {  // lane (r, j) holds keys key0 + 16 j + 8 kk + 4 t + e
                 if (!hidden) return;
+                asm volatile("");  // (a branch, not 16 selects on every page)
 #pragma unroll
                 for (int rg = 0; rg < 2; ++rg) {
                   const int base = key0 + 16 * j4 + 8 * kk + 4 * t, vis = hi[rg] - base, begins = lo[rg] - base, sink_end = a.sinks - base;
@@ -610,7 +607,13 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
             }
           }
         }
-        cur = next, next = after, stage = S::STAGE - stage;
+        if (next >= 0) {
+          put(S::STAGE - stage, next);
+          if (after >= 0) load(after);
+        }
+        cur = next, next = after;
+        koff += S::STAGE - 2 * stage, voff += S::STAGE - 2 * stage;
+        stage = S::STAGE - stage;
         barrier_nofence();
       }
     }
@@ -657,33 +660,27 @@ __global__ __launch_bounds__(256) void ca_cache_combine_kernel(const AttendArgs 
   float top[RW], sum[RW];
 #pragma unroll
   for (int x = 0; x < RW; ++x) top[x] = NO_MAX, sum[x] = 0.f, y[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i = lane; i < head.x; i += 64) {
+  auto add = [&](int x, float m, float l, const f32x4 &z) __attribute__((always_inline)) {
+    const float grown = fmaxf(top[x], m), old = fast_exp2(top[x] - grown), w = fast_exp2(m - grown);
+    top[x] = grown, sum[x] = sum[x] * old + w * l;
 #pragma unroll
-    for (int x = 0; x < RW; ++x)
-      if (head.z + r0 + x <= head.w) top[x] = fmaxf(top[x], part(i)[R * D + 2 * (r0 + x)]);
-  }
-#pragma unroll
-  for (int x = 0; x < RW; ++x)
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top[x] = fmaxf(top[x], __shfl_xor(top[x], o));
+    for (int e = 0; e < 4; ++e) y[x][e] = y[x][e] * old + w * z[e];
+  };
+  // (rows behind the tile's last one are read and not stored: their parts are whatever the workers left there)
 #pragma unroll RW == 1 ? 8 : 2
   for (int i = mine; i < head.x; i += AT_A_TIME) {
-    const float *const p = part(i);
+    const float *const p = part(i) + r0 * D + col, *const ml = part(i) + R * D + 2 * r0;
 #pragma unroll
-    for (int x = 0; x < RW; ++x) {
-      if (head.z + r0 + x > head.w) continue;
-      const float w = fast_exp2(p[R * D + 2 * (r0 + x)] - top[x]);
-      sum[x] += w * p[R * D + 2 * (r0 + x) + 1];
-      y[x] += w * *reinterpret_cast<const f32x4 *>(p + (r0 + x) * D + col);
-    }
+    for (int x = 0; x < RW; ++x) add(x, ml[2 * x], ml[2 * x + 1], *reinterpret_cast<const f32x4 *>(p + x * D));
   }
 #pragma unroll
   for (int x = 0; x < RW; ++x) {
 #pragma unroll
     for (int o = LANES; o < 64; o <<= 1) {
-      sum[x] += __shfl_xor(sum[x], o);
+      f32x4 z;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[x][e] += __shfl_xor(y[x][e], o);
+      for (int e = 0; e < 4; ++e) z[e] = __shfl_xor(y[x][e], o);
+      add(x, __shfl_xor(top[x], o), __shfl_xor(sum[x], o), z);
     }
     const int at = head.z + r0 + x, token = at / G, h = hk * G + at - token * G;
     if (mine != 0 || at > head.w) continue;
