@@ -45,66 +45,86 @@ __device__ __forceinline__ Seq seq_of(const SeqArgs &a, int s) {
   return q;
 }
 
-// What the workgroup keeps of the sequences in LDS: pre[i] = sum of the units of sequences 0 .. i - 1, and the sequences themselves, so
-// that finding a unit and its sequence costs no trip to memory.  (Sums stop growing at MOST_UNITS: only sequences that overlap,
-// against their description, come so far, and then nothing overflows.)
+// The sequences as a wave finds them: how many units of work lie before each, and itself, without a trip to memory.  Up to 64 are in
+// the lanes of every wave (one token of one sequence: 2.7K cycles to the first unit fewer than through LDS and its barriers), more in LDS.
+// (Sums stop growing at MOST_UNITS: only sequences that overlap, against their description, come so far, and then nothing overflows.)
 constexpr int MOST_UNITS = (1 << 30) - 1;
 __device__ __forceinline__ int sum_units(int a, int b) { return min(a + b, MOST_UNITS); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_lanes(int x) {
+  return sum_units(x, __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ int wave_prefix(int x) {  // inclusive
+  x = add_lanes<0x111, 0xF>(x);  // row_shr 1, 2, 4, 8: inside each 16 lanes
+  x = add_lanes<0x112, 0xF>(x);
+  x = add_lanes<0x114, 0xF>(x);
+  x = add_lanes<0x118, 0xF>(x);
+  x = add_lanes<0x142, 0xA>(x);         // the last lane of the 16 before
+  return add_lanes<0x143, 0xC>(x);      // ... and of the 32 before
+}
+constexpr size_t seq_table_bytes(int n_seqs) { return n_seqs <= 64 ? 0 : 64 + size_t(n_seqs + 4) / 4 * 16 * 4; }
 struct SeqTable {
-  int *wave_sums, *pre, *row0, *n, *len;
+  int n_seqs;
+  Seq mine;         // up to 64 sequences: of this lane,
+  int upto;         // and the units up to it and with it
+  int *wave_sums, *pre, *row0, *n, *len;  // more
+
+  // for all threads of the workgroup (T); returns the sum of all units
+  template <int T, class F>
+  __device__ __forceinline__ int fill(void *lds, const SeqArgs &a, F units) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    n_seqs = a.n_seqs;
+    if (n_seqs <= 64) {
+      mine = seq_of(a, min(lane, n_seqs - 1));
+      upto = wave_prefix(lane < n_seqs ? units(mine) : 0);
+      return __builtin_amdgcn_readlane(upto, 63);
+    }
+    const int stride = (n_seqs + 4) / 4 * 4;
+    wave_sums = static_cast<int *>(lds), pre = wave_sums + 16, row0 = pre + stride, n = row0 + stride, len = n + stride;
+    int carry = 0;
+    for (int base = 0; base < n_seqs; base += T) {
+      const int i = base + int(threadIdx.x);
+      int x = 0;
+      if (i < n_seqs) {
+        const Seq q = seq_of(a, i);
+        row0[i] = q.row0, n[i] = q.n, len[i] = q.len;
+        x = units(q);
+      }
+      x = wave_prefix(x);
+      if (lane == 63) wave_sums[wave] = x;
+      __syncthreads();
+      int before = carry;
+#pragma unroll
+      for (int w = 0; w < T / 64; ++w) {
+        const int sum = wave_sums[w];
+        before = sum_units(before, w < wave ? sum : 0);
+        carry = sum_units(carry, sum);
+      }
+      if (i < n_seqs) pre[i + 1] = sum_units(before, x);
+      if (i == 0) pre[0] = 0;
+      __syncthreads();
+    }
+    return __builtin_amdgcn_readfirstlane(carry);
+  }
   __device__ __forceinline__ Seq at(int s) const {
+    if (n_seqs <= 64) return {__builtin_amdgcn_readlane(mine.row0, s), __builtin_amdgcn_readlane(mine.n, s), __builtin_amdgcn_readlane(mine.len, s)};
     return {__builtin_amdgcn_readfirstlane(row0[s]), __builtin_amdgcn_readfirstlane(n[s]), __builtin_amdgcn_readfirstlane(len[s])};
   }
+  __device__ __forceinline__ int before(int s) const {  // units of the sequences before s
+    if (n_seqs <= 64) return s == 0 ? 0 : __builtin_amdgcn_readlane(upto, s - 1);
+    return __builtin_amdgcn_readfirstlane(pre[s]);
+  }
+  __device__ __forceinline__ int find(int u) const {  // the sequence that has unit u (less than all units)
+    if (n_seqs <= 64) return __builtin_popcountll(__ballot(upto <= u));
+    int lo = 0, hi = n_seqs;  // pre[lo] <= u < pre[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pre[mid] <= u) lo = mid;
+      else hi = mid;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+  }
 };
-constexpr size_t seq_table_bytes(int n_seqs) { return 64 + size_t(n_seqs + 4) / 4 * 16 * 4; }
-__device__ __forceinline__ SeqTable seq_table(void *lds, int n_seqs) {
-  const int stride = (n_seqs + 4) / 4 * 4;
-  int *const p = static_cast<int *>(lds);
-  return {p, p + 16, p + 16 + stride, p + 16 + 2 * stride, p + 16 + 3 * stride};
-}
-// fills the table for all threads of the workgroup; returns the sum of all units
-template <int T, class F>
-__device__ __forceinline__ int fill_table(const SeqTable &tab, const SeqArgs &a, F units) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int carry = 0;
-  for (int base = 0; base < a.n_seqs; base += T) {
-    const int i = base + int(threadIdx.x);
-    int x = 0;
-    if (i < a.n_seqs) {
-      const Seq q = seq_of(a, i);
-      tab.row0[i] = q.row0, tab.n[i] = q.n, tab.len[i] = q.len;
-      x = units(q);
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(x, o);
-      if (lane >= o) x = sum_units(x, y);
-    }
-    if (lane == 63) tab.wave_sums[wave] = x;
-    __syncthreads();
-    int before = carry;
-#pragma unroll
-    for (int w = 0; w < T / 64; ++w) {
-      const int sum = tab.wave_sums[w];
-      before = sum_units(before, w < wave ? sum : 0);
-      carry = sum_units(carry, sum);
-    }
-    if (i < a.n_seqs) tab.pre[i + 1] = sum_units(before, x);
-    if (i == 0) tab.pre[0] = 0;
-    __syncthreads();
-  }
-  return __builtin_amdgcn_readfirstlane(carry);
-}
-// the entry whose run of units holds unit u < pre[n]
-__device__ __forceinline__ int find_unit(const int *pre, int n, int u) {
-  int lo = 0, hi = n;  // pre[lo] <= u < pre[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (pre[mid] <= u) lo = mid;
-    else hi = mid;
-  }
-  return __builtin_amdgcn_readfirstlane(lo);
-}
 
 // ------------------------------------------------------------------------------------------------ attention
 struct AttendArgs {
@@ -117,7 +137,12 @@ struct AttendArgs {
   float *parts;  // [worker][2][KV head][R rows][D] and then [R][2] {running maximum, sum}
   int4 *heads;   // [worker][KV head], of the tile that begins in this worker and is cut: {parts, first row of its sequence, first and last row}
   int hq, hkv, window, sinks;
-  float c;  // softmax_scale * log2(e)
+  int G;          // query heads per KV head
+  uint32_t by_g;  // 2^32 / G, rounded up: x / G is the high word of x * by_g for x < 2^32 / G (G > 1)
+  float c;        // softmax_scale * log2(e)
+  float by_workers;  // a little more than 1 / (workers per KV head)
+
+  __device__ __forceinline__ int token_of(int row) const { return G == 1 ? row : int(__umulhi(uint32_t(row), by_g)); }
 };
 
 // Rows of a sequence and KV head, token by token and then by head of the group, make up tiles of R = 16 NR; a unit of work is a page
@@ -138,23 +163,33 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b) {
   return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
+// x / y of two uniform numbers, x >= 0, y > 0.  (A 32-bit division is 40 dependent instructions; below 2^24 a quotient in fp32 is off by
+// at most one.)
+__device__ __forceinline__ int quotient(int x, int y) {
+  if (x >= 1 << 24) return x / y;
+  const int q = int(float(x) * __builtin_amdgcn_rcpf(float(y))), r = x - q * y;
+  return __builtin_amdgcn_readfirstlane(q + (r >= y) - (r < 0));
+}
+
 // The workers' shares of the units: worker w has units bound(w) .. bound(w + 1) - 1.
 struct WorkSplit {
   SeqTable tab;
-  int n_seqs, total, run, R, G, window, sinks;
+  int total, run, R, G, window, sinks;
+  template <int T>
+  __device__ __forceinline__ void make(void *lds, const AttendArgs &a, int rows, int n_workers, int least) {
+    R = rows, G = a.G, window = a.window, sinks = a.sinks;
+    total = tab.fill<T>(lds, a.s, [&](const Seq &q) { return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, window, sinks); });
+    run = max(least, n_workers == 1 ? total : __builtin_amdgcn_readfirstlane(int(float(total) * a.by_workers)) + 1);
+  }
   __device__ __forceinline__ int bound(int w) const {
-    const int u = min(w, (total + run - 1) / run) * run;
-    if (u >= total || u == 0) return min(u, total);
-    const int s = find_unit(tab.pre, n_seqs, u), n = tile_pages(tab.at(s).len, R, G, window, sinks);
-    const int into = __builtin_amdgcn_readfirstlane(u - tab.pre[s]) % n;
-    return n > CUT ? u : 2 * into < n ? u - into : u - into + n;
+    const int u = min(w * run, total);
+    if (u >= total || u == 0) return u;
+    const int s = tab.find(u), n = tile_pages(tab.at(s).len, R, G, window, sinks);
+    if (n > CUT) return u;
+    const int x = u - tab.before(s), into = x - quotient(x, n) * n;
+    return 2 * into < n ? u - into : u - into + n;
   }
 };
-template <int T>
-__device__ __forceinline__ WorkSplit split_work(const SeqTable &tab, const AttendArgs &a, int R, int G, int n_workers, int least) {
-  const int total = fill_table<T>(tab, a.s, [&](const Seq &q) { return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, a.window, a.sinks); });
-  return {tab, a.s.n_seqs, total, max(least, (total + n_workers - 1) / n_workers), R, G, a.window, a.sinks};
-}
 
 // Scores x of a page (of row group rg; -infinity where a key is not seen) to the operand of P V; ks and vs: the page's scales, ks with
 // the softmax's factor in base 2.  The reference m moves when some row's maximum has grown by more than 2^8 (see the forward kernel).
@@ -193,43 +228,35 @@ struct AttendShape {
 };
 
 template <int D, int NR, int W>
-__global__ __launch_bounds__(64 * W, 2) void ca_cache_attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kernel(const AttendArgs a) {
   using S = AttendShape<D, NR, W>;
   constexpr int R = S::R, NH = D / 64, NB = D / 16;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const SeqTable tab = seq_table(smem, a.s.n_seqs);
-  float *const merge = reinterpret_cast<float *>(smem + seq_table_bytes(a.s.n_seqs)), *const merge_ml = merge + W * R * S::ROW;
+  float *const merge = reinterpret_cast<float *>(smem), *const merge_ml = merge + W * R * S::ROW;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j4 = lane >> 4, li = lane & 15;
-  const int G = a.hq / a.hkv, hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv, n_workers = gridDim.x / a.hkv;
-
-  const WorkSplit split = split_work<64 * W>(tab, a, R, G, n_workers, W);
+  const int G = a.G, n_workers = gridDim.y, worker = blockIdx.y, hk = blockIdx.x;
+  WorkSplit split;
+  split.make<64 * W>(smem + S::MERGE, a, R, n_workers, W);
+  const SeqTable &tab = split.tab;
   const int begin = split.bound(worker), end = split.bound(worker + 1);
   int4 head = {0, 0, 0, 0};
+  const uint32_t k_lane = uint32_t(16 * (li >> 2) + (li & 3)) * D + 16 * j4, v_lane = uint32_t(li) * PAGE + 16 * j4;
 
-  for (int u = begin, s = begin < end ? find_unit(tab.pre, a.s.n_seqs, begin) : 0; u < end;) {
-    while (tab.pre[s + 1] <= u) ++s;
-    s = __builtin_amdgcn_readfirstlane(s);
+  for (int u = begin; u < end;) {
+    const int s = tab.find(u), in_seq = u - tab.before(s);
     const Seq q = tab.at(s);
     const int per_tile = tile_pages(q.len, R, G, a.window, a.sinks);
-    const int tile = __builtin_amdgcn_readfirstlane((u - tab.pre[s]) / per_tile), first = __builtin_amdgcn_readfirstlane((u - tab.pre[s]) % per_tile);
+    const int tile = quotient(in_seq, per_tile), first = in_seq - tile * per_tile;
     const int n = min(end - u, per_tile - first);
     u += n;
     // the rows
     const int last_row = min((tile + 1) * R, q.n * G) - 1, pos0 = q.len - q.n;
-    const int p0 = pos0 + tile * R / G, p1 = pos0 + last_row / G;  // of the tile's first and last row
-    const int from = max(0, p0 - a.window + 1);                    // the first key of a window that some row has
+    const int p0 = pos0 + a.token_of(tile * R), p1 = pos0 + a.token_of(last_row);  // of the tile's first and last row
+    const int from = max(0, p0 - a.window + 1);                                    // the first key of a window that some row has
     const int n_sink = min((a.sinks + PAGE - 1) / PAGE, from / PAGE);
     int hi[NR], lo[NR];
     bf16x8 qf[2 * NH][NR];
-#pragma unroll
-    for (int rg = 0; rg < NR; ++rg) {
-      const int r = tile * R + 16 * rg + li, ok = r <= last_row, i = ok ? r / G : 0, h = hk * G + (ok ? r - i * G : 0);
-      hi[rg] = ok ? pos0 + i : -1, lo[rg] = max(0, pos0 + i - a.window + 1);
-      const bf16_t *const qp = a.q + (size_t(q.row0 + i) * a.hq + h) * D + 16 * j4;
-#pragma unroll
-      for (int f = 0; f < 2 * NH; ++f) qf[f][rg] = *reinterpret_cast<const bf16x8 *>(qp + 64 * (f >> 1) + 8 * (f & 1));
-    }
     f32x4 acc[NB][NR];
     float m[NR], l[NR];
 #pragma unroll
@@ -240,31 +267,49 @@ __global__ __launch_bounds__(64 * W, 2) void ca_cache_attend_kernel(const Attend
     }
     // pages first + wave, first + wave + W, ..: their ids and scales, 64 at a time, one per lane
     const int n_mine = (n - wave + W - 1) / W;
-    for (int base = 0; base < n_mine; base += 64) {
+    for (int base = 0; base == 0 || base < n_mine; base += 64) {
       int id = -1, at = 0;
-      float ks = 0.f, vs = 0.f;
       if (base + lane < n_mine) {
         const int i = first + wave + W * (base + lane);
         at = i < n_sink ? i : from / PAGE + i - n_sink;
         if (at * PAGE <= p1) id = a.s.table[size_t(s) * a.s.width + at];
         if (id >= a.s.n_pages) id = -1;
-        if (id >= 0) ks = fmaxf(a.k_scale[size_t(id) * a.hkv + hk] * a.c, LEAST_SCALE), vs = a.v_scale[size_t(id) * a.hkv + hk];
+      }
+      if (base == 0) {
+#pragma unroll
+        for (int rg = 0; rg < NR; ++rg) {
+          const int r = tile * R + 16 * rg + li, ok = r <= last_row, i = ok ? a.token_of(r) : 0, h = hk * G + (ok ? r - i * G : 0);
+          hi[rg] = ok ? pos0 + i : -1, lo[rg] = max(0, pos0 + i - a.window + 1);
+          const bf16_t *const qp = a.q + (size_t(q.row0 + i) * a.hq + h) * D + 16 * j4;
+#pragma unroll
+          for (int f = 0; f < 2 * NH; ++f) qf[f][rg] = *reinterpret_cast<const bf16x8 *>(qp + 64 * (f >> 1) + 8 * (f & 1));
+        }
       }
       uint64_t left = __ballot(id >= 0);
-      const uint32_t k_lane = uint32_t(16 * (li >> 2) + (li & 3)) * D + 16 * j4, v_lane = uint32_t(li) * PAGE + 16 * j4;
+      auto pop = [&]() __attribute__((always_inline)) {
+        if (!left) return -1;
+        const int i = __builtin_ctzll(left);
+        left &= left - 1;
+        return i;
+      };
       u32x4 kr[4 * NH], vr[NB];
-      auto load_k = [&](int i) {
+      auto load_k = [&](int i) __attribute__((always_inline)) {
         const uint8_t *const p = a.k + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
 #pragma unroll
         for (int f = 0; f < 4 * NH; ++f) kr[f] = *reinterpret_cast<const u32x4 *>(p + k_lane + 4 * (f / NH) * D + 64 * (f % NH));
       };
-      if (left) load_k(__builtin_ctzll(left));
-      while (left) {
-        const int i = __builtin_ctzll(left);
-        left &= left - 1;
-        const uint8_t *const vp = a.v + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
+      auto load_v = [&](int i) __attribute__((always_inline)) {
+        const uint8_t *const p = a.v + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) vr[b] = *reinterpret_cast<const u32x4 *>(vp + v_lane + 16 * PAGE * b);
+        for (int b = 0; b < NB; ++b) vr[b] = *reinterpret_cast<const u32x4 *>(p + v_lane + 16 * PAGE * b);
+      };
+      int cur = pop(), next;
+      if (cur >= 0) load_k(cur), load_v(cur);
+      float ks = 0.f, vs = 0.f;  // (behind the first codes: they are needed later)
+      if (id >= 0) ks = fmaxf(a.k_scale[size_t(id) * a.hkv + hk] * a.c, LEAST_SCALE), vs = a.v_scale[size_t(id) * a.hkv + hk];
+      for (; cur >= 0; cur = next) {
+        next = pop();
+        const int i = cur;
         const int key0 = __builtin_amdgcn_readlane(at, i) * PAGE;
         const float ksi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), i));
         const float vsi = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vs), i));
@@ -281,9 +326,10 @@ __global__ __launch_bounds__(64 * W, 2) void ca_cache_attend_kernel(const Attend
               x[t][rg] = mfma16(k1, qf[2 * f + 1][rg], x[t][rg]);
             }
           }
-        if (left) load_k(__builtin_ctzll(left));  // of the next page
+        if (next >= 0) load_k(next);
         // some row does not see some key: lane (r, j) holds keys key0 + 16 j + 4 t + e
         if (key0 + PAGE - 1 > p0 || (key0 < p1 - a.window + 1 && key0 + PAGE > a.sinks)) {
+          asm volatile("");  // (a branch)
           const int key = key0 + 16 * j4;
 #pragma unroll
           for (int rg = 0; rg < NR; ++rg)
@@ -319,14 +365,16 @@ __global__ __launch_bounds__(64 * W, 2) void ca_cache_attend_kernel(const Attend
             acc[b][rg] = mfma16(v1, pb[1][rg], acc[b][rg]);
           }
         }
+        if (next >= 0) load_v(next);
       }
     }
     // The waves' sums meet in LDS, CW columns at a time.  A tile that this worker has from its first page to its last is done; of
     // any other the sums go to the workspace.
+    float sum[NR];
 #pragma unroll
     for (int rg = 0; rg < NR; ++rg) {
-      const float sum = quad_sum(l[rg]);
-      if (j4 == 0) merge_ml[(wave * R + 16 * rg + li) * 2] = m[rg], merge_ml[(wave * R + 16 * rg + li) * 2 + 1] = sum;
+      sum[rg] = quad_sum(l[rg]);
+      if (j4 == 0) merge_ml[wave * R + 16 * rg + li] = m[rg];
     }
     __syncthreads();
     const bool whole = n == per_tile;
@@ -338,8 +386,9 @@ __global__ __launch_bounds__(64 * W, 2) void ca_cache_attend_kernel(const Attend
     for (int rg = 0; rg < NR; ++rg) {
       float top = NO_MAX;
 #pragma unroll
-      for (int w = 0; w < W; ++w) top = fmaxf(top, merge_ml[(w * R + 16 * rg + li) * 2]);
+      for (int w = 0; w < W; ++w) top = fmaxf(top, merge_ml[w * R + 16 * rg + li]);
       factor[rg] = m[rg] == NO_MAX ? 0.f : fast_exp2(m[rg] - top);
+      if (j4 == 0) merge_ml[(W + wave) * R + 16 * rg + li] = sum[rg] * factor[rg];
     }
     for (int c0 = 0; c0 < D; c0 += S::CW) {
 #pragma unroll
@@ -351,27 +400,32 @@ __global__ __launch_bounds__(64 * W, 2) void ca_cache_attend_kernel(const Attend
       __syncthreads();
       for (int i = threadIdx.x; i < R * S::CW / 4; i += 64 * W) {
         const int r = i / (S::CW / 4), col = 4 * (i % (S::CW / 4)), at = tile * R + r;
-        f32x4 y = *reinterpret_cast<const f32x4 *>(&merge[r * S::ROW + col]);
+        if (at > last_row) break;
+        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+        float all = 0.f;
 #pragma unroll
-        for (int w = 1; w < W; ++w) y += *reinterpret_cast<const f32x4 *>(&merge[(w * R + r) * S::ROW + col]);
-        if (at > last_row) continue;
-        float top = NO_MAX, sum = 0.f;
+        for (int w = 0; w < W; ++w) {
+          all += merge_ml[(W + w) * R + r];
+          y += *reinterpret_cast<const f32x4 *>(&merge[(w * R + r) * S::ROW + col]);
+        }
+        const bool stats = c0 + col == 0;
+        float top = NO_MAX;
+        if (stats) {
 #pragma unroll
-        for (int w = 0; w < W; ++w) top = fmaxf(top, merge_ml[(w * R + r) * 2]);
-#pragma unroll
-        for (int w = 0; w < W; ++w) sum += merge_ml[(w * R + r) * 2 + 1] * fast_exp2(merge_ml[(w * R + r) * 2] - top);
+          for (int w = 0; w < W; ++w) top = fmaxf(top, merge_ml[w * R + r]);
+        }
         if (!whole) {
           *reinterpret_cast<f32x4 *>(part + r * D + c0 + col) = y;
-          if (c0 + col == 0) part[R * D + 2 * r] = top, part[R * D + 2 * r + 1] = sum;
+          if (stats) part[R * D + 2 * r] = top, part[R * D + 2 * r + 1] = all;
           continue;
         }
-        const int token = at / G, h = hk * G + at - token * G;
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;  // (a row that sees nothing: O = 0, LSE = -inf)
+        const int token = a.token_of(at), h = hk * G + at - token * G;
+        const float inv = all == 0.f ? 0.f : 1.0f / all;  // (a row that sees nothing: O = 0, LSE = -inf)
         *reinterpret_cast<u32x2 *>(a.o + (size_t(q.row0 + token) * a.hq + h) * D + c0 + col) =
             u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
-        if (c0 + col == 0 && a.lse) a.lse[size_t(h) * a.s.total + q.row0 + token] = 0.6931471805599453f * (top + fast_log2(sum));
+        if (stats && a.lse) a.lse[size_t(h) * a.s.total + q.row0 + token] = 0.6931471805599453f * (top + fast_log2(all));
       }
-      __syncthreads();
+      if (c0 + S::CW < D || u < end) __syncthreads();
     }
   }
   if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
@@ -395,11 +449,12 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
   constexpr int R = 128, NK = D / 32, NB = D / 16, ROWB = 2 * D, NL = D / 64;  // NL: loads of K, and of V, of a wave per page
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(CA_LDS char *)smem;
-  const SeqTable tab = seq_table(smem + S::TOTAL, a.s.n_seqs);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j4 = lane >> 4, li = lane & 15;
-  const int G = a.hq / a.hkv, hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv, n_workers = gridDim.x / a.hkv;
-  const WorkSplit split = split_work<256>(tab, a, R, G, n_workers, 4);
+  const int G = a.G, n_workers = gridDim.y, worker = blockIdx.y, hk = blockIdx.x;
+  WorkSplit split;
+  split.make<256>(smem + S::TOTAL, a, R, n_workers, 4);
+  const SeqTable &tab = split.tab;
   const int begin = split.bound(worker), end = split.bound(worker + 1);
   int4 head = {0, 0, 0, 0};
   // where the wave's codes come from in a page, and where they go: K row i of tile `wave` is key 16 (i / 4) + 4 wave + i % 4
@@ -415,25 +470,24 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
   }
   uint32_t koff = lds0 + li * ROWB + 16 * (j4 ^ tile_sw<D>(li)), voff = lds0 + S::V_OFF + li * (2 * PAGE) + 16 * (j4 ^ tile_sw<64>(li)), stage = 0;
 
-  for (int u = begin, s = begin < end ? find_unit(tab.pre, a.s.n_seqs, begin) : 0; u < end;) {
-    while (tab.pre[s + 1] <= u) ++s;
-    s = __builtin_amdgcn_readfirstlane(s);
+  for (int u = begin; u < end;) {
+    const int s = tab.find(u), in_seq = u - tab.before(s);
     const Seq q = tab.at(s);
     const int per_tile = tile_pages(q.len, R, G, a.window, a.sinks);
-    const int tile = __builtin_amdgcn_readfirstlane((u - tab.pre[s]) / per_tile), first = __builtin_amdgcn_readfirstlane((u - tab.pre[s]) % per_tile);
+    const int tile = quotient(in_seq, per_tile), first = in_seq - tile * per_tile;
     const int n = min(end - u, per_tile - first);
     u += n;
     // the rows: of the tile, and of the wave (w..)
     const int last_row = min((tile + 1) * R, q.n * G) - 1, pos0 = q.len - q.n, row_w = tile * R + 32 * wave;
-    const int p0 = pos0 + tile * R / G, p1 = pos0 + last_row / G;
+    const int p0 = pos0 + a.token_of(tile * R), p1 = pos0 + a.token_of(last_row);
     const int from = max(0, p0 - a.window + 1), n_sink = min((a.sinks + PAGE - 1) / PAGE, from / PAGE);
-    const int p0w = pos0 + row_w / G, p1w = row_w <= last_row ? pos0 + min(row_w + 31, last_row) / G : -1;
+    const int p0w = pos0 + a.token_of(row_w), p1w = row_w <= last_row ? pos0 + a.token_of(min(row_w + 31, last_row)) : -1;
     const int from_w = max(0, p0w - a.window + 1);
     int hi[2], lo[2];
     bf16x8 qf[NK][2];
 #pragma unroll
     for (int rg = 0; rg < 2; ++rg) {
-      const int r = row_w + 16 * rg + li, ok = r <= last_row, i = ok ? r / G : 0, h = hk * G + (ok ? r - i * G : 0);
+      const int r = row_w + 16 * rg + li, ok = r <= last_row, i = ok ? a.token_of(r) : 0, h = hk * G + (ok ? r - i * G : 0);
       hi[rg] = ok ? pos0 + i : -1, lo[rg] = max(0, pos0 + i - a.window + 1);
       const bf16_t *const qp = a.q + (size_t(q.row0 + i) * a.hq + h) * D + 8 * j4;
 #pragma unroll
@@ -621,10 +675,10 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
     if (n == per_tile) {
       const float f0 = sum[0] == 0.f ? 0.f : 1.0f / sum[0], f1 = sum[1] == 0.f ? 0.f : 1.0f / sum[1];
       store_tile16_as_lines<0>(lds0 + wave * PATCH_BYTES, acc, f0, f1, lane, [&](int p) __attribute__((always_inline)) -> bf16_t * {
-        const int r = row_w + p, i = r / G;
+        const int r = row_w + p, i = a.token_of(r);
         return r <= last_row ? a.o + (size_t(q.row0 + i) * a.hq + hk * G + r - i * G) * D : nullptr;
       });
-      const int r = row_w + lane, i = r / G;
+      const int r = row_w + lane, i = a.token_of(r);
       if (lane < 32 && r <= last_row && a.lse)
         a.lse[size_t(hk * G + r - i * G) * a.s.total + q.row0 + i] = 0.6931471805599453f * ((lane < 16 ? m[0] : m[1]) + fast_log2(lane < 16 ? sum[0] : sum[1]));
     } else {
@@ -638,7 +692,7 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
       float *const ml = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2)) + R * D + 64 * wave;
       if (lane < 32) ml[2 * lane] = lane < 16 ? m[0] : m[1], ml[2 * lane + 1] = lane < 16 ? sum[0] : sum[1];
     }
-    __syncthreads();  // the patches lie in the stages
+    if (u < end) __syncthreads();  // the patches lie in the stages
   }
   if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
 }
@@ -647,9 +701,9 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
 template <int D, int NR>
 __global__ __launch_bounds__(256) void ca_cache_combine_kernel(const AttendArgs a) {
   constexpr int R = 16 * NR, LANES = D / 4, AT_A_TIME = 64 / LANES, RW = NR == 8 ? 4 : 1;
-  const int hk = blockIdx.x % a.hkv, worker = blockIdx.x / a.hkv;
+  const int hk = blockIdx.x, worker = blockIdx.y;
   const int4 head = a.heads[worker * a.hkv + hk];  // {parts, first row of the sequence, first row of the tile, last row of the tile}
-  const int G = a.hq / a.hkv, lane = threadIdx.x & 63, r0 = RW * (4 * blockIdx.y + (threadIdx.x >> 6));
+  const int G = a.G, lane = threadIdx.x & 63, r0 = RW * (4 * blockIdx.z + (threadIdx.x >> 6));
   if (head.x < 2 || head.z + r0 > head.w) return;
   const size_t stride = size_t(2 * a.hkv) * (R * (D + 2));
   const float *const first = a.parts + size_t((worker * 2 + 1) * a.hkv + hk) * (R * (D + 2));
@@ -682,7 +736,7 @@ __global__ __launch_bounds__(256) void ca_cache_combine_kernel(const AttendArgs 
       for (int e = 0; e < 4; ++e) z[e] = __shfl_xor(y[x][e], o);
       add(x, __shfl_xor(top[x], o), __shfl_xor(sum[x], o), z);
     }
-    const int at = head.z + r0 + x, token = at / G, h = hk * G + at - token * G;
+    const int at = head.z + r0 + x, token = a.token_of(at), h = hk * G + at - token * G;
     if (mine != 0 || at > head.w) continue;
     const float inv = sum[x] == 0.f ? 0.f : 1.0f / sum[x];
     *reinterpret_cast<u32x2 *>(a.o + (size_t(head.y + token) * a.hq + h) * D + col) =
@@ -742,15 +796,15 @@ __global__ __launch_bounds__(256) void ca_cache_append_kernel(const AppendArgs a
   constexpr int LPT = D / 8, TPI = 64 / LPT, NI = PAGE / TPI;  // K: lanes per token, tokens per load, loads per page
   constexpr int VL = D / 2, VT = 64 / VL, NV = PAGE / VT;      // V: lanes per token, halves, tokens per half of a whole page
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  const SeqTable tab = seq_table(smem, a.s.n_seqs);
+  SeqTable tab;
   auto first_pos = [](const Seq &q) { return max(0, q.len - q.n); };
-  const int total = fill_table<256>(tab, a.s, [&](const Seq &q) { return q.n > 0 && q.len > 0 ? (q.len - 1) / PAGE - first_pos(q) / PAGE + 1 : 0; });
+  const int total = tab.fill<256>(smem, a.s, [&](const Seq &q) { return q.n > 0 && q.len > 0 ? (q.len - 1) / PAGE - first_pos(q) / PAGE + 1 : 0; });
   const int unit = int(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int touch = unit / (2 * a.hkv), h = unit / 2 % a.hkv, lane = threadIdx.x & 63;
   if (touch >= total) return;
-  const int s = find_unit(tab.pre, a.s.n_seqs, touch);
+  const int s = tab.find(touch);
   const Seq q = tab.at(s);
-  const int index = __builtin_amdgcn_readfirstlane(first_pos(q) / PAGE + touch - tab.pre[s]);
+  const int index = first_pos(q) / PAGE + touch - tab.before(s);
   const int page = a.s.table[size_t(s) * a.s.width + index];
   if (page < 0 || page >= a.s.n_pages) return;
   const int begin = max(first_pos(q) - index * PAGE, 0), end = min(q.len - index * PAGE, PAGE);  // the page's tokens that are new
@@ -934,14 +988,16 @@ static int launched(const char *what, hipError_t e) {
   return fail(CA_ERR_HIP, std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")");
 }
 
-// Workers per KV head: about one workgroup of eight waves, or two of four, for each CU.
-// (NR: 16-row groups of a tile; 8: chunks)
+// Waves of a worker, and workers per KV head: as many as are on the chip at a time (NR: 16-row groups of a tile; 8: chunks).
 template <int NR>
 constexpr int WAVES = NR == 1 ? 8 : 4;
-static int n_workers(int hkv, int waves) { return std::max(1, N_CU * 8 / waves / hkv); }
+template <int NR>
+static int n_workers(int hkv) {
+  return std::max(1, N_CU * (NR == 8 ? 2 : 1) / hkv);
+}
 template <int D, int NR>
 static size_t attend_bytes(int hkv) {
-  const size_t workers = size_t(n_workers(hkv, WAVES<NR>));
+  const size_t workers = size_t(n_workers<NR>(hkv));
   return workers * hkv * sizeof(int4) + workers * 2 * hkv * (16 * NR * (D + 2)) * 4;
 }
 static size_t attend_bytes(const ca_cache *c) {
@@ -953,7 +1009,8 @@ static size_t attend_bytes(const ca_cache *c) {
 template <int D, int NR>
 static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
   constexpr int W = WAVES<NR>;
-  const int workers = n_workers(a.hkv, W);
+  const int workers = n_workers<NR>(a.hkv);
+  a.by_workers = 1.0001f / float(workers);
   a.heads = static_cast<int4 *>(ws);
   a.parts = reinterpret_cast<float *>(a.heads + size_t(workers) * a.hkv);
   void (*kern)(AttendArgs);
@@ -965,8 +1022,9 @@ static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
   static std::atomic<bool> done[16];
   if (e == hipSuccess) e = set_smem(kern, int(bytes + seq_table_bytes(MAX_SEQS)), device, done);
   if (e != hipSuccess) return launched("cache attention", e);
-  hipLaunchKernelGGL(kern, dim3(unsigned(workers * a.hkv)), dim3(64 * W), bytes + seq_table_bytes(a.s.n_seqs), st, a);
-  hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(workers * a.hkv), NR == 8 ? 8 : 4 * NR), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(kern, dim3(unsigned(a.hkv), unsigned(workers)), dim3(64 * W), bytes + seq_table_bytes(a.s.n_seqs), st, a);
+  // (no tile has more pages than the table is wide, and none of up to CUT pages is cut)
+  if (a.s.width > CUT) hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(a.hkv), unsigned(workers), NR == 8 ? 8 : 4 * NR), dim3(256), 0, st, a);
   return launched("cache attention", hipSuccess);
 }
 
@@ -1001,11 +1059,12 @@ int ca_cache_attend(const ca_cache *c, const ca_cache_batch *b, int32_t n_q_head
   const int64_t g = n_q_heads / c->n_kv_heads;
   if ((b->total_rows * g / 16 + b->n_seqs) * std::max(1, b->table_width) >= int64_t(1) << 30)
     return fail(CA_ERR_UNSUPPORTED, "batch: rows times pages beyond 2^30");
+  if ((b->total_rows * g + 128) * g >= int64_t(1) << 32) return fail(CA_ERR_UNSUPPORTED, "batch: rows times the square of the heads per KV head beyond 2^32");
   AttendArgs a = {};
   a.s = seq_args(c, b);
   a.k = static_cast<const uint8_t *>(c->k), a.v = static_cast<const uint8_t *>(c->v), a.k_scale = c->k_scale, a.v_scale = c->v_scale;
   a.q = static_cast<const bf16_t *>(q), a.o = static_cast<bf16_t *>(o), a.lse = lse;
-  a.hq = n_q_heads, a.hkv = c->n_kv_heads;
+  a.hq = n_q_heads, a.hkv = c->n_kv_heads, a.G = int(g), a.by_g = uint32_t(((uint64_t(1) << 32) + uint64_t(g) - 1) / uint64_t(g));
   a.window = window == 0 ? 1 << 30 : int(std::min<int64_t>(window, 1 << 30));
   a.sinks = window == 0 ? 0 : int(std::min<int64_t>(sinks, 1 << 30));
   a.c = (softmax_scale > 0.f ? softmax_scale : c->head_dim == 128 ? 0.08838834764831845f : 0.125f) * 1.4426950408889634f;
