@@ -12,9 +12,9 @@ constexpr float L2_PADDING = 1.0e30f;  // exp2(x - 1e30) == 0 for every finite s
 
 // ------------------------------------------------------------------------------------------------ dQ
 // Eight waves on a CU of their own have four stages; workgroups of four, two to a CU, share its LDS.
-template <int D, int W>
+template <int D, int W, bool WINDOW = false>
 struct DqSmem {
-  static constexpr int NST = D == 128 && W == 4 ? 2 : 4;
+  static constexpr int NST = D == 128 && W == 4 ? 2 : WINDOW ? 3 : 4;
   static constexpr int TILE = FWD_BN * 2 * D;
   // a stage holds the K tile and then the V tile of one key block: both are reached from one address register
   // through the 16-bit offset field of the LDS instructions
@@ -38,7 +38,7 @@ __device__ __forceinline__ void dq_workgroup(const FwdUnit &u, const int half, c
                                              const bf16_t *__restrict__ dO, const float *__restrict__ l2_slot,
                                              const float *__restrict__ delta_slot, bf16_t *__restrict__ dQ,
                                              float *__restrict__ parts, int Hq, int Hkv, int64_t padded, float scale) {
-  using S = DqSmem<D, W>;
+  using S = DqSmem<D, W, WINDOW>;
   constexpr int NK = D / 32, ND = D / 16, CH = D / 8, RPI = 64 / CH, NLD = FWD_BN / (W * RPI), NST = S::NST;
   constexpr int ROWB = 2 * D, HALF = 16 * ROWB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];

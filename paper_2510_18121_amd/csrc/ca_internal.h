@@ -172,4 +172,5 @@ struct ca_plan {
 namespace ca {
 void set_error(const std::string &msg);
 int build_plan(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out);  // host only; window 0: none
+size_t backward_layout(ca_plan_t *p);  // offsets of the backward workspace in slot order; its size
 }  // namespace ca

@@ -12,10 +12,9 @@
 
 namespace ca {
 
-size_t backward_layout(ca_plan_t *p);  // offsets of the backward workspace in slot order; its size
-
 // Returns false where there are too many padded rows.
 inline bool schedule_window(ca_plan_t *p) {
+  constexpr size_t MAX_PARTS = size_t(256) << 20;
   auto up = [](int64_t x, int64_t m) { return (x + m - 1) / m * m; };
   const int hq = p->hq, hkv = p->hkv, g = hq / hkv;
   const int hp = g % 8 == 0 ? 8 : g % 4 == 0 ? 4 : g % 2 == 0 ? 2 : 1;
@@ -113,20 +112,24 @@ inline bool schedule_window(ca_plan_t *p) {
       p->fwd_steps += t.cost;
     }
 
-  // Backward: a tile with sinks is seen by every later row of its document, and a small batch has few units.  Units longer than T
-  // steps are cut along their query blocks; T leaves about eight workgroups per CU, and the fp32 parts within 256 MiB.
+  // Backward: a tile with sinks is seen by every later row of its document, and a small batch has few units.  Units longer than what
+  // each of the workgroups that run at a time would have, were the launch's work spread evenly, are cut along their query blocks, and
+  // those with sinks that are longer than a quarter of that: they have one busy wave of four, and are better off beside others than first
+  // (64K tokens, window 1024, 4 sinks, 32/8 heads: 5.68 -> 5.45 ms).  (A dQ half does 3 products per pair of its 128 rows and 64 keys, a
+  // dK/dV step 4 of as many pairs.)
   auto steps = [](const BwdUnit &u) { return int64_t(u.slot_end - u.slot_begin) / BWD_BQ * u.heads; };
   for (const WindowUnit &u : btiles) p->bwd_steps += steps(u) * hkv;
-  int64_t piece = std::max<int64_t>(64, p->bwd_steps / (8 * N_CU));
+  const int64_t slots = (p->d == 64 ? 3 : 2) * N_CU, mean = (p->bwd_steps + 2 * p->fwd_steps * 3 / 4) / slots;
+  int64_t piece = std::max<int64_t>(24, mean);
   auto pieces_of = [&](const WindowUnit &u) {
-    const int64_t n = steps(u);
-    return n > piece + piece / 2 ? std::min((n + piece - 1) / piece, int64_t(u.slot_end - u.slot_begin) / BWD_BQ) : int64_t(1);
+    const int64_t n = steps(u), most = u.key_pos0 < p->sinks ? std::max<int64_t>(24, piece / 4) : piece;
+    return n > most ? std::min((n + most - 1) / most, int64_t(u.slot_end - u.slot_begin) / BWD_BQ) : int64_t(1);
   };
   for (;; piece *= 2) {
     int64_t parts = 0;
     for (const WindowUnit &u : btiles)
       if (const int64_t k = pieces_of(u); k > 1) parts += k * hkv;
-    if (size_t(parts) * part_bytes(p->d) <= size_t(256) << 20) break;
+    if (size_t(parts) * part_bytes(p->d) <= MAX_PARTS) break;
   }
   std::vector<WindowUnit> tiles;
   std::vector<int32_t> parts_per_head;

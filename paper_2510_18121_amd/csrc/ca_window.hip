@@ -26,26 +26,32 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_fwd_window_kernel(
                                total_q, c);
 }
 
+// dK/dV workgroups, then dQ workgroups (halves of units), in one launch: both are of four waves, two to a CU (three at head_dim 64), and
+// the second kind fills the CUs that the first leaves idle.
+struct WindowArgs {
+  const WindowUnit *units;
+  const FwdUnit *dq_units;
+  const int32_t *slot_row, *slot_pos, *slot_lo;
+  const bf16_t *q, *k, *v, *d_o, *q_sorted, *do_sorted;
+  const float *l2_slot, *delta_slot, *stats_kv;
+  bf16_t *dq, *dk, *dv;
+  float *parts;
+  int n_dkv, n_dq, hq, hkv, sinks;
+  int64_t padded;
+  float scale;
+};
 template <int D>
-__global__ __launch_bounds__(512, 2) void ca_dq_window_kernel(const FwdUnit *__restrict__ units, const int32_t *__restrict__ slot_row,
-                                                              const int32_t *__restrict__ slot_pos, const int32_t *__restrict__ slot_lo,
-                                                              int sinks, const bf16_t *__restrict__ Q, const bf16_t *__restrict__ K,
-                                                              const bf16_t *__restrict__ V, const bf16_t *__restrict__ dO,
-                                                              const float *__restrict__ l2_slot, const float *__restrict__ delta_slot,
-                                                              bf16_t *__restrict__ dQ, int Hq, int Hkv, int64_t padded, float scale) {
-  dq_workgroup<D, 8, true>(units[blockIdx.x], 0, slot_row, slot_pos, slot_lo, sinks, Q, K, V, dO, l2_slot, delta_slot, dQ, nullptr, Hq, Hkv,
-                           padded, scale);
-}
-
-template <int D>
-__global__ __launch_bounds__(256, 2) void ca_dkv_window_kernel(const WindowUnit *__restrict__ units, const int32_t *__restrict__ slot_pos,
-                                                               const int32_t *__restrict__ slot_lo, int sinks,
-                                                               const bf16_t *__restrict__ Qs, const bf16_t *__restrict__ K,
-                                                               const bf16_t *__restrict__ V, const bf16_t *__restrict__ dOs,
-                                                               const float *__restrict__ stats_kv, bf16_t *__restrict__ dK,
-                                                               bf16_t *__restrict__ dV, float *__restrict__ parts, int Hq, int Hkv,
-                                                               float scale) {
-  dkv_workgroup<D, true>(int(blockIdx.x), units, slot_pos, slot_lo, sinks, Qs, K, V, dOs, stats_kv, dK, dV, parts, Hq, Hkv, scale);
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_bwd_window_kernel(const WindowArgs a) {
+  const int i = int(blockIdx.x);
+  if (i < a.n_dkv) {
+    dkv_workgroup<D, true>(i, a.units, a.slot_pos, a.slot_lo, a.sinks, a.q_sorted, a.k, a.v, a.do_sorted, a.stats_kv, a.dk, a.dv, a.parts, a.hq,
+                           a.hkv, a.scale);
+  } else {
+    int unit = i - a.n_dkv, half;
+    half_of_unit(unit, a.n_dq, half);
+    dq_workgroup<D, 4, true>(a.dq_units[unit], half, a.slot_row, a.slot_pos, a.slot_lo, a.sinks, a.q, a.k, a.v, a.d_o, a.l2_slot, a.delta_slot,
+                             a.dq, nullptr, a.hq, a.hkv, a.padded, a.scale);
+  }
 }
 
 template <int D>
@@ -70,37 +76,37 @@ hipError_t launch_fwd_window(const ca_plan_t *p, const void *q, const void *k, c
 template <int D>
 static hipError_t launch_bwd_window_t(const ca_plan_t *p, const void *q, const void *k, const void *v, const void *o, const void *d_o,
                                       const float *lse, void *dq, void *dk, void *dv, void *ws, hipStream_t st, hipEvent_t *ev) {
+  constexpr int SMEM = std::max(DkvSmem<D>::TOTAL, DqSmem<D, 4, true>::TOTAL);
+  auto kern = ca_bwd_window_kernel<D>;
+  static std::atomic<bool> done[16];
+  const hipError_t e = set_smem(kern, SMEM, p->device, done);
+  if (e != hipSuccess) return e;
   char *const at = static_cast<char *>(ws);
-  const float *const delta_slot = reinterpret_cast<float *>(at), *const l2_slot = reinterpret_cast<float *>(at + p->ws_off_l2);
-  const float *const stats_kv = reinterpret_cast<float *>(at + p->ws_off_stats_kv);
-  const bf16_t *const q_sorted = reinterpret_cast<bf16_t *>(at + p->ws_off_qs), *const do_sorted = reinterpret_cast<bf16_t *>(at + p->ws_off_dos);
-  float *const parts = reinterpret_cast<float *>(at + p->ws_off_parts_kv);
+  auto in = [](const void *x) { return static_cast<const bf16_t *>(x); };
+  auto out = [](void *x) { return static_cast<bf16_t *>(x); };
+  WindowArgs a = {};
+  a.units = p->d_window_units, a.dq_units = p->d_fwd_units, a.slot_row = p->d_slot_row, a.slot_pos = p->d_slot_pos, a.slot_lo = p->d_slot_lo;
+  a.q = in(q), a.k = in(k), a.v = in(v), a.d_o = in(d_o);
+  a.q_sorted = reinterpret_cast<bf16_t *>(at + p->ws_off_qs), a.do_sorted = reinterpret_cast<bf16_t *>(at + p->ws_off_dos);
+  a.delta_slot = reinterpret_cast<float *>(at), a.l2_slot = reinterpret_cast<float *>(at + p->ws_off_l2);
+  a.stats_kv = reinterpret_cast<float *>(at + p->ws_off_stats_kv);
+  a.dq = out(dq), a.dk = out(dk), a.dv = out(dv), a.parts = reinterpret_cast<float *>(at + p->ws_off_parts_kv);
+  a.hq = p->hq, a.hkv = p->hkv, a.sinks = p->sinks, a.padded = int64_t(p->slot_row.size()), a.scale = p->scale;
+  auto launch = [&](int n_dkv, int n_dq) {
+    a.n_dkv = n_dkv, a.n_dq = n_dq;
+    if (n_dkv + n_dq > 0) hipLaunchKernelGGL(kern, dim3(unsigned(n_dkv + 2 * n_dq)), dim3(256), SMEM, st, a);
+  };
   if (ev) (void)hipEventRecord(ev[0], st);
   prepare_bwd(p, q, o, d_o, lse, dq, dk, dv, ws, false, st);
   if (ev) (void)hipEventRecord(ev[1], st);
-  if (p->bwd_workgroups > 0) {
-    auto kern = ca_dkv_window_kernel<D>;
-    static std::atomic<bool> done[16];
-    const hipError_t e = set_smem(kern, DkvSmem<D>::TOTAL, p->device, done);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3(unsigned(p->bwd_workgroups)), dim3(256), DkvSmem<D>::TOTAL, st, p->d_window_units, p->d_pos_kv, p->d_slot_lo,
-                       p->sinks, q_sorted, static_cast<const bf16_t *>(k), static_cast<const bf16_t *>(v), do_sorted, stats_kv,
-                       static_cast<bf16_t *>(dk), static_cast<bf16_t *>(dv), parts, p->hq, p->hkv, p->scale);
+  const int n_dq = int(p->fwd_units.size());
+  launch(p->bwd_workgroups, ev ? 0 : n_dq);  // (with timing enabled the same workgroups run as two launches, so that each kind has a time)
+  if (!p->bwd_combine.empty()) combine_dkv(p, a.parts, dk, dv, st);
+  if (ev) {
+    (void)hipEventRecord(ev[2], st);
+    launch(0, n_dq);
+    (void)hipEventRecord(ev[3], st);
   }
-  if (!p->bwd_combine.empty()) combine_dkv(p, parts, dk, dv, st);
-  if (ev) (void)hipEventRecord(ev[2], st);
-  if (!p->fwd_units.empty()) {
-    auto kern = ca_dq_window_kernel<D>;
-    static std::atomic<bool> done[16];
-    constexpr int SMEM = DqSmem<D, 8>::TOTAL;
-    const hipError_t e = set_smem(kern, SMEM, p->device, done);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3(unsigned(p->fwd_units.size())), dim3(512), SMEM, st, p->d_fwd_units, p->d_slot_row,
-                       p->d_slot_pos, p->d_slot_lo, p->sinks, static_cast<const bf16_t *>(q), static_cast<const bf16_t *>(k),
-                       static_cast<const bf16_t *>(v), static_cast<const bf16_t *>(d_o), l2_slot, delta_slot, static_cast<bf16_t *>(dq), p->hq,
-                       p->hkv, int64_t(p->slot_row.size()), p->scale);
-  }
-  if (ev) (void)hipEventRecord(ev[3], st);
   return hipGetLastError();
 }
 
