@@ -147,13 +147,13 @@ __device__ __forceinline__ void dq_workgroup(const FwdUnit &u, const int half, c
     const bool seen = j0 <= wmax && (!WINDOW || j0 + FWD_BN > lo_min || j0 < sinks);  // some row of this wave sees the tile
     const bool masked = j0 + FWD_BN - 1 > wmin || (WINDOW && j0 < lo_max && j0 + FWD_BN > sinks);
     // one 64-key tile; MASKED is a compile-time constant in each of the two instantiations below
-    auto tile = [&](const bool MASKED) __attribute__((always_inline)) {
+    auto tile = [&](const int KB0, const int KB1, const bool MASKED) __attribute__((always_inline)) {
       // Fragments come from LDS AHEAD fragments before the MFMAs that use them: per 32-key block 2 NK of K (scores), 2 NK of V
       // (dP) and ND of K transposed (dQ).
       constexpr int NF = 2 * NK + 2 * NK + ND, AHEAD = 4;
       bf16x8 fr[AHEAD];
       auto fetch = [&](int i) __attribute__((always_inline)) -> bf16x8 {
-        const int kb = i / NF, f = i % NF;
+        const int kb = KB0 + i / NF, f = i % NF;
         const int KT = S::K_OFF + 32 * kb * ROWB, VT = S::V_OFF + 32 * kb * ROWB;
         if (f < 4 * NK) return lds_read8_at((f < 2 * NK ? KT : VT) + HALF * (f & 1) + (koff ^ (64 * (f % (2 * NK) / 2))));
         const int ta = toff ^ (32 * (f - 4 * NK));
@@ -162,9 +162,9 @@ __device__ __forceinline__ void dq_workgroup(const FwdUnit &u, const int half, c
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) fr[i] = fetch(i);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = KB0; kb < KB1; ++kb) {
         auto next = [&](int f) __attribute__((always_inline)) {  // fragment f is used: its registers take the one AHEAD later
-          if (NF * kb + f + AHEAD < 2 * NF) fr[f % AHEAD] = fetch(NF * kb + f + AHEAD);
+          if (NF * (kb - KB0) + f + AHEAD < NF * (KB1 - KB0)) fr[f % AHEAD] = fetch(NF * (kb - KB0) + f + AHEAD);
         };
         static_assert(NF % AHEAD == 0);
         f32x4 sa[2][2], pa[2][2];  // [16 keys][16 rows]
@@ -222,8 +222,17 @@ __device__ __forceinline__ void dq_workgroup(const FwdUnit &u, const int half, c
       }
     };
     if (seen) {
-      if (masked) tile(true);
-      else tile(false);
+      if (!masked) {
+        tile(0, 2, false);
+      } else if (!WINDOW) {
+        tile(0, 2, true);
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const int k0 = j0 + 32 * kb;
+          if (k0 <= wmax && (k0 + 32 > lo_min || k0 < sinks)) tile(kb, kb + 1, true);
+        }
+      }
     }
     // the offsets follow the stages round
     const int adv = (j % NST) == NST - 1 ? -(NST - 1) * S::STAGE : S::STAGE;
