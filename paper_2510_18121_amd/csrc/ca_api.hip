@@ -75,7 +75,7 @@ static void free_device(ca_plan_t *p) {
   p->d_fwd_units = p->d_fwd_pieces = nullptr;
   p->d_bwd_units = p->d_bwd_pieces = p->d_fused_units = nullptr;
   p->d_fwd_combine = p->d_bwd_combine = nullptr;
-  p->d_slot_lo = nullptr, p->d_window_units = nullptr;
+  p->d_slot_lo = p->d_slot_src = nullptr, p->d_window_units = nullptr;
   if (cur >= 0 && cur != p->device) (void)hipSetDevice(cur);
   p->device = -1;
 }
@@ -141,7 +141,7 @@ int ca_plan_upload(ca_plan_t *p, void *hip_stream) {
     auto add = [&](const auto &src) { arrays.push_back({src.data(), src.size() * sizeof(src[0]), 0}); };
     add(p->slot_row), add(p->slot_pos), add(p->block_rpk), add(p->pos_kv), add(p->fwd_units), add(p->bwd_units);
     add(p->fwd_pieces), add(p->bwd_pieces), add(p->fwd_combine), add(p->bwd_combine), add(p->joint_order), add(p->fused_units);
-    add(p->slot_lo), add(p->window_units);
+    add(p->slot_lo), add(p->slot_src), add(p->window_units);
     for (const bool large : {false, true}) {
       for (Array &a : arrays)
         if ((a.bytes > SMALL_ARRAY) == large) a.at = bytes, bytes = (bytes + a.bytes + 255) / 256 * 256;
@@ -175,7 +175,7 @@ int ca_plan_upload(ca_plan_t *p, void *hip_stream) {
   place(p->d_slot_row, 0), place(p->d_slot_pos, 1), place(p->d_block_rpk, 2), place(p->d_pos_kv, 3);
   place(p->d_fwd_units, 4), place(p->d_bwd_units, 5), place(p->d_fwd_pieces, 6), place(p->d_bwd_pieces, 7);
   place(p->d_fwd_combine, 8), place(p->d_bwd_combine, 9), place(p->d_joint_order, 10), place(p->d_fused_units, 11);
-  place(p->d_slot_lo, 12), place(p->d_window_units, 13);
+  place(p->d_slot_lo, 12), place(p->d_slot_src, 13), place(p->d_window_units, 14);
   // the vectors and `blob` stay alive in the plan, so the asynchronous copies read valid memory
   return CA_OK;
 }

@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256, 2) void ca_bwd_dkv_kernel(const BwdUnit *__res
                                                             const float *__restrict__ stats_kv, bf16_t *__restrict__ dK,
                                                             bf16_t *__restrict__ dV, float *__restrict__ parts, int Hq, int Hkv,
                                                             float scale) {
-  dkv_workgroup<D>(int(blockIdx.x), units, slot_pos, nullptr, 0, Qs, K, V, dOs, stats_kv, dK, dV, parts, Hq, Hkv, scale);
+  dkv_workgroup<D>(int(blockIdx.x), units, slot_pos, nullptr, nullptr, 0, Qs, K, V, dOs, stats_kv, dK, dV, parts, Hq, Hkv, scale);
 }
 
 // dK/dV units and dQ half units (workgroups of 4 groups of 32 rows) in one launch, longest first.  For batches too small to
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256, 2) void ca_bwd_joint_kernel(const JointArgs a)
     w = -1 - (unit + half * a.n_dq);
   }
   if (w >= 0) {
-    dkv_workgroup<D>(w, a.units, a.pos_kv, nullptr, 0, a.q_sorted, a.k, a.v, a.do_sorted, a.stats_kv, a.dk, a.dv, a.parts_kv, a.hq, a.hkv, a.scale);
+    dkv_workgroup<D>(w, a.units, a.pos_kv, nullptr, nullptr, 0, a.q_sorted, a.k, a.v, a.do_sorted, a.stats_kv, a.dk, a.dv, a.parts_kv, a.hq, a.hkv, a.scale);
   } else {
     const int half = -1 - w >= a.n_dq ? 1 : 0;
     dq_workgroup<D, 4>(a.dq_units[-1 - w - half * a.n_dq], half, a.slot_row, a.slot_pos, nullptr, 0, a.q, a.k, a.v, a.d_o, a.l2_slot,
@@ -213,17 +213,19 @@ static void launch_fill(void *p, size_t bytes, hipStream_t st) {
   hipLaunchKernelGGL(ca_fill_zero_kernel, dim3(blocks), dim3(256), 0, st, static_cast<u32x4 *>(p), n16);
 }
 
-void prepare_bwd(const ca_plan_t *p, const void *q, const void *o, const void *d_o, const float *lse, void *dq, void *dk, void *dv,
-                 void *ws, bool fused, hipStream_t st) {
-  char *const at = static_cast<char *>(ws);
-  const size_t q_bytes = size_t(p->total_q) * p->hq * p->d * 2, kv_bytes = size_t(p->total_kv) * p->hkv * p->d * 2;
-  const int64_t padded = int64_t(p->slot_row.size());
-  // rows that belong to no work unit (KV outside every scheduled document, Q rows outside every task)
+void fill_uncovered(const ca_plan_t *p, void *dq, void *dk, void *dv, hipStream_t st) {
   if (!p->kv_covered) {
-    launch_fill(dk, kv_bytes, st);
-    launch_fill(dv, kv_bytes, st);
+    launch_fill(dk, size_t(p->total_kv) * p->hkv * p->d * 2, st);
+    launch_fill(dv, size_t(p->total_kv) * p->hkv * p->d * 2, st);
   }
-  if (!p->q_covered) launch_fill(dq, q_bytes, st);
+  if (!p->q_covered) launch_fill(dq, size_t(p->total_q) * p->hq * p->d * 2, st);
+}
+
+static void prepare_bwd(const ca_plan_t *p, const void *q, const void *o, const void *d_o, const float *lse, void *dq, void *dk, void *dv,
+                        void *ws, bool fused, hipStream_t st) {
+  char *const at = static_cast<char *>(ws);
+  const int64_t padded = int64_t(p->slot_row.size());
+  fill_uncovered(p, dq, dk, dv, st);
   if (padded > 0) {
     const int64_t threads = padded * p->hq * (p->d / 8);
     hipLaunchKernelGGL(ca_bwd_prep_kernel, dim3(unsigned((threads + 255) / 256)), dim3(256), 0, st, p->d_slot_row,

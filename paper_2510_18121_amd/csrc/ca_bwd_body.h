@@ -256,7 +256,9 @@ __device__ __forceinline__ void dq_workgroup(const FwdUnit &u, const int half, c
 }
 
 // ------------------------------------------------------------------------------------------------ dK, dV
-template <int D>
+// WINDOW: Q and dO come from where they are, by their rows, not from slot-ordered copies: few tiles of keys share a row (9 with a window
+// of 1024), and the copies cost as much traffic as two fifths of them save.  The rows of a block are fetched NST - 1 tiles before the tile is.
+template <int D, bool WINDOW = false>
 struct DkvSmem {
   static constexpr int NST = D == 128 ? 2 : 3;      // two workgroups share a CU's LDS at head_dim 128, three at 64
   static constexpr int TILE = BWD_BQ * 2 * D;       // one Q or dO tile of 64 slots
@@ -267,8 +269,9 @@ struct DkvSmem {
   static constexpr int POS_OFF = L2_OFF + 512;
   static constexpr int SPARE_OFF = POS_OFF + 256;
   static constexpr int STAGE = 2 * TILE + 1024;
-  static constexpr int TOTAL = NST * STAGE;
-  static_assert(4 * PATCH_BYTES <= TOTAL, "patches fit in the stages");
+  static constexpr int ROWS_OFF = NST * STAGE;      // WINDOW: packed rows of the tiles that are fetched next, [NST][64]
+  static constexpr int TOTAL = ROWS_OFF + (WINDOW ? NST * 256 : 0);
+  static_assert(4 * PATCH_BYTES <= NST * STAGE, "patches fit in the stages");
 };
 
 // A unit, or a chain of short units one after the other, in a workgroup of four waves, each of which owns 32 keys: K and V
@@ -286,17 +289,17 @@ template <int D, bool WINDOW = false>
 __device__ __forceinline__ void dkv_workgroup(const int me /* index of the first unit */,
                                               const std::conditional_t<WINDOW, WindowUnit, BwdUnit> *__restrict__ units,
                                               const int32_t *__restrict__ slot_pos, const int32_t *__restrict__ slot_lo,
-                                              const int sinks, const bf16_t *__restrict__ Qs,
+                                              const int32_t *__restrict__ slot_src, const int sinks, const bf16_t *__restrict__ Qs,
                                               const bf16_t *__restrict__ K, const bf16_t *__restrict__ V,
                                               const bf16_t *__restrict__ dOs, const float *__restrict__ stats_kv,
                                               bf16_t *__restrict__ dK,
                                               bf16_t *__restrict__ dV, float *__restrict__ parts, int Hq, int Hkv, float scale) {
-  using S = DkvSmem<D>;
+  using S = DkvSmem<D, WINDOW>;
   constexpr int NK = D / 32, ND = D / 16, CH = D / 8, RPI = 64 / CH, NST = S::NST;
   constexpr int NLD = BWD_BQ / (4 * RPI);  // direct loads per wave per Q (or dO) tile
   constexpr int RPW = BWD_BQ / 4;          // tile rows fetched by one wave (contiguous)
   constexpr int ROWB = 2 * D;
-  constexpr int LPI = 2 * NLD + 1;  // loads per wave per iteration
+  constexpr int LPI = 2 * NLD + 1 + WINDOW;  // loads per wave per iteration
   constexpr int SUB = 32 * ROWB, HALF = 16 * ROWB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(CA_LDS char *)smem;  // LDS byte address of the dynamic segment
@@ -336,8 +339,35 @@ __device__ __forceinline__ void dkv_workgroup(const int me /* index of the first
     const float *aux_ptr = (wave < 2 ? stats_kv + hk * G * 128 + wave * 64 : reinterpret_cast<const float *>(WINDOW && wave == 3 ? slot_lo : slot_pos)) +
                            (u.slot_begin / BWD_BQ + n_blocks - 1) * aux_bstride;
     const uint32_t aux_lds = wave < 2 ? S::L2_OFF + 256 * wave : wave == 2 ? S::POS_OFF : S::SPARE_OFF;
+    // WINDOW: the rows of tile t are fetched with tile t - NST + 1, every wave for itself (all write the same), and are there when t is
+    // issued, NST - 1 steps later
+    int row_block = u.slot_begin / BWD_BQ + n_blocks - 1, row_ph = 0, row_left = n_it, rst = 0;
+    auto issue_rows = [&]() __attribute__((always_inline)) {
+      load_lds4_sbase(slot_src + int64_t(row_block) * BWD_BQ, uint32_t(lane_id_here()) * 4, lds0 + S::ROWS_OFF + 256 * rst);
+      rst = rst + 1 == NST ? 0 : rst + 1;
+      if (--row_left > 0 && ++row_ph == Gu) row_ph = 0, --row_block;
+    };
     auto issue_next = [&]() __attribute__((always_inline)) {
       const uint32_t st = lds0 + pst * S::STAGE;
+      if constexpr (WINDOW) {
+        const int l = lane_id_here(), r0 = RPW * wave + l / CH;
+        const uint32_t chunk = 16 * ((l % CH) ^ tile_sw<D>(r0));
+        const uint64_t head = (uint64_t)(uintptr_t)Qs + (uint64_t)(hk * G + ph) * ROWB, to_do = (uint64_t)(uintptr_t)dOs - (uint64_t)(uintptr_t)Qs;
+#pragma unroll
+        for (int n = 0; n < NLD; ++n) {
+          const uint32_t row = lds_ld<uint32_t>(lds0 + S::ROWS_OFF + 256 * pst + 4 * (r0 + RPI * n));
+          const uint64_t a = head + (uint64_t)row * uint32_t(Hq * ROWB) + (chunk ^ (D == 128 ? 16 * (2 * ((n & 1) ^ (n >> 1)) + (n >> 1)) : 48 * n));
+          load_lds16_addr(a, st + S::Q_OFF + (RPW * wave + RPI * n) * ROWB);
+          load_lds16_addr(a + to_do, st + S::DO_OFF + (RPW * wave + RPI * n) * ROWB);
+        }
+        load_lds4_sbase(aux_ptr, uint32_t(l) * 4, st + aux_lds);
+        pst = pst + 1 == NST ? 0 : pst + 1;
+        issue_rows();
+        if (--left <= 0) return;
+        if (ph + 1 < Gu) ++ph, aux_ptr += aux_hstride;
+        else ph = 0, aux_ptr -= (Gu - 1) * aux_hstride + aux_bstride;
+        return;
+      }
       uint32_t ld0 = ld_off;
       asm volatile("" : "+v"(ld0));
 #pragma unroll
@@ -360,6 +390,11 @@ __device__ __forceinline__ void dkv_workgroup(const int me /* index of the first
       }
     };
     if (n_it > 0) {
+      if (WINDOW) {
+#pragma unroll
+        for (int i = 0; i < NST - 1; ++i) issue_rows();
+        wait_vmcnt<0>();
+      }
 #pragma unroll
       for (int i = 0; i < NST - 1; ++i) issue_next();
     }

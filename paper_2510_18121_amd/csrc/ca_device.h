@@ -136,6 +136,11 @@ __device__ __forceinline__ void load_lds16_sbase(const void *base_uniform, uint3
                : "v"(lane_off), "s"(sb), "s"(m0v)
                : "memory", "m0");
 }
+// ... from an address per lane
+__device__ __forceinline__ void load_lds16_addr(uint64_t addr, uint32_t lds_off_uniform) {
+  const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds_off_uniform);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(addr), "s"(m0v) : "memory", "m0");
+}
 // the 4-byte form
 __device__ __forceinline__ void load_lds4_sbase(const void *base_uniform, uint32_t lane_off, uint32_t lds_off_uniform) {
   const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds_off_uniform);

@@ -150,9 +150,9 @@ struct ca_plan {
   // windowed plans
   int64_t window = 0;  // 0: none
   int32_t sinks = 0;
-  std::vector<int32_t> slot_lo;
+  std::vector<int32_t> slot_lo, slot_src;  // slot_src: slot_row, with the last row of the run in place of padding
   std::vector<ca::WindowUnit> window_units;  // in place of bwd_units; long ones cut into pieces whose parts are part of ws_bwd
-  const int32_t *d_slot_lo = nullptr;
+  const int32_t *d_slot_lo = nullptr, *d_slot_src = nullptr;
   const ca::WindowUnit *d_window_units = nullptr;
   // device copies
   int device = -1;
@@ -172,5 +172,4 @@ struct ca_plan {
 namespace ca {
 void set_error(const std::string &msg);
 int build_plan(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out);  // host only; window 0: none
-size_t backward_layout(ca_plan_t *p);  // offsets of the backward workspace in slot order; its size
 }  // namespace ca

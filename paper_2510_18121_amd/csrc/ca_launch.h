@@ -8,9 +8,8 @@
 
 namespace ca {
 
-// The backward's first launches: zeros for rows that belong to no unit, and the preparation (with `fused` also what the one pass counts on).
-void prepare_bwd(const ca_plan_t *p, const void *q, const void *o, const void *d_o, const float *lse, void *dq, void *dk, void *dv,
-                 void *ws, bool fused, hipStream_t st);
+// Zeros for gradients of rows that belong to no work unit (KV outside every scheduled document, Q rows outside every task).
+void fill_uncovered(const ca_plan_t *p, void *dq, void *dk, void *dv, hipStream_t st);
 // Adds up the pieces of dK/dV units.
 void combine_dkv(const ca_plan_t *p, const float *parts, void *dk, void *dv, hipStream_t st);
 hipError_t launch_fwd_window(const ca_plan_t *p, const void *q, const void *k, const void *v, void *o, float *lse, hipStream_t st);

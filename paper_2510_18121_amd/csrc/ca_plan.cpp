@@ -563,6 +563,18 @@ bool schedule(ca_plan_t *p, bool beyond_static) {
   for (size_t blk = 0; blk < p->block_rpk.size(); ++blk)
     if (const int rpk = p->block_rpk[blk])
       for (int i = 0; i < BWD_BQ; ++i) p->pos_kv[blk * BWD_BQ + i] = p->slot_pos[blk * BWD_BQ + i % rpk];
+  auto base_workspace = [&]() {
+    // workspace of backward, all in slot order: per (head, slot) fp32 -Delta and log2(e)*LSE, then bf16 copies of Q
+    // and dO as [block of 64 slots][head][64][head_dim] (the dK/dV kernel re-reads their 64-slot tiles once per 128-key
+    // tile: in this layout a tile is one contiguous run and needs no row indices)
+    const size_t per = (size_t(padded) * hq * sizeof(float) + 255) / 256 * 256;
+    const size_t copy = (size_t(padded) * hq * p->d * 2 + 255) / 256 * 256;
+    p->ws_off_l2 = per;
+    p->ws_off_qs = 2 * per;
+    p->ws_off_dos = 2 * per + copy;
+    p->ws_off_stats_kv = 2 * per + 2 * copy;
+    return 4 * per + 2 * copy;
+  };
   // Partial results are bounded: at most this much more than whole units need, and, unless beyond_static, no more than what the
   // library's static workspace has left over (at 8 query heads of 128 it holds 15.8K rows, so from 8K rows on too little to cut
   // with: forward + backward of 9K rows, 8/1 heads, 1.75 ms with what is left and 0.85 ms with 256 MiB).
@@ -637,7 +649,7 @@ bool schedule(ca_plan_t *p, bool beyond_static) {
       }
     };
     lay_out(chains, btiles, p->bwd_units, {}, p->bwd_workgroups);
-    p->ws_bwd = backward_layout(p);
+    p->ws_bwd = base_workspace();
     // the list in which long units that run alone are cut along their query blocks
     cut_budget = p->ws_bwd <= CA_STATIC_WS_BYTES && !beyond_static ? CA_STATIC_WS_BYTES - p->ws_bwd : MAX_CUT_BYTES;
     limits = {cut_budget, MAX_CUT_BYTES};
@@ -927,20 +939,6 @@ std::unique_ptr<ca_plan_t> described(const ca_batch_desc *desc) {
   return p;
 }
 }  // namespace
-
-size_t backward_layout(ca_plan_t *p) {
-  // workspace of backward, all in slot order: per (head, slot) fp32 -Delta and log2(e)*LSE, then bf16 copies of Q
-  // and dO as [block of 64 slots][head][64][head_dim] (the dK/dV kernel re-reads their 64-slot tiles once per 128-key
-  // tile: in this layout a tile is one contiguous run and needs no row indices)
-  const size_t padded = p->slot_row.size();
-  const size_t per = (padded * p->hq * sizeof(float) + 255) / 256 * 256;
-  const size_t copy = (padded * p->hq * p->d * 2 + 255) / 256 * 256;
-  p->ws_off_l2 = per;
-  p->ws_off_qs = 2 * per;
-  p->ws_off_dos = 2 * per + copy;
-  p->ws_off_stats_kv = 2 * per + 2 * copy;
-  return 4 * per + 2 * copy;
-}
 
 int build_plan(const ca_batch_desc *desc, int64_t window, int64_t sinks, ca_plan_t **out) {
   if (!out) {

@@ -58,7 +58,7 @@ inline bool schedule_window(ca_plan_t *p) {
       if (at + n >= size_t(INT32_MAX) - SLOT_ALIGN) return false;
       for (size_t i = 0; i < n; ++i) {
         const Row &r = rows[std::min(a + i, b - 1)];
-        p->slot_row.push_back(a + i < b ? r.row : -1), p->slot_pos.push_back(r.hi), p->slot_lo.push_back(r.lo);
+        p->slot_row.push_back(a + i < b ? r.row : -1), p->slot_pos.push_back(r.hi), p->slot_lo.push_back(r.lo), p->slot_src.push_back(r.row);
       }
       for (size_t i = a; i < b; i += size_t(sub)) {
         const size_t e = std::min(b, i + size_t(sub));
@@ -98,8 +98,6 @@ inline bool schedule_window(ca_plan_t *p) {
     }
     covered_kv += doc_len;
   }
-  p->block_rpk.assign(p->slot_row.size() / BWD_BQ, 0);
-  p->pos_kv = p->slot_pos;
 
   // longest first; unit index modulo KV heads = KV head (see the plan without a window)
   std::stable_sort(ftiles.begin(), ftiles.end(), [](const Tile &a, const Tile &b) { return a.cost > b.cost; });
@@ -186,7 +184,10 @@ inline bool schedule_window(ca_plan_t *p) {
         p->window_units.push_back(f);
       }
     }
-  p->ws_bwd = p->ws_off_parts_kv = backward_layout(p);
+  // workspace of backward: per (head, slot) -Delta and log2(e) * LSE, both once more in the order of dK/dV's tiles, and the parts
+  const size_t per = (p->slot_row.size() * size_t(hq) * sizeof(float) + 255) / 256 * 256;
+  p->ws_off_l2 = per, p->ws_off_stats_kv = 2 * per;
+  p->ws_bwd = p->ws_off_parts_kv = 4 * per;
   p->ws_bwd += size_t(p->n_bwd_parts) * part_bytes(p->d);
   p->ws_bwd_split = p->ws_bwd;
   p->q_covered = covered_q == p->total_q;

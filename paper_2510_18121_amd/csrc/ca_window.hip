@@ -26,13 +26,43 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_fwd_window_kernel(
                                total_q, c);
 }
 
+// Per (slot, head): -Delta = -<dO, O> and log2(e) * LSE, by (head, slot) for dQ and in the order of dK/dV's tiles; rows of padding get
+// probabilities of 0.  D / 8 lanes each.  Bound by memory: 64K tokens of 32 heads of 128 (1.07 GB) in 0.2 ms.
+template <int D>
+__global__ __launch_bounds__(256) void ca_window_prep_kernel(const int32_t *__restrict__ slot_row, const bf16_t *__restrict__ O,
+                                                             const bf16_t *__restrict__ dO, const float *__restrict__ LSE,
+                                                             float *__restrict__ delta_slot, float *__restrict__ l2_slot,
+                                                             float *__restrict__ stats_kv, int64_t padded, int64_t total_q, int Hq) {
+  constexpr int LANES = D / 8;
+  const int64_t pair = int64_t(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const int c = threadIdx.x % LANES;
+  if (pair >= padded * Hq) return;  // (whole groups of lanes)
+  const int64_t slot = pair / Hq;
+  const int h = int(pair - slot * Hq), row = slot_row[slot];
+  float s = 0.f;
+  if (row >= 0) {
+    const size_t off = (size_t(row) * Hq + h) * D + 8 * c;
+    const bf16x8 a = *reinterpret_cast<const bf16x8 *>(O + off), b = *reinterpret_cast<const bf16x8 *>(dO + off);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += float(a[i]) * float(b[i]);
+  }
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
+  if (c != 0) return;
+  const float nd = row >= 0 ? -s : 0.f, l2 = row >= 0 ? LSE[int64_t(h) * total_q + row] * LOG2E : L2_PADDING;
+  delta_slot[int64_t(h) * padded + slot] = nd;
+  l2_slot[int64_t(h) * padded + slot] = l2;
+  float *const st = stats_kv + (((slot / BWD_BQ) * Hq + h) * 2 + slot % BWD_BQ / 32) * 64 + slot % 32;
+  st[0] = l2, st[32] = nd;
+}
+
 // dK/dV workgroups, then dQ workgroups (halves of units), in one launch: both are of four waves, two to a CU (three at head_dim 64), and
 // the second kind fills the CUs that the first leaves idle.
 struct WindowArgs {
   const WindowUnit *units;
   const FwdUnit *dq_units;
-  const int32_t *slot_row, *slot_pos, *slot_lo;
-  const bf16_t *q, *k, *v, *d_o, *q_sorted, *do_sorted;
+  const int32_t *slot_row, *slot_pos, *slot_lo, *slot_src;
+  const bf16_t *q, *k, *v, *d_o;
   const float *l2_slot, *delta_slot, *stats_kv;
   bf16_t *dq, *dk, *dv;
   float *parts;
@@ -44,7 +74,7 @@ template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_bwd_window_kernel(const WindowArgs a) {
   const int i = int(blockIdx.x);
   if (i < a.n_dkv) {
-    dkv_workgroup<D, true>(i, a.units, a.slot_pos, a.slot_lo, a.sinks, a.q_sorted, a.k, a.v, a.do_sorted, a.stats_kv, a.dk, a.dv, a.parts, a.hq,
+    dkv_workgroup<D, true>(i, a.units, a.slot_pos, a.slot_lo, a.slot_src, a.sinks, a.q, a.k, a.v, a.d_o, a.stats_kv, a.dk, a.dv, a.parts, a.hq,
                            a.hkv, a.scale);
   } else {
     int unit = i - a.n_dkv, half;
@@ -76,7 +106,8 @@ hipError_t launch_fwd_window(const ca_plan_t *p, const void *q, const void *k, c
 template <int D>
 static hipError_t launch_bwd_window_t(const ca_plan_t *p, const void *q, const void *k, const void *v, const void *o, const void *d_o,
                                       const float *lse, void *dq, void *dk, void *dv, void *ws, hipStream_t st, hipEvent_t *ev) {
-  constexpr int SMEM = std::max(DkvSmem<D>::TOTAL, DqSmem<D, 4, true>::TOTAL);
+  constexpr int SMEM = std::max(DkvSmem<D, true>::TOTAL, DqSmem<D, 4, true>::TOTAL);
+  static_assert((D == 64 ? 3 : 2) * SMEM <= 160 * 1024, "as many workgroups to a CU as the registers allow");
   auto kern = ca_bwd_window_kernel<D>;
   static std::atomic<bool> done[16];
   const hipError_t e = set_smem(kern, SMEM, p->device, done);
@@ -85,11 +116,11 @@ static hipError_t launch_bwd_window_t(const ca_plan_t *p, const void *q, const v
   auto in = [](const void *x) { return static_cast<const bf16_t *>(x); };
   auto out = [](void *x) { return static_cast<bf16_t *>(x); };
   WindowArgs a = {};
-  a.units = p->d_window_units, a.dq_units = p->d_fwd_units, a.slot_row = p->d_slot_row, a.slot_pos = p->d_slot_pos, a.slot_lo = p->d_slot_lo;
+  a.units = p->d_window_units, a.dq_units = p->d_fwd_units, a.slot_row = p->d_slot_row, a.slot_pos = p->d_slot_pos, a.slot_lo = p->d_slot_lo, a.slot_src = p->d_slot_src;
   a.q = in(q), a.k = in(k), a.v = in(v), a.d_o = in(d_o);
-  a.q_sorted = reinterpret_cast<bf16_t *>(at + p->ws_off_qs), a.do_sorted = reinterpret_cast<bf16_t *>(at + p->ws_off_dos);
-  a.delta_slot = reinterpret_cast<float *>(at), a.l2_slot = reinterpret_cast<float *>(at + p->ws_off_l2);
-  a.stats_kv = reinterpret_cast<float *>(at + p->ws_off_stats_kv);
+  float *const delta_slot = reinterpret_cast<float *>(at), *const l2_slot = reinterpret_cast<float *>(at + p->ws_off_l2);
+  float *const stats_kv = reinterpret_cast<float *>(at + p->ws_off_stats_kv);
+  a.delta_slot = delta_slot, a.l2_slot = l2_slot, a.stats_kv = stats_kv;
   a.dq = out(dq), a.dk = out(dk), a.dv = out(dv), a.parts = reinterpret_cast<float *>(at + p->ws_off_parts_kv);
   a.hq = p->hq, a.hkv = p->hkv, a.sinks = p->sinks, a.padded = int64_t(p->slot_row.size()), a.scale = p->scale;
   auto launch = [&](int n_dkv, int n_dq) {
@@ -97,7 +128,12 @@ static hipError_t launch_bwd_window_t(const ca_plan_t *p, const void *q, const v
     if (n_dkv + n_dq > 0) hipLaunchKernelGGL(kern, dim3(unsigned(n_dkv + 2 * n_dq)), dim3(256), SMEM, st, a);
   };
   if (ev) (void)hipEventRecord(ev[0], st);
-  prepare_bwd(p, q, o, d_o, lse, dq, dk, dv, ws, false, st);
+  fill_uncovered(p, dq, dk, dv, st);
+  if (a.padded > 0) {
+    const int64_t groups = (a.padded * a.hq + 256 / (D / 8) - 1) / (256 / (D / 8));
+    hipLaunchKernelGGL(ca_window_prep_kernel<D>, dim3(unsigned(groups)), dim3(256), 0, st, p->d_slot_row, in(o), in(d_o), lse, delta_slot,
+                       l2_slot, stats_kv, a.padded, p->total_q, a.hq);
+  }
   if (ev) (void)hipEventRecord(ev[1], st);
   const int n_dq = int(p->fwd_units.size());
   launch(p->bwd_workgroups, ev ? 0 : n_dq);  // (with timing enabled the same workgroups run as two launches, so that each kind has a time)
