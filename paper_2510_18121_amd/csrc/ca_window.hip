@@ -26,33 +26,41 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_fwd_window_kernel(
                                total_q, c);
 }
 
-// Per (slot, head): -Delta = -<dO, O> and log2(e) * LSE, by (head, slot) for dQ and in the order of dK/dV's tiles; rows of padding get
-// probabilities of 0.  D / 8 lanes each.  Bound by memory: 64K tokens of 32 heads of 128 (1.07 GB) in 0.2 ms.
+// -Delta = -<dO, O> and log2(e) * LSE of 64 slots and a head, by (head, slot) for dQ and in the order of dK/dV's tiles; rows of padding get
+// probabilities of 0.  D / 8 lanes per row; the statistics leave through LDS as whole lines.  Bound by memory.
 template <int D>
 __global__ __launch_bounds__(256) void ca_window_prep_kernel(const int32_t *__restrict__ slot_row, const bf16_t *__restrict__ O,
                                                              const bf16_t *__restrict__ dO, const float *__restrict__ LSE,
                                                              float *__restrict__ delta_slot, float *__restrict__ l2_slot,
                                                              float *__restrict__ stats_kv, int64_t padded, int64_t total_q, int Hq) {
-  constexpr int LANES = D / 8;
-  const int64_t pair = int64_t(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
-  const int c = threadIdx.x % LANES;
-  if (pair >= padded * Hq) return;  // (whole groups of lanes)
-  const int64_t slot = pair / Hq;
-  const int h = int(pair - slot * Hq), row = slot_row[slot];
-  float s = 0.f;
-  if (row >= 0) {
-    const size_t off = (size_t(row) * Hq + h) * D + 8 * c;
-    const bf16x8 a = *reinterpret_cast<const bf16x8 *>(O + off), b = *reinterpret_cast<const bf16x8 *>(dO + off);
+  constexpr int LANES = D / 8, ROWS = 256 / LANES, N = BWD_BQ / ROWS;
+  __shared__ float delta[BWD_BQ];
+  const int64_t block = blockIdx.x / Hq;
+  const int h = int(blockIdx.x - block * Hq), i0 = threadIdx.x / LANES, c = threadIdx.x % LANES;
+  const int32_t *const rows = slot_row + block * BWD_BQ;
+  bf16x8 a[N], b[N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += float(a[i]) * float(b[i]);
+  for (int n = 0; n < N; ++n) {
+    const int row = max(0, rows[i0 + ROWS * n]);
+    const size_t off = (size_t(row) * Hq + h) * D + 8 * c;
+    a[n] = *reinterpret_cast<const bf16x8 *>(O + off), b[n] = *reinterpret_cast<const bf16x8 *>(dO + off);
   }
 #pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
-  if (c != 0) return;
-  const float nd = row >= 0 ? -s : 0.f, l2 = row >= 0 ? LSE[int64_t(h) * total_q + row] * LOG2E : L2_PADDING;
-  delta_slot[int64_t(h) * padded + slot] = nd;
-  l2_slot[int64_t(h) * padded + slot] = l2;
-  float *const st = stats_kv + (((slot / BWD_BQ) * Hq + h) * 2 + slot % BWD_BQ / 32) * 64 + slot % 32;
+  for (int n = 0; n < N; ++n) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += float(a[n][i]) * float(b[n][i]);
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (c == 0) delta[i0 + ROWS * n] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x >= BWD_BQ) return;
+  const int i = threadIdx.x, row = rows[i];
+  const float nd = row >= 0 ? -delta[i] : 0.f, l2 = row >= 0 ? LSE[int64_t(h) * total_q + row] * LOG2E : L2_PADDING;
+  delta_slot[int64_t(h) * padded + block * BWD_BQ + i] = nd;
+  l2_slot[int64_t(h) * padded + block * BWD_BQ + i] = l2;
+  float *const st = stats_kv + ((block * Hq + h) * 2 + i / 32) * 64 + i % 32;
   st[0] = l2, st[32] = nd;
 }
 
@@ -130,8 +138,7 @@ static hipError_t launch_bwd_window_t(const ca_plan_t *p, const void *q, const v
   if (ev) (void)hipEventRecord(ev[0], st);
   fill_uncovered(p, dq, dk, dv, st);
   if (a.padded > 0) {
-    const int64_t groups = (a.padded * a.hq + 256 / (D / 8) - 1) / (256 / (D / 8));
-    hipLaunchKernelGGL(ca_window_prep_kernel<D>, dim3(unsigned(groups)), dim3(256), 0, st, p->d_slot_row, in(o), in(d_o), lse, delta_slot,
+    hipLaunchKernelGGL(ca_window_prep_kernel<D>, dim3(unsigned(a.padded / BWD_BQ * a.hq)), dim3(256), 0, st, p->d_slot_row, in(o), in(d_o), lse, delta_slot,
                        l2_slot, stats_kv, a.padded, p->total_q, a.hq);
   }
   if (ev) (void)hipEventRecord(ev[1], st);
