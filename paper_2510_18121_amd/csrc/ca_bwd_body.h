@@ -269,8 +269,10 @@ struct DkvSmem {
   static constexpr int POS_OFF = L2_OFF + 512;
   static constexpr int SPARE_OFF = POS_OFF + 256;
   static constexpr int STAGE = 2 * TILE + 1024;
-  static constexpr int ROWS_OFF = NST * STAGE;      // WINDOW: packed rows of the tiles that are fetched next, [NST][64]
-  static constexpr int TOTAL = ROWS_OFF + (WINDOW ? NST * 256 : 0);
+  // WINDOW: packed rows of the tiles that are fetched next, [NROWS][64].  A wave that is ahead of the others before the first barrier has
+  // issued NST - 1 tiles and fetched the rows of as many more, while another may not have read those of tile 0.
+  static constexpr int NROWS = 2 * NST - 2, ROWS_OFF = NST * STAGE;
+  static constexpr int TOTAL = ROWS_OFF + (WINDOW ? NROWS * 256 : 0);
   static_assert(4 * PATCH_BYTES <= NST * STAGE, "patches fit in the stages");
 };
 
@@ -341,10 +343,10 @@ __device__ __forceinline__ void dkv_workgroup(const int me /* index of the first
     const uint32_t aux_lds = wave < 2 ? S::L2_OFF + 256 * wave : wave == 2 ? S::POS_OFF : S::SPARE_OFF;
     // WINDOW: the rows of tile t are fetched with tile t - NST + 1, every wave for itself (all write the same), and are there when t is
     // issued, NST - 1 steps later
-    int row_block = u.slot_begin / BWD_BQ + n_blocks - 1, row_ph = 0, row_left = n_it, rst = 0;
+    int row_block = u.slot_begin / BWD_BQ + n_blocks - 1, row_ph = 0, row_left = n_it, rst = 0, rd = 0;
     auto issue_rows = [&]() __attribute__((always_inline)) {
       load_lds4_sbase(slot_src + int64_t(row_block) * BWD_BQ, uint32_t(lane_id_here()) * 4, lds0 + S::ROWS_OFF + 256 * rst);
-      rst = rst + 1 == NST ? 0 : rst + 1;
+      rst = rst + 1 == S::NROWS ? 0 : rst + 1;
       if (--row_left > 0 && ++row_ph == Gu) row_ph = 0, --row_block;
     };
     auto issue_next = [&]() __attribute__((always_inline)) {
@@ -355,13 +357,14 @@ __device__ __forceinline__ void dkv_workgroup(const int me /* index of the first
         const uint64_t head = (uint64_t)(uintptr_t)Qs + (uint64_t)(hk * G + ph) * ROWB, to_do = (uint64_t)(uintptr_t)dOs - (uint64_t)(uintptr_t)Qs;
 #pragma unroll
         for (int n = 0; n < NLD; ++n) {
-          const uint32_t row = lds_ld<uint32_t>(lds0 + S::ROWS_OFF + 256 * pst + 4 * (r0 + RPI * n));
+          const uint32_t row = lds_ld<uint32_t>(lds0 + S::ROWS_OFF + 256 * rd + 4 * (r0 + RPI * n));
           const uint64_t a = head + (uint64_t)row * uint32_t(Hq * ROWB) + (chunk ^ (D == 128 ? 16 * (2 * ((n & 1) ^ (n >> 1)) + (n >> 1)) : 48 * n));
           load_lds16_addr(a, st + S::Q_OFF + (RPW * wave + RPI * n) * ROWB);
           load_lds16_addr(a + to_do, st + S::DO_OFF + (RPW * wave + RPI * n) * ROWB);
         }
         load_lds4_sbase(aux_ptr, uint32_t(l) * 4, st + aux_lds);
         pst = pst + 1 == NST ? 0 : pst + 1;
+        rd = rd + 1 == S::NROWS ? 0 : rd + 1;
         issue_rows();
         if (--left <= 0) return;
         if (ph + 1 < Gu) ++ph, aux_ptr += aux_hstride;

@@ -147,8 +147,9 @@ struct AttendArgs {
 
 // Rows of a sequence and KV head, token by token and then by head of the group, make up tiles of R = 16 NR; a unit of work is a page
 // of a tile.  The units of all sequences, in order, are dealt to the workers in equal runs, whatever the sequences' lengths
-// are; a run that ends inside a tile of at most CUT pages is moved to the tile's nearer end, longer tiles are cut.
-constexpr int CUT = 24;
+// are; a run that ends inside a tile of at most CUT pages is moved to the tile's nearer end, longer tiles are cut.  (A CU takes 1100
+// cycles per page that it reads alone, of head_dim 128, and what adding up the parts takes 10 thousand, most of it between launches.)
+constexpr int CUT = 16;
 __device__ __forceinline__ int tile_pages(int len, int R, int G, int window, int sinks) {
   const int pages = (len + PAGE - 1) / PAGE;
   if (window >= len) return max(1, pages);
@@ -193,9 +194,11 @@ struct WorkSplit {
 
 // Scores x of a page (of row group rg; -infinity where a key is not seen) to the operand of P V; ks and vs: the page's scales, ks with
 // the softmax's factor in base 2.  The reference m moves when some row's maximum has grown by more than 2^8 (see the forward kernel).
+// P is the sum of two bf16 operands (hi + lo): rounded once more to one alone, O would be off by 1.4 times what its own rounding costs, and
+// the matrix pipe is idle most of the time here.
 template <int NB, int NR>
 __device__ __forceinline__ void softmax_page(const f32x4 (&x)[4][NR], int rg, float ks, float vs, float &m, float &l, f32x4 (&acc)[NB][NR],
-                                             bf16x8 (&pb)[2][NR]) {
+                                             bf16x8 (&pb)[2][NR], bf16x8 (&pl)[2][NR]) {
   float top = x[0][rg][0];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
@@ -208,17 +211,26 @@ __device__ __forceinline__ void softmax_page(const f32x4 (&x)[4][NR], int rg, fl
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b][rg] *= f;
   }
-  uint32_t w[2][4];
+  uint32_t w[2][4], r[2][4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     float p[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) p[e] = fast_exp2(fmaf(x[t][rg][e], ks, -m));
     l += (p[0] + p[1]) + (p[2] + p[3]);
-    w[t >> 1][2 * (t & 1)] = pack_bf16(p[0] * vs, p[1] * vs), w[t >> 1][2 * (t & 1) + 1] = pack_bf16(p[2] * vs, p[3] * vs);
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      const float a = p[e] * vs, b = p[e + 1] * vs;
+      const uint32_t hi = pack_bf16(a, b);
+      w[t >> 1][2 * (t & 1) + e / 2] = hi;
+      r[t >> 1][2 * (t & 1) + e / 2] = pack_bf16(a - __builtin_bit_cast(float, hi << 16), b - __builtin_bit_cast(float, hi & 0xFFFF0000u));
+    }
   }
-  pb[0][rg] = __builtin_bit_cast(bf16x8, u32x4{w[0][0], w[0][1], w[0][2], w[0][3]});
-  pb[1][rg] = __builtin_bit_cast(bf16x8, u32x4{w[1][0], w[1][1], w[1][2], w[1][3]});
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    pb[kk][rg] = __builtin_bit_cast(bf16x8, u32x4{w[kk][0], w[kk][1], w[kk][2], w[kk][3]});
+    pl[kk][rg] = __builtin_bit_cast(bf16x8, u32x4{r[kk][0], r[kk][1], r[kk][2], r[kk][3]});
+  }
 }
 
 template <int D, int NR, int W>
@@ -353,9 +365,9 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kerne
             for (int b = 0; b < NB; ++b) vr[b][w] &= keep;
           }
         }
-        bf16x8 pb[2][NR];
+        bf16x8 pb[2][NR], pl[2][NR];
 #pragma unroll
-        for (int rg = 0; rg < NR; ++rg) softmax_page<NB>(x, rg, ksi, vsi, m[rg], l[rg], acc, pb);
+        for (int rg = 0; rg < NR; ++rg) softmax_page<NB>(x, rg, ksi, vsi, m[rg], l[rg], acc, pb, pl);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           const bf16x8 v0 = codes_to_bf16(vr[b][0], vr[b][1]), v1 = codes_to_bf16(vr[b][2], vr[b][3]);
@@ -363,6 +375,8 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kerne
           for (int rg = 0; rg < NR; ++rg) {
             acc[b][rg] = mfma16(v0, pb[0][rg], acc[b][rg]);
             acc[b][rg] = mfma16(v1, pb[1][rg], acc[b][rg]);
+            acc[b][rg] = mfma16(v0, pl[0][rg], acc[b][rg]);
+            acc[b][rg] = mfma16(v1, pl[1][rg], acc[b][rg]);
           }
         }
         if (next >= 0) load_v(next);

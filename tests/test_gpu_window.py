@@ -66,6 +66,25 @@ def test_windows_of_many_tiles_and_cut_sink_tiles():
     check(b, 1024, 4, run(b, 1024, 4, tensors), tensors)
 
 
+@pytest.mark.parametrize("heads,d", [((16, 16), 64), ((16, 16), 128), ((8, 8), 64)])
+def test_chained_units_of_many_documents(heads, d):
+    """Short dK/dV units, several to a workgroup one after the other, and more workgroups than run at a time."""
+    n_docs, n = 26, 650
+    b = U.batch([n] * n_docs, [(i, 0, n) for i in range(n_docs)], *heads, d, seed=11)
+    info = B.ca_plan_host(b, window=100, sinks=0).info()
+    assert (info["n_bwd_workgroups"] < info["n_bwd_units"]) == (heads == (16, 16))  # (the other: whole units alone)
+    tensors = W.make_tensors(b, DEV)
+    first = run(b, 100, 0, tensors)
+    one = U.batch([n], [(0, 0, n)], 2, 2, d)
+    for doc, h in ((0, 0), (13, 4), (25, heads[0] - 2), (7, 2)):
+        of = slice(doc * n, doc * n + n), slice(h, h + 2)
+        part = {x: y[of] if x != "lse" else y[h:h + 2, of[0]] for x, y in first.items()}
+        check(one, 100, 0, part, tuple(x[of] for x in tensors))
+    for _ in range(3):
+        again = run(b, 100, 0, tensors)
+        assert all(torch.equal(again[x], first[x]) for x in first)
+
+
 @pytest.mark.parametrize("factor", [8.0, 60.0])
 def test_scores_that_outgrow_the_first_keys(factor):
     """Early keys are small and later ones large: the reference of the exponentials is outgrown and rows are computed again."""
