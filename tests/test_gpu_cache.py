@@ -144,6 +144,50 @@ def test_scores_that_grow_along_the_pages_and_a_softmax_scale():
     U.check(*attend(c, q, [1], lens, table, softmax_scale=0.3), U.attend(c, q, [1], lens, table, scale=0.3))
 
 
+@pytest.mark.parametrize("rows", [1, 20, 200])
+def test_scales_far_from_one(rows):
+    """V's of 0, tiny, huge and not a power of two, beside each other; a K scale of 0."""
+    lens = [600]
+    table, pages = U.layout(lens, seed=21)
+    c = filled(pages, 2, 64)
+    for i, p in enumerate(table[0].tolist()):
+        c.v_scale[p] = (0.3, 0.0, 2.0 ** -60, 1e-3, 2.0 ** -120, 0.7, 1.0, 2.0 ** -39, 3.0, 0.5)[i]
+        if i == 3:
+            c.k_scale[p] = 0.0
+    q = queries(rows, 4, 64)
+    U.check(*attend(c, q, [rows], lens, table), U.attend(c, q, [rows], lens, table))
+    c.v_scale *= 2.0 ** 50
+    o, lse = attend(c, q, [rows], lens, table)
+    want = U.attend(c, q, [rows], lens, table)
+    U.check(o, lse, want)
+
+
+def test_as_many_sequences_as_there_may_be():
+    n, lens = [1] * 4096, (np.arange(4096) % 3 + 1).tolist()
+    table, pages = U.layout(lens, seed=22)
+    c = power_scales(filled(pages, 1, 64))
+    new, q = new_tokens(4096, 1, 64, 23), queries(4096, 2, 64)
+    want = held(c)
+    U.append(want, new.double().cpu().numpy(), n, lens, table)
+    do_append(c, new, n, lens, table)
+    same(c, want)
+    U.check(*attend(c, q, n, lens, table), U.attend(c, q, n, lens, table))
+    with pytest.raises(B.CaError) as e:
+        attend(c, q, n + [0], lens + [0], np.concatenate([table, table[:1]]))
+    assert e.value.code == B.CA_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("g", [3, 5, 7, 24, 64])
+def test_groups_that_are_no_power_of_two_and_rows_that_cross_tiles(g):
+    n, lens = [37, 90, 1], [500, 90, 33]
+    table, pages = U.layout(lens, seed=24)
+    c = filled(pages, 1, 64)
+    poison(c, lens, table)
+    q = queries(sum(n), g, 64)
+    for window, sinks in ((None, 0), (50, 2)):
+        U.check(*attend(c, q, n, lens, table, window, sinks), U.attend(c, q, n, lens, table, window, sinks))
+
+
 def test_runs_repeat_bit_for_bit_also_from_a_graph_that_follows_the_lengths():
     lens = [5000, 700, 64]
     table, pages = U.layout([5200, 900, 200], seed=8)
@@ -214,7 +258,7 @@ def same(c, want):
 @pytest.mark.parametrize("heads,d", [(2, 64), (1, 128), (8, 128), (5, 64)])
 @pytest.mark.parametrize("spread", [0.0, 3.0])
 @pytest.mark.parametrize("n,lens", [([1, 1, 1, 1, 1, 1], [1, 64, 65, 100, 128, 1000]), ([300, 0, 1, 64, 63, 7], [300, 40, 70, 130, 63, 71]),
-                                    ([128, 2], [128, 3])])
+                                    ([128, 2], [128, 3]), ([1, 2] * 50, [5, 130] * 50)])
 def test_append_bit_for_bit(heads, d, spread, n, lens):
     table, pages = U.layout(lens, seed=11)
     c = power_scales(filled(pages, heads, d, seed=1))
