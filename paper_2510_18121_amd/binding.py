@@ -391,74 +391,70 @@ def ca_sum_partial_dq(part_rows, dq_part, dq, stream=None):
     _check(lib().ca_sum_partial_dq(_p(part_rows), n_rows, n_parts, _p(dq_part), tq, _p(dq), hq, d, _stream_ptr(stream)))
 
 
+# The calls on a cache run once per layer and token: what they check of their tensors is a good part of what the small ones take.
+def _on_cache(cache, t, shape, dtype, name) -> int:
+    """Address of a contiguous tensor of that shape and type on the cache's device."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != cache.index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous tensor {tuple(shape)} {dtype} on {cache.device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
 def _cache_batch(cache, rows, q_start, kv_len, page_table) -> CacheBatch:
-    import torch
-    n = kv_len.shape[0]
+    i32, n = cache.i32, kv_len.shape[0]
     if page_table.dim() != 2:
         raise ValueError(f"page_table: expected [{n}, pages], got {tuple(page_table.shape)}")
-    for t, shape, name in ((q_start, (n + 1,), "q_start"), (kv_len, (n,), "kv_len"), (page_table, (n, page_table.shape[1]), "page_table")):
-        _expect(t, shape, torch.int32, name)
-        if t.device != cache.device:
-            raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
-    return CacheBatch(n, page_table.shape[1], rows, _p(q_start), _p(kv_len), _p(page_table))
+    width = page_table.shape[1]
+    return CacheBatch(n, width, rows, _on_cache(cache, q_start, (n + 1,), i32, "q_start"), _on_cache(cache, kv_len, (n,), i32, "kv_len"),
+                      _on_cache(cache, page_table, (n, width), i32, "page_table"))
 
 
-def _expect_on(cache, t, shape, dtype, name):
-    _expect(t, shape, dtype, name)
-    if t.device != cache.device:
-        raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
-
-
-def _current(cache):
-    """The cache's memory is on the current device (the streams of another would not order the work with its own)."""
-    import torch
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {cache.device}, the current device is {torch.cuda.current_device()}")
+def _cache_stream(cache, stream):
+    """The stream's address; the cache's memory has to be on the current device, whose streams order the work on it."""
+    current = cache.current_device()
+    if cache.index != current:
+        raise ValueError(f"the cache is on {cache.device}, the current device is {current}")
+    return _stream_ptr(stream) if stream is not None or cache.raw_stream is None else cache.raw_stream(current)
 
 
 def ca_cache_append(cache, k, v, q_start, kv_len, page_table, stream=None):
     """Quantise the rows of k and v (bf16 [rows, n_kv_heads, head_dim]) into the pages of their sequences (cache: cache.KVCache; the
     arrays: device int32, see the header).  On torch's current stream, or `stream`."""
-    import torch
-    for t, name in ((k, "k"), (v, "v")):
-        _expect_on(cache, t, (k.shape[0], cache.n_kv_heads, cache.head_dim), torch.bfloat16, name)
-    b = _cache_batch(cache, k.shape[0], q_start, kv_len, page_table)
-    _current(cache)
-    _check(lib().ca_cache_append(ctypes.byref(cache.desc), ctypes.byref(b), _p(k), _p(v), _stream_ptr(stream)))
+    rows = k.shape[0]
+    shape = (rows, cache.n_kv_heads, cache.head_dim)
+    kp, vp = _on_cache(cache, k, shape, cache.bf16, "k"), _on_cache(cache, v, shape, cache.bf16, "v")
+    b = _cache_batch(cache, rows, q_start, kv_len, page_table)
+    _check(lib().ca_cache_append(cache.desc_ref, ctypes.byref(b), kp, vp, _cache_stream(cache, stream)))
 
 
 def ca_cache_attend(cache, q, o, lse, q_start, kv_len, page_table, ws, window=None, sinks=0, softmax_scale=0.0, stream=None):
     """Attention of the rows of q (bf16 [rows, n_q_heads, head_dim]) over the cached tokens of their sequences.  Writes o (like q) and,
     unless it is None, lse (fp32 [n_q_heads, rows]); ws: alloc_cache_workspace."""
-    import torch
-    rows, hq, _ = q.shape
-    _expect_on(cache, q, (rows, hq, cache.head_dim), torch.bfloat16, "q")
-    _expect_on(cache, o, q.shape, torch.bfloat16, "o")
-    if lse is not None:
-        _expect_on(cache, lse, (hq, rows), torch.float32, "lse")
-    if window is not None and operator.index(window) < 1:
+    rows, hq, _ = shape = q.shape
+    if window is None:
+        window = 0
+    elif operator.index(window) < 1:
         raise ValueError(f"window {window}: at least 1, or None")
+    qp = _on_cache(cache, q, (rows, hq, cache.head_dim), cache.bf16, "q")
+    op = _on_cache(cache, o, shape, cache.bf16, "o")
+    lp = None if lse is None else _on_cache(cache, lse, (hq, rows), cache.f32, "lse")
     b = _cache_batch(cache, rows, q_start, kv_len, page_table)
-    _current(cache)
-    _check(lib().ca_cache_attend(ctypes.byref(cache.desc), ctypes.byref(b), hq, float(softmax_scale), 0 if window is None else operator.index(window),
-                                 operator.index(sinks), _p(q), _p(o), _p(lse), _p(ws), ws.numel() * ws.element_size() if ws is not None else 0,
-                                 _stream_ptr(stream)))
+    wp, n = (None, 0) if ws is None else (_on_cache(cache, ws, ws.shape, ws.dtype, "ws"), ws.numel() * ws.element_size())
+    _check(lib().ca_cache_attend(cache.desc_ref, ctypes.byref(b), hq, softmax_scale, operator.index(window), operator.index(sinks), qp, op, lp, wp,
+                                 n, _cache_stream(cache, stream)))
 
 
 def ca_cache_copy_pages(cache, src, dst, stream=None):
     """Copy page src[i] of the cache to page dst[i] (device int32 [n]; no page is written twice or both written and read)."""
-    import torch
-    for t, name in ((src, "src"), (dst, "dst")):
-        _expect_on(cache, t, (src.shape[0],), torch.int32, name)
-    _current(cache)
-    _check(lib().ca_cache_copy_pages(ctypes.byref(cache.desc), _p(src), _p(dst), src.shape[0], _stream_ptr(stream)))
+    n = src.shape[0]
+    sp, dp = _on_cache(cache, src, (n,), cache.i32, "src"), _on_cache(cache, dst, (n,), cache.i32, "dst")
+    _check(lib().ca_cache_copy_pages(cache.desc_ref, sp, dp, n, _cache_stream(cache, stream)))
 
 
 def alloc_cache_workspace(cache, n_q_heads, device=None):
     """A torch uint8 buffer big enough for ca_cache_attend on that cache.  Calls that may overlap in time need one each."""
     import torch
     n = ctypes.c_size_t()
-    _check(lib().ca_cache_attend_workspace_bytes(ctypes.byref(cache.desc), operator.index(n_q_heads), ctypes.byref(n)))
+    _check(lib().ca_cache_attend_workspace_bytes(cache.desc_ref, operator.index(n_q_heads), ctypes.byref(n)))
     return torch.empty(n.value, dtype=torch.uint8, device=cache.device if device is None else device)
 
 

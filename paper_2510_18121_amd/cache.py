@@ -46,6 +46,11 @@ class KVCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.n_kv_heads, self.head_dim, self.device = pages, heads, dim, k.device
         self.desc = CacheDesc(pages, heads, dim, *(t.data_ptr() if pages else None for t in (k, v, k_scale, v_scale)))
+        self.desc_ref = ctypes.byref(self.desc)
+        # what the calls look up every time
+        self.index = k.get_device() if k.is_cuda else None  # (None: no tensor is there)
+        self.i32, self.f32, self.bf16 = torch.int32, torch.float32, torch.bfloat16
+        self.current_device, self.raw_stream = torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
     @classmethod
     def empty(cls, n_pages, n_kv_heads, head_dim, device="cuda"):
