@@ -16,6 +16,7 @@ One `Sequences` serves the caches of all layers, which then hold a token in the 
 from __future__ import annotations
 
 import ctypes
+import operator
 
 import numpy as np
 
@@ -109,7 +110,7 @@ class Sequences:
     def extend(self, seqs, rows, device=None):
         """Room for rows[i] more tokens of seqs[i], and the call's arrays: q_start, kv_len and page_table on the device.  A last page that
         other sequences hold too is copied for each of them first.  On the current stream."""
-        seqs, rows = list(seqs), [int(n) for n in rows]
+        seqs, rows = list(seqs), [operator.index(n) for n in rows]
         if len(seqs) != len(rows) or len(set(seqs)) != len(seqs) or any(n < 0 for n in rows):
             raise ValueError("extend: one count of rows, not negative, for each of the sequences, and each of them once")
         need, copies, taken = 0, [], {}
@@ -150,7 +151,8 @@ class Sequences:
         return tuple(torch.from_numpy(x).to(device) for x in (start, np.array([self.lengths[s] for s in seqs], np.int32), table))
 
     def compact(self):
-        """Moves the pages in use to the front of the pool; returns how many are in use."""
+        """Moves the pages in use to the front of the pool, on the current stream; returns how many are in use.  Page tables made before are
+        out of date."""
         n = sum(u > 0 for u in self.uses)
         holes = [p for p in range(n) if self.uses[p] == 0]
         moved = dict(zip([p for p in range(n, len(self.uses)) if self.uses[p]], holes))

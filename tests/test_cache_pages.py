@@ -67,6 +67,9 @@ def test_a_full_pool_refuses_and_changes_nothing():
             s.extend(seqs, rows)
     with pytest.raises(KeyError):
         s.extend([99], [1])
+    with pytest.raises(TypeError):
+        s.extend([a], [1.5])
+    assert before == (s.lengths, s.pages, s.uses, s.free_pages)
 
 
 @pytest.mark.parametrize("window,sinks", [(1, 0), (64, 0), (65, 3), (200, 64), (130, 65)])

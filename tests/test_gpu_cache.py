@@ -327,6 +327,16 @@ def test_append_leaves_other_pages_alone_and_skips_missing_ones():
     same(c, want)
 
 
+def test_more_rows_than_tokens():
+    """Rows before a sequence's first token are not stored."""
+    table = np.array([[1], [0]], np.int32)
+    c, d = power_scales(filled(2, 2, 64, seed=4)), power_scales(filled(2, 2, 64, seed=4))
+    new = new_tokens(8, 2, 64, 31)
+    do_append(c, new, [5, 3], [3, 3], table)
+    do_append(d, new[:, 2:].contiguous(), [3, 3], [3, 3], table)
+    same(c, held(d))
+
+
 def test_copies():
     c = filled(9, 3, 64, seed=3)
     before = [x.clone() for x in (c.k.view(torch.uint8), c.v.view(torch.uint8), c.k_scale, c.v_scale)]

@@ -144,7 +144,7 @@ def test_differentiable_op_and_gradients_against_differences():
     assert abs((loss(1e-5) - loss(-1e-5)) / 2e-5 - slope) <= 1e-6 * abs(slope) + 1e-6
 
 
-def test_replayed_from_a_graph_beside_an_eager_graph_of_the_same_leaves():
+def test_replayed_from_a_graph_with_eager_work_between():
     b = U.batch([800], [(0, 0, 800)], 8, 2, 64, seed=9)
     q, k, v, d_o = W.make_tensors(b, DEV)
     want = run(b, 100, 4, (q, k, v, d_o))
@@ -184,6 +184,60 @@ def test_too_small_a_workspace_is_refused():
     with pytest.raises(B.CaError) as e:
         B.ca_backward(plan, q, k, v, q, d_o, lse, torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), ws)
     assert e.value.code == B.CA_ERR_WORKSPACE
+
+
+def test_on_the_librarys_own_workspace():
+    b = U.batch([800], [(0, 0, 800)], 8, 2, 64, seed=9)
+    q, k, v, d_o = tensors = W.make_tensors(b, DEV)
+    want = run(b, 100, 4, tensors)
+    plan = B.ca_plan(b, window=100, sinks=4)
+    got = {n: torch.full_like(want[n], 7.0) for n in ("dq", "dk", "dv")}
+    B.ca_backward_static_ws(plan, q, k, v, want["o"], d_o, want["lse"], got["dq"], got["dk"], got["dv"])
+    assert all(torch.equal(got[n], want[n]) for n in got)
+
+
+def test_two_streams_share_a_plan():
+    b = U.batch([900], [(0, 0, 900)], 4, 2, 128, seed=10)
+    tensors = [W.make_tensors(b, DEV), tuple(x.flip(0).contiguous() for x in W.make_tensors(b, DEV))]
+    want = [run(b, 60, 1, x) for x in tensors]
+    plan = B.ca_plan(b, window=60, sinks=1)
+    torch.cuda.synchronize()
+    got, streams = [], [torch.cuda.Stream() for _ in tensors]
+    for (q, k, v, d_o), st in zip(tensors, streams):
+        with torch.cuda.stream(st):
+            x = {"o": torch.empty_like(q), "lse": torch.empty(4, 900, device=DEV), "dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v)}
+            ws = B.alloc_workspace(plan, DEV)
+            B.ca_forward(plan, q, k, v, x["o"], x["lse"], ws)
+            B.ca_backward(plan, q, k, v, x["o"], d_o, x["lse"], x["dq"], x["dk"], x["dv"], ws)
+            got.append(x)
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert all(torch.equal(x[n], y[n]) for n in y)
+
+
+def test_windowed_shards_with_key_windows_merge_to_the_whole():
+    """Partial results of a windowed shard over two key windows of its context (positions counted from each), merged, and the gradients."""
+    n, cut, window = 700, 384, 250
+    whole = U.batch([n], [(0, 450, 250)], 4, 2, 64, seed=12)
+    q, k, v, d_o = W.make_tensors(whole, DEV)
+    # keys [0, cut) and [cut, n) as documents of their own, the shard a task on both; the first one's rows sit behind its keys
+    parts = W.custom([cut, n - cut], [(0, 450, 250), (1, 450 - cut, 250)], 4, 2, 64, seed=12)
+    parts.task_kv_len[0] = cut
+    plan = B.ca_plan(parts, window=window)
+    ws = B.alloc_workspace(plan, DEV)
+    qp, dop = torch.cat([q, q]), torch.cat([d_o, d_o])
+    op, lp = torch.empty_like(qp), torch.empty(4, 500, device=DEV)
+    o, lse = torch.empty_like(q), torch.empty(4, 250, device=DEV)
+    rows = torch.arange(500, dtype=torch.int32, device=DEV).view(2, 250)
+    B.ca_forward(plan, qp, k, v, op, lp, ws)
+    assert torch.isinf(lp[:, 249]).all()  # the last row's window begins behind the first part's keys
+    B.ca_merge_partials(rows, op, lp, o, lse, op, lp)
+    dqp, dq, dk, dv = torch.empty_like(qp), torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    B.ca_backward(plan, qp, k, v, op, dop, lp, dqp, dk, dv, ws)
+    B.ca_sum_partial_dq(rows, dqp, dq)
+    want, far = U.reference(whole, window, 0, q, k, v, d_o, o)
+    # (a part's O, and its dQ, are rounded to bf16 once more than the whole's: the bounds count that rounding twice)
+    U.check({"o": o, "dq": dq, "dk": dk, "dv": dv}, want, {x: 2 * y for x, y in far.items()}, ("o", "dq", "dk", "dv"))
 
 
 def test_kernel_times_are_read():
