@@ -101,7 +101,8 @@ int ca_plan(const ca_batch_desc *desc, ca_plan_t **out);
  * window >= 1 counts the row's own position (1: the row itself alone, and the sinks); sinks >= 0.  Everything that takes a plan takes
  * this one too: ca_forward and ca_backward run the windowed kernels, with the workspaces of ca_plan_workspace_bytes (which
  * here includes the partial results of tiles with sinks; the forward needs none).  A row that sees nothing (its task's kv_len ends
- * before its window and there are no sinks) gets O = 0 and LSE = -inf, dQ = 0, and adds nothing to dK and dV.  A window that hides
+ * before its window and there are no sinks) gets O = 0 and LSE = -inf, dQ = 0, and adds nothing to dK and dV.  Keys and values that no
+ * row of their document sees may hold anything, and their dK and dV are 0.  q, k, v, o and their gradients are 16-byte aligned.  A window that hides
  * nothing from any row gives the plan of ca_plan.  Results are bit-reproducible from run to run; the tiles of keys with sinks
  * are summed in pieces whose number depends on the batch.
  * With ca_merge_partials (shards with a sub-range of their context) window and sinks count within the "document" that the sub-range is.
@@ -241,7 +242,7 @@ typedef struct {
 } ca_cache_batch;
 
 /*
- * ca_cache_append: quantises the rows of k and v (device bf16 [total_rows][n_kv_heads][head_dim]) into the pages of their sequences.
+ * ca_cache_append: quantises the rows of k and v (device bf16 [total_rows][n_kv_heads][head_dim], 16-byte aligned) into the pages of their sequences.
  * The scale of a (page, head) becomes the smallest power of two, at least 2^-126, that is no less than (largest finite magnitude of
  * the new tokens) / 448 and, unless the page's token 0 is among the new ones (what the page held before is forgotten then), no less
  * than the scale it has.  New codes are value / scale to the nearest, ties to even (Inf and NaN become NaN); where the scale has grown the
@@ -254,11 +255,11 @@ int ca_cache_append(const ca_cache *cache, const ca_cache_batch *batch, const vo
 /*
  * ca_cache_attend: O = softmax(softmax_scale Q K^T) V over the cached tokens of each row's sequence: the row at position p sees the
  * tokens j <= p (itself among them: append first), with a window (>= 1; 0: none) only those with p - j < window or j < sinks.
- * q, o: device bf16 [total_rows][n_q_heads][head_dim]; lse: device fp32 [n_q_heads][total_rows], or NULL.  softmax_scale <= 0 selects
+ * q, o: device bf16 [total_rows][n_q_heads][head_dim], 16-byte aligned; lse: device fp32 [n_q_heads][total_rows], or NULL.  softmax_scale <= 0 selects
  * 1/sqrt(head_dim).  A row that sees nothing gets O = 0 and LSE = -inf.  Tokens that no row of a tile of rows sees may hold anything
  * (pages that have left every window may be freed and their table entries set to -1); tokens that only some rows see are finite.
  * ws: device workspace of ca_cache_attend_workspace_bytes, 256-byte aligned, written; calls that may overlap in time need one each.
- * Two launches on hip_stream; allocates nothing, never synchronises, bit-reproducible.  How the work is split, and with it the last bits of
+ * One launch on hip_stream, or two where the table is more than 16 pages wide; allocates nothing, never synchronises, bit-reproducible.  How the work is split, and with it the last bits of
  * a row's result, depends on the whole batch.
  */
 int ca_cache_attend(const ca_cache *cache, const ca_cache_batch *batch, int32_t n_q_heads, float softmax_scale, int64_t window,

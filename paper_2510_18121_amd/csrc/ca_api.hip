@@ -5,6 +5,7 @@
 #include <mutex>
 #include <new>
 #include <sstream>
+#include <initializer_list>
 #include <type_traits>
 
 #include "ca_internal.h"
@@ -78,6 +79,16 @@ static void free_device(ca_plan_t *p) {
   p->d_slot_lo = p->d_slot_src = nullptr, p->d_window_units = nullptr;
   if (cur >= 0 && cur != p->device) (void)hipSetDevice(cur);
   p->device = -1;
+}
+
+// of the tensors of a windowed plan, which come into LDS 16 bytes at a time
+static bool aligned16(std::initializer_list<const void *> tensors) {
+  for (const void *x : tensors)
+    if (reinterpret_cast<uintptr_t>(x) % 16 != 0) {
+      set_error("a tensor is not 16-byte aligned");
+      return false;
+    }
+  return true;
 }
 
 static int check_call(const ca_plan_t *p, void *ws, size_t ws_bytes, size_t need) {
@@ -274,6 +285,7 @@ int ca_forward(const ca_plan_t *p, const void *q, const void *k, const void *v, 
     set_error("k or v is null");
     return CA_ERR_INVALID_ARG;
   }
+  if (p->window > 0 && !aligned16({q, k, v, o})) return CA_ERR_INVALID_ARG;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   ca_plan_t *mp = const_cast<ca_plan_t *>(p);  // timing state only
   if (p->profile) (void)hipEventRecord(static_cast<hipEvent_t>(mp->ev[0]), st);
@@ -304,6 +316,7 @@ int ca_backward(const ca_plan_t *p, const void *q, const void *k, const void *v,
     set_error("k, v, dk or dv is null");
     return CA_ERR_INVALID_ARG;
   }
+  if (p->window > 0 && !aligned16({q, k, v, o, d_o, dq, dk, dv})) return CA_ERR_INVALID_ARG;
   ca_plan_t *mp = const_cast<ca_plan_t *>(p);  // timing state only
   const ca_plan_t *const use = p->within_static && ws_bytes < p->ws_bwd_split ? p->within_static.get() : p;
   const bool split = use->ws_bwd_split > use->ws_bwd && ws_bytes >= use->ws_bwd_split;

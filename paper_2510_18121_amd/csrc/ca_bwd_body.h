@@ -63,9 +63,11 @@ __device__ __forceinline__ void dq_workgroup(const FwdUnit &u, const int half, c
     dl[rg] = delta_slot[int64_t(head) * padded + slot + 16 * rg];
   }
   const int wmax = wave_max(max(pos[0], pos[1])), wmin = wave_min(min(pos[0], pos[1]));
-  const int lo_min = WINDOW ? wave_min(min(lo[0], lo[1])) : 0, lo_max = WINDOW ? wave_max(max(lo[0], lo[1])) : 0;
+  int lo_min = WINDOW ? wave_min(min(lo[0], lo[1])) : 0;
+  if (WINDOW && lo_min > wmax) lo_min = INT_MAX;  // (all windows are empty)
+  const int lo_max = WINDOW ? wave_max(max(lo[0], lo[1])) : 0;
   // tiles some row of the workgroup sees (positions are sorted; at least one, which then is masked)
-  const int key_lo = WINDOW ? u.key0 : 0, n_sink = WINDOW ? min((sinks + FWD_BN - 1) / FWD_BN, key_lo / FWD_BN) : 0;
+  const int key_lo = WINDOW ? u.key0 : 0, first_key = WINDOW ? -1 - u.part : 0, n_sink = WINDOW ? min((sinks + FWD_BN - 1) / FWD_BN, key_lo / FWD_BN) : 0;
   auto key_of = [&](int tile) __attribute__((always_inline)) {  // the first key of a tile
     return tile < n_sink ? FWD_BN * tile : key_lo + FWD_BN * (tile - n_sink);
   };
@@ -88,10 +90,10 @@ __device__ __forceinline__ void dq_workgroup(const FwdUnit &u, const int half, c
   const char *vg = reinterpret_cast<const char *>(V + (size_t(u.kv_row0) * Hkv + hk) * D);
   const size_t tile_bytes = size_t(FWD_BN) * kv_row_bytes;
   auto issue_kv = [&](int tile) __attribute__((always_inline)) {
-    const bool last = tile >= last_tile;
+    const bool last = tile >= last_tile, edge = last || (WINDOW && (tile == n_sink || tile == n_sink - 1));  // (see the forward)
     const size_t at = WINDOW ? size_t(key_of(last ? last_tile : tile)) * kv_row_bytes : size_t(last ? last_tile : tile) * tile_bytes;
     const uint32_t dst = lds0 + uint32_t((tile % NST) * S::STAGE + 1024 * wave);
-    if (!last) {
+    if (!edge) {
 #pragma unroll
       for (int n = 0; n < NLD; ++n) {
         load_lds16_sbase(kg + at + n * W * RPI * kv_row_bytes, ld_off, dst + S::K_OFF + 1024 * W * n);
@@ -100,7 +102,10 @@ __device__ __forceinline__ void dq_workgroup(const FwdUnit &u, const int half, c
     } else {
 #pragma unroll
       for (int n = 0; n < NLD; ++n) {
-        const uint32_t off = uint32_t(min(ld_row0 + W * RPI * n, last_key_in_tile)) * kv_row_bytes + ld_cbytes;
+        int row = ld_row0 + W * RPI * n;
+        if (WINDOW) row = seen_row(last ? last_key_in_tile : FWD_BN - 1, key_of(last ? last_tile : tile), first_key, sinks, row);
+        else row = min(row, last_key_in_tile);
+        const uint32_t off = uint32_t(row) * kv_row_bytes + ld_cbytes;
         load_lds16_sbase(kg + at, off, dst + S::K_OFF + 1024 * W * n);
         load_lds16_sbase(vg + at, off, dst + S::V_OFF + 1024 * W * n);
       }
@@ -513,7 +518,9 @@ __device__ __forceinline__ void dkv_workgroup(const int me /* index of the first
 #pragma unroll
           for (int i = 8 * b / ND; i < 8 * (b + 1) / ND; ++i) {
             const int e = 2 * (i & 1), rt = (i >> 1) & 1, kg = i >> 2;
-            dw[kg][2 * rt + e / 2] = pack_bf16(sa[rt][kg][e] * pa[rt][kg][e], sa[rt][kg][e + 1] * pa[rt][kg][e + 1]);
+            // (values of keys that nobody sees may be anything: 0 times it is 0)
+            auto times = [&](float x, float y) { return WINDOW && MASK && x == 0.f ? 0.f : x * y; };
+            dw[kg][2 * rt + e / 2] = pack_bf16(times(sa[rt][kg][e], pa[rt][kg][e]), times(sa[rt][kg][e + 1], pa[rt][kg][e + 1]));
           }
           next();
         }

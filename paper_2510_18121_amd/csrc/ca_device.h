@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <climits>
 #include <cstdint>
 
 namespace ca {
@@ -305,6 +306,13 @@ __device__ __forceinline__ void combine_parts(const float *src, size_t src_strid
   if (dst)
     *reinterpret_cast<u32x4 *>(dst + ocol) = u32x4{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
                                                    pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv)};
+}
+
+// Of a tile of keys from key0 on, of which rows up to `upto` are there: the row to fetch in place of `row`, which some row of a windowed
+// unit sees, where any is (see the forward): up to `upto`, and of no key in [sinks, from), `from` being the first of the unit's windows.
+__device__ __forceinline__ int seen_row(int upto, int key0, int from, int sinks, int row) {
+  const int r = min(row, upto), begin = from - key0, sink_end = sinks - key0;
+  return r < sink_end || r >= begin ? r : begin <= upto ? begin : max(0, sink_end - 1);
 }
 
 }  // namespace ca

@@ -89,7 +89,7 @@ __device__ __forceinline__ void fwd_workgroup(const FwdUnit *__restrict__ units,
     return u.slot0 + ((pair0 + (rg >> 1)) >> hp_lg) * 32 + 16 * (rg & 1) + li;
   };
   // WINDOW: tiles 0 .. n_sink - 1 are the document's first ones, the others begin at key key_lo (a multiple of FWD_BN)
-  const int key_lo = WINDOW ? u.key0 : 0, pos_base = WINDOW ? 0 : u.key0;
+  const int key_lo = WINDOW ? u.key0 : 0, first_key = WINDOW ? -1 - u.part : 0, pos_base = WINDOW ? 0 : u.key0;
   const int n_sink = WINDOW ? min((sinks + FWD_BN - 1) / FWD_BN, key_lo / FWD_BN) : 0;
   auto key_of = [&](int tile) __attribute__((always_inline)) {  // the first key of a tile
     return !WINDOW ? tile * FWD_BN : tile < n_sink ? FWD_BN * tile : key_lo + FWD_BN * (tile - n_sink);
@@ -115,11 +115,12 @@ __device__ __forceinline__ void fwd_workgroup(const FwdUnit *__restrict__ units,
     const int lane = lane_id_here(), ld_row0 = RPI * wave + lane / CH;
     ld_off = uint32_t(ld_row0) * kv_row_bytes + uint32_t((lane % CH) ^ tile_sw<D>(ld_row0)) * 16;
   }
-  // tile j into its stage; rows beyond the last key are fetched as the last key, tiles beyond the last as the last
+  // tile j into its stage; rows beyond the last key are fetched as the last key, tiles beyond the last as the last.  WINDOW: keys that no
+  // row of the unit sees are fetched as one that some row does, so that nothing non-finite comes in with them (0 times it is not 0).
   auto issue_kv = [&](int tile) __attribute__((always_inline)) {
     const size_t at = WINDOW ? size_t(key_of(min(tile, last_tile))) * kv_row_bytes : size_t(min(tile, last_tile)) * tile_bytes;
     const uint32_t dst = lds0 + uint32_t((tile % NST) * S::STAGE + 1024 * wave);
-    if (tile < last_tile) {
+    if (tile < last_tile && (!WINDOW || (tile != n_sink && tile != n_sink - 1))) {
 #pragma unroll
       for (int n = 0; n < NLD; ++n) {
         load_lds16_sbase(kg + at + n * W * RPI * kv_row_bytes, ld_off, dst + S::K_OFF + 1024 * W * n);
@@ -130,7 +131,10 @@ __device__ __forceinline__ void fwd_workgroup(const FwdUnit *__restrict__ units,
       const uint32_t cbytes = uint32_t((lane % CH) ^ tile_sw<D>(ld_row0)) * 16;
 #pragma unroll
       for (int n = 0; n < NLD; ++n) {
-        const uint32_t off = uint32_t(min(ld_row0 + W * RPI * n, last_key_in_tile)) * kv_row_bytes + cbytes;
+        int row = ld_row0 + W * RPI * n;
+        if (WINDOW) row = seen_row(min(tile, last_tile) == last_tile ? last_key_in_tile : FWD_BN - 1, key_of(min(tile, last_tile)), first_key, sinks, row);
+        else row = min(row, last_key_in_tile);
+        const uint32_t off = uint32_t(row) * kv_row_bytes + cbytes;
         load_lds16_sbase(kg + at, off, dst + S::K_OFF + 1024 * W * n);
         load_lds16_sbase(vg + at, off, dst + S::V_OFF + 1024 * W * n);
       }
@@ -156,7 +160,9 @@ __device__ __forceinline__ void fwd_workgroup(const FwdUnit *__restrict__ units,
   if (WINDOW) {
     const int lane = lane_id_here();
     const int lo = slot_lo[u.slot0 + ((lane < 32 ? pair0 & ~1 : pair0 | 1) >> hp_lg) * 32 + (lane & 31)];
-    lo_min = __builtin_amdgcn_readfirstlane(wave_min(lo)), lo_max = __builtin_amdgcn_readfirstlane(wave_max(lo));
+    lo_min = __builtin_amdgcn_readfirstlane(wave_min(lo));
+    if (lo_min > wmax64) lo_min = INT_MAX;  // (all windows are empty)
+    lo_max = __builtin_amdgcn_readfirstlane(wave_max(lo));
   }
   // WINDOW: some of the 64 rows may see some of the n keys from k0 on; all of them see all of those
   auto seen = [&](int k0, int n) __attribute__((always_inline)) { return k0 <= wmax64 && (k0 + n > lo_min || k0 < sinks); };

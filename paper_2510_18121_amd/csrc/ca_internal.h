@@ -20,8 +20,9 @@ constexpr int BWD_BQ = 64;   // query rows per backward inner step
 
 // A windowed plan (attention with a sliding window and sinks): a row at document position p sees the keys j <= min(p, kv_len - 1)
 // with j > p - window or j < sinks.  slot_pos holds the last of them, slot_lo where the row's window begins (one behind slot_pos
-// where it is empty); key0 of a forward unit is where the unit's window tiles begin, positions and n_keys are absolute.  All units
-// are head-packed (rows of few positions and many heads waste least on the window's edges), and slots are padded wherever windows no longer overlap.
+// where it is empty); key0 of a forward unit is where the unit's window tiles begin, positions and n_keys are absolute, and `part` is
+// -1 - (the first key that a window of the unit's rows holds; n_keys where none holds any).  All units
+// are head-packed (rows of few positions and many heads waste least on the window's edges), and slots are padded wherever a key lies between windows.
 
 // One workgroup of the forward / dQ kernels, or two (halves; always in the joint backward launch): 8 row groups of 32 slots, one or
 // two to a wave.  A full tile of a document is 256 slots of one query head (hp = 1).  The slots a document has left over

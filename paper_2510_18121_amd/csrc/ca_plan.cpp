@@ -1060,7 +1060,11 @@ int64_t ca_plan_fwd_units(const ca_plan_t *p, int32_t *units) {
 
 int64_t ca_plan_window_units(const ca_plan_t *p, int32_t kind, int32_t *out) {
   if (!p || p->window == 0) return 0;
-  if (kind == 0) return leading_fields(p->fwd_units, out, sizeof(ca::FwdUnit) / 4);
+  if (kind == 0) {
+    const int64_t n = leading_fields(p->fwd_units, out, sizeof(ca::FwdUnit) / 4);
+    for (int64_t i = 0; i < n && out; ++i) out[8 * i + 6] = -1;
+    return n;
+  }
   if (kind == 1) return leading_fields(p->window_units, out, sizeof(ca::WindowUnit) / 4);
   if (kind != 2) return 0;
   if (out) std::copy(p->slot_lo.begin(), p->slot_lo.end(), out);

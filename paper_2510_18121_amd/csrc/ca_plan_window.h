@@ -50,9 +50,10 @@ inline bool schedule_window(ca_plan_t *p) {
     if (!std::is_sorted(rows.begin(), rows.end(), before)) std::stable_sort(rows.begin(), rows.end(), before);
     const size_t s0 = p->slot_row.size();
     const int32_t kv_row0 = int32_t(p->doc_kv_start[dd]);
-    // runs of rows whose windows overlap, each padded: a unit does not span keys between windows that nobody sees
+    // runs of rows whose windows leave no key between them out, each padded: what a unit's window tiles hold from its first window on is
+    // seen by somebody
     for (size_t a = 0, b; a < rows.size(); a = b) {
-      for (b = a + 1; b < rows.size() && rows[b].lo <= rows[b - 1].hi + FWD_BN; ++b) {
+      for (b = a + 1; b < rows.size() && rows[b].lo <= rows[b - 1].hi + 1; ++b) {
       }
       const size_t n = size_t(up(int64_t(b - a), align)), at = p->slot_row.size();
       if (at + n >= size_t(INT32_MAX) - SLOT_ALIGN) return false;
@@ -68,7 +69,7 @@ inline bool schedule_window(ca_plan_t *p) {
         const int32_t n_keys = rows[e - 1].hi + 1, key0 = std::min(lo, n_keys - 1) / FWD_BN * FWD_BN;
         const int32_t n_sink = std::min((p->sinks + FWD_BN - 1) / FWD_BN, key0 / FWD_BN);
         ftiles.push_back({n_sink + (n_keys - key0 + FWD_BN - 1) / FWD_BN,
-                          {int32_t(at + i - a), kv_row0, n_keys, 0, int32_t(hp), key0, -1, int32_t(e - i)}});
+                          {int32_t(at + i - a), kv_row0, n_keys, 0, int32_t(hp), key0, -1 - std::min(lo, n_keys), int32_t(e - i)}});
       }
     }
     // backward tiles: every resident key of the document (those that nobody sees get zeros)

@@ -253,3 +253,56 @@ def test_kernel_times_are_read():
     B.ca_backward(plan, q, k, v, got["o"], d_o, got["lse"], got["dq"], got["dk"], got["dv"], ws)
     assert all(t > 0 for t in plan.profile_read().values())
     assert all(torch.equal(got[n], want[n]) for n in want)
+
+
+@pytest.mark.parametrize("heads,d", [((4, 2), 64), ((4, 1), 128), ((2, 2), 128)])
+@pytest.mark.parametrize("window,sinks", [(37, 0), (37, 5), (100, 70), (1, 0), (5, 129)])
+def test_keys_that_nobody_sees_may_hold_anything(window, sinks, heads, d):
+    """NaN or Inf in K and V before, between and behind the windows: every result as with finite values there, zero for those keys.  Task 3's
+    keys end before its rows' windows, document 2 is seen by nobody without sinks."""
+    b = U.batch([700, 300, 200], [(0, 150, 40), (0, 190 + 2 * window, 70), (0, 650, 1), (0, 600, 3), (1, 10, 64), (2, 150, 30)], *heads, d,
+                {3: 300, 5: 20}, seed=4)
+    q, k, v, d_o = W.make_tensors(b, DEV)
+    see = U.visible(b, window, sinks)
+    unseen = torch.from_numpy(~see.any(0)).to(DEV)
+    assert unseen.sum() > 300
+    want = run(b, window, sinks, (q, k, v, d_o))
+    check(b, window, sinks, want, (q, k, v, d_o))
+    for value in (float("nan"), float("inf"), -float("inf")):
+        for both in ("k", "v", "kv"):
+            kk, vv = k.clone(), v.clone()
+            if "k" in both:
+                kk[unseen] = value
+            if "v" in both:
+                vv[unseen] = value
+            got = run(b, window, sinks, (q, kk, vv, d_o))
+            for n, x in want.items():
+                assert torch.equal(got[n], x), (n, value, both)
+    for n in ("dk", "dv"):
+        assert not want[n][unseen].any()
+
+
+def test_tensors_out_of_line_are_refused():
+    b = U.batch([300], [(0, 0, 300)], 2, 1, 64)
+    tensors = W.make_tensors(b, DEV)
+    plan = B.ca_plan(b, window=20)
+    q, k, v, d_o = tensors
+    o, lse = torch.zeros_like(q), torch.zeros(2, 300, device=DEV)
+    ws = torch.empty(plan.workspace_bytes()[1], dtype=torch.uint8, device=DEV)
+    B.ca_forward(plan, q, k, v, o, lse, ws)
+
+    def shifted(x):
+        return torch.cat([x.new_zeros(1), x.flatten()])[1:].view(x.shape)
+
+    for i in range(4):
+        args = [q, k, v, o]
+        args[i] = shifted(args[i])
+        with pytest.raises(B.CaError) as e:
+            B.ca_forward(plan, *args, lse, ws)
+        assert e.value.code == B.CA_ERR_INVALID_ARG
+    for i in range(8):
+        args = [q, k, v, o, d_o, torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)]
+        args[i] = shifted(args[i])
+        with pytest.raises(B.CaError) as e:
+            B.ca_backward(plan, *args[:5], lse, *args[5:], ws)
+        assert e.value.code == B.CA_ERR_INVALID_ARG

@@ -134,3 +134,21 @@ def test_positions_far_beyond_the_keys():
     plan = B.ca_plan_host(b, window=1000, sinks=3)
     _, _, lo = plan.window_units()
     assert set(lo.tolist()) == {100}
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (5, 0), (30, 7), (30, 100)])
+def test_no_unit_spans_keys_between_its_windows_that_nobody_sees(window, sinks):
+    """From the first key of its windows on, a unit's keys are all seen by some row of it: tasks a few positions apart, whose keys end early or not."""
+    for gap in (0, 1, 2, 40, 63, 64):
+        at = [200 + (10 + window - 1 + gap) * i for i in range(6)]
+        b = U.batch([900], [(0, p, 10) for p in at], 4, 1, 64, {2: at[2] - window + 2, 4: at[4] + 5})
+        plan = B.ca_plan_host(b, window=window, sinks=sinks)
+        fwd, _, lo = plan.window_units()
+        rows, hi = plan.rows()
+        for slot0, _, n_keys, _, hp, key0, _, n in fwd:
+            seen = np.zeros(n_keys + 1, bool)
+            for s in range(slot0, slot0 + n):
+                seen[lo[s]:hi[s] + 1] = True
+            first = np.flatnonzero(seen)
+            assert len(first) == 0 or (seen[first[0]:first[-1] + 1].all() and key0 == first[0] // 64 * 64)
+            assert len(first) == 0 or first[-1] == n_keys - 1 or not seen[n_keys - 1:].any()
