@@ -102,6 +102,8 @@ class Sequences:
 
     def leave_window(self, seq, window, sinks=0):
         """Gives back the pages that no later row of `seq` sees with that window and those sinks."""
+        if operator.index(window) < 1 or operator.index(sinks) < 0:
+            raise ValueError(f"window {window}, sinks {sinks}: at least 1, and not negative")
         pages = self.pages[seq]
         for i in range(-(-sinks // PAGE_TOKENS), min(max(0, self.lengths[seq] - window + 1) // PAGE_TOKENS, len(pages))):
             self._let_go(pages[i])

@@ -716,7 +716,8 @@ template <int D, int NR>
 __global__ __launch_bounds__(256) void ca_cache_combine_kernel(const AttendArgs a) {
   constexpr int R = 16 * NR, LANES = D / 4, AT_A_TIME = 64 / LANES, RW = NR == 8 ? 4 : 1;
   const int hk = blockIdx.x, worker = blockIdx.y;
-  const int4 head = a.heads[worker * a.hkv + hk];  // {parts, first row of the sequence, first row of the tile, last row of the tile}
+  int4 head = a.heads[worker * a.hkv + hk];  // {parts, first row of the sequence, first row of the tile, last row of the tile}
+  head.x = min(head.x, int(gridDim.y) - worker);  // (sequences that overlap, against their description, may have more units than are counted)
   const int G = a.G, lane = threadIdx.x & 63, r0 = RW * (4 * blockIdx.z + (threadIdx.x >> 6));
   if (head.x < 2 || head.z + r0 > head.w) return;
   const size_t stride = size_t(2 * a.hkv) * (R * (D + 2));
@@ -974,13 +975,15 @@ static int fail(int code, const std::string &msg) {
   set_error(msg);
   return code;
 }
+static bool aligned(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+constexpr int64_t MOST_GROUPS = (int64_t(1) << 24) - 1;  // workgroups of 256 threads of a launch, whose threads number less than 2^32
 static int check_cache(const ca_cache *c) {
   if (!c) return fail(CA_ERR_INVALID_ARG, "cache is null");
   if (c->head_dim != 64 && c->head_dim != 128) return fail(CA_ERR_UNSUPPORTED, "head_dim not supported (64 or 128)");
   if (c->n_pages < 0 || c->n_kv_heads < 1) return fail(CA_ERR_INVALID_ARG, "cache: n_pages must not be negative, n_kv_heads at least 1");
   if (c->n_kv_heads > 1024) return fail(CA_ERR_UNSUPPORTED, "cache: more than 1024 KV heads");
   if (c->n_pages > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return fail(CA_ERR_INVALID_ARG, "cache: k, v, k_scale or v_scale is null");
-  if ((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) % 16 != 0) return fail(CA_ERR_INVALID_ARG, "cache: k or v is not 16-byte aligned");
+  if (!aligned(c->k) || !aligned(c->v)) return fail(CA_ERR_INVALID_ARG, "cache: k or v is not 16-byte aligned");
   return CA_OK;
 }
 static int check_batch(const ca_cache_batch *b) {
@@ -1064,6 +1067,7 @@ int ca_cache_attend(const ca_cache *c, const ca_cache_batch *b, int32_t n_q_head
   if (window < 0 || sinks < 0) return fail(CA_ERR_INVALID_ARG, "negative window or sinks");
   if (b->n_seqs == 0 || b->total_rows == 0) return CA_OK;
   if (!q || !o) return fail(CA_ERR_INVALID_ARG, "q or o is null");
+  if (!aligned(q) || !aligned(o)) return fail(CA_ERR_INVALID_ARG, "q or o is not 16-byte aligned");
   const size_t need = attend_bytes(c);
   if (!ws || ws_bytes < need || reinterpret_cast<uintptr_t>(ws) % 256 != 0) {
     std::ostringstream os;
@@ -1096,12 +1100,13 @@ int ca_cache_append(const ca_cache *c, const ca_cache_batch *b, const void *k, c
   if (const int rc = check_batch(b); rc != CA_OK) return rc;
   if (b->n_seqs == 0 || b->total_rows == 0 || b->table_width == 0) return CA_OK;
   if (!k || !v) return fail(CA_ERR_INVALID_ARG, "k or v is null");
+  if (!aligned(k) || !aligned(v)) return fail(CA_ERR_INVALID_ARG, "k or v is not 16-byte aligned");
   const AppendArgs a = {seq_args(c, b), static_cast<uint8_t *>(c->k), static_cast<uint8_t *>(c->v), c->k_scale, c->v_scale,
                         static_cast<const bf16_t *>(k), static_cast<const bf16_t *>(v), c->n_kv_heads};
   // pages that n rows of a sequence can touch: at most (n - 1) / 64 + 2, and no more than n
   const int64_t touches = std::min<int64_t>(b->total_rows, b->total_rows / PAGE + 2 * int64_t(b->n_seqs));
   const int64_t groups = (touches * 2 * c->n_kv_heads + 3) / 4;
-  if (groups >= int64_t(1) << 31) return fail(CA_ERR_UNSUPPORTED, "batch: rows times KV heads too many");
+  if (groups > MOST_GROUPS) return fail(CA_ERR_UNSUPPORTED, "batch: rows times KV heads too many");
   const size_t smem = seq_table_bytes(b->n_seqs);
   auto kern = c->head_dim == 128 ? ca_cache_append_kernel<128> : ca_cache_append_kernel<64>;
   int device = 0;
@@ -1119,8 +1124,9 @@ int ca_cache_copy_pages(const ca_cache *c, const int32_t *src, const int32_t *ds
   if (n < 0) return fail(CA_ERR_INVALID_ARG, "negative number of pages");
   if (n == 0) return CA_OK;
   if (!src || !dst) return fail(CA_ERR_INVALID_ARG, "src or dst is null");
+  // (a workgroup per 16 KiB)
   const int64_t page_bytes = int64_t(c->n_kv_heads) * PAGE * c->head_dim, chunks = (page_bytes + COPY_BYTES - 1) / COPY_BYTES;
-  if (2 * chunks * n >= int64_t(1) << 31) return fail(CA_ERR_UNSUPPORTED, "too many pages");
+  if (n > MOST_GROUPS || 2 * chunks * n > MOST_GROUPS) return fail(CA_ERR_UNSUPPORTED, "too many pages");
   hipLaunchKernelGGL(ca_cache_copy_kernel, dim3(unsigned(2 * chunks * n)), dim3(256), 0, static_cast<hipStream_t>(hip_stream),
                      static_cast<uint8_t *>(c->k), static_cast<uint8_t *>(c->v), c->k_scale, c->v_scale, src, dst, c->n_pages, c->n_kv_heads,
                      int(page_bytes), int(chunks));

@@ -175,3 +175,32 @@ def test_calls_refuse_on_the_host():
         assert attend(b=b, q=None, o=None, ws=None) == B.CA_OK
         assert L.ca_cache_append(ref(CacheDesc, good), ref(B.CacheBatch, b), None, None, None) == B.CA_OK
     assert L.ca_cache_copy_pages(ref(CacheDesc, good), None, None, 0, None) == B.CA_OK
+
+
+def test_refusals_of_rows_out_of_line_and_of_more_work_than_a_launch_holds():
+    """Bytes that are read 16 at a time lie on multiples of 16; a launch has less than 2^24 workgroups."""
+    L, fake, arg, uns = B.lib(), 1 << 20, B.CA_ERR_INVALID_ARG, B.CA_ERR_UNSUPPORTED
+    cache = ctypes.byref(CacheDesc(4, 1024, 128, fake, fake, fake, fake))
+    small = ctypes.byref(CacheDesc(4, 1, 64, fake, fake, fake, fake))
+    batch = ctypes.byref(B.CacheBatch(2, 3, 4, fake, fake, fake))
+    large = ctypes.byref(B.CacheBatch(2, 3, 1 << 22, fake, fake, fake))
+    for off in (2, 8):
+        assert L.ca_cache_append(cache, batch, fake + off, fake, None) == L.ca_cache_append(cache, batch, fake, fake + off, None) == arg
+        for q, o in ((fake + off, fake), (fake, fake + off)):
+            assert L.ca_cache_attend(cache, batch, 1024, 0.0, 0, 0, q, o, None, fake, 1 << 40, None) == arg
+    assert L.ca_cache_append(cache, large, fake, fake, None) == uns
+    for n in (1 << 23, 1 << 40, (1 << 63) - 1):
+        assert L.ca_cache_copy_pages(small, fake, fake, n, None) == uns
+    assert L.ca_cache_copy_pages(cache, fake, fake, 1 << 14, None) == uns
+
+
+def test_a_window_that_is_none_is_refused():
+    s = Sequences(n_pages=4)
+    a = s.add()
+    s.extend([a], [200])
+    for window, sinks in ((0, 0), (-5, 0), (64, -1)):
+        with pytest.raises(ValueError):
+            s.leave_window(a, window, sinks)
+    with pytest.raises(TypeError):
+        s.leave_window(a, 64.0)
+    assert s.pages[a] == [0, 1, 2, 3]
