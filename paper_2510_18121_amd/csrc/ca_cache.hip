@@ -8,6 +8,17 @@
 //   O^T += V^T P^T: the probabilities of two tiles are the B operand as they stand, and the lane's A operand is 8 consecutive
 //   tokens of a V^T row.
 // e4m3 is exact in bf16; the scales go into the exponent's factor (K) and into the probabilities (V).
+//
+// O = softmax(scale Q K^T) V and LSE need the codes once, 2 D bytes per (token, KV head): reading them bounds single tokens, and
+// matrix products bound chunks.  Measured (kernel times, 8 KV heads of 128 unless noted):
+//   attend   64 sequences of about 4096 tokens, 32 heads      164 us, 5.4 TB/s (a large copy: 4.97 read and written)
+//            4 sequences of 130K tokens, 64 heads             184 us, 5.7 TB/s
+//            32 sequences, window 4096, 16/16 heads of 64      50 us, 5.3 TB/s
+//            one sequence of 901 tokens                      11.5 us (14 bytes per cycle and CU, 8 CUs)
+//   chunk    4 chunks of 500 rows behind 8192 tokens          225 us, 0.92 PFLOP/s executed
+//   combine  of these                                         4 to 5 us, 14 us
+//   append   128 tokens; 16 prompts of 2048                   6.6 us; 31 us, 4.4 TB/s
+//   copy     4000 pages of 128 KiB                            215 us, 4.9 TB/s
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -239,6 +250,9 @@ struct AttendShape {
   static constexpr int MERGE = (W * R * ROW + W * R * 2) * 4;
 };
 
+// Single tokens and the like: tiles of 16 NR rows.  A wave has pages of its own, every W-th of the worker's run: codes come to registers
+// in 16-byte runs, the next page's K while this one's scores are multiplied, its V behind this one's (a page further ahead: 167 -> 175 us on 64 sequences
+// of about 4096 tokens, 184 -> 197 on 4 of 130K).  No barrier before the waves' sums meet.
 template <int D, int NR, int W>
 __global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kernel(const AttendArgs a) {
   using S = AttendShape<D, NR, W>;
@@ -450,6 +464,9 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kerne
 // converted once per 128 rows, and all read its fragments from there.  The page after the next is on its way to registers, the
 // next one is written to the other stage while this one is multiplied; one barrier per page.  K's rows stand in the order of
 // the four tiles' rows, V^T's chunks of 8 keys in the order of its fragments, both swizzled as the other kernels' tiles are.
+// (4 chunks of 500 rows behind 8192 tokens, 32/8 heads of 128, the whole call: 412 us with 64 rows to a wave of the kernel above, 305 through
+// LDS, 258 with fragments fetched ahead and exponentials between MFMAs, 236 now.  MFMAs 38 % busy, vector instructions issue 46 %: conversions,
+// exponentials and packing beside them bound it.)  P is one bf16 operand here (its rounding is as large as O's own), not two as above.
 template <int D>
 struct ChunkSmem {
   static constexpr int V_OFF = PAGE * 2 * D, STAGE = 2 * PAGE * 2 * D;
@@ -711,7 +728,9 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
   if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
 }
 
-// Adds up the parts of the tiles that were cut, in their order: a wave takes RW rows, and two (four) parts of each at a time.
+// Adds up the parts of the tiles that were cut, in their order: a wave takes RW rows, and two (four) parts of each at a time.  4 to 5 us, of which
+// most is the way to the first load (14 us for chunks: 29 MB of parts); a worker adding them up in the first kernel would need counters that
+// somebody clears.
 template <int D, int NR>
 __global__ __launch_bounds__(256) void ca_cache_combine_kernel(const AttendArgs a) {
   constexpr int R = 16 * NR, LANES = D / 4, AT_A_TIME = 64 / LANES, RW = NR == 8 ? 4 : 1;
@@ -806,6 +825,8 @@ __device__ __forceinline__ float wave_top(uint32_t top) { return __builtin_bit_c
 // from the caches.  Where such a page's scale grows, all that it holds is rounded again, from old / new of the scales: exact but for codes
 // that leave the normal range.
 // K: D / 8 lanes per token, 8 columns each.  V: a lane has two columns; at head_dim 64 the wave's halves take tokens of their own.
+// (128 single tokens: 22 us with a workgroup per page, K and V one after the other; 8.6 with a wave each; 6.8 with the sequences in lanes or LDS.
+// 16 prompts of 2048 tokens: 47, 40.7 and 31 us.)
 template <int D>
 __global__ __launch_bounds__(256) void ca_cache_append_kernel(const AppendArgs a) {
   constexpr int LPT = D / 8, TPI = 64 / LPT, NI = PAGE / TPI;  // K: lanes per token, tokens per load, loads per page
@@ -944,7 +965,7 @@ __global__ __launch_bounds__(256) void ca_cache_append_kernel(const AppendArgs a
 }
 
 // ------------------------------------------------------------------------------------------------ copies
-// 16 KiB of a page's keys, then of its values, per workgroup.
+// 16 KiB of a page's keys, then of its values, per workgroup, all loads before the stores.  At the rate of a large copy; 16 pages take 3.4 us.
 constexpr int COPY_BYTES = 16384;
 __global__ __launch_bounds__(256) void ca_cache_copy_kernel(uint8_t *__restrict__ k, uint8_t *__restrict__ v, float *__restrict__ k_scale,
                                                             float *__restrict__ v_scale, const int32_t *__restrict__ src,
