@@ -1026,28 +1026,25 @@ static int launched(const char *what, hipError_t e) {
   return fail(CA_ERR_HIP, std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")");
 }
 
-// Waves of a worker, and workers per KV head: as many as are on the chip at a time (NR: 16-row groups of a tile; 8: chunks).
-template <int NR>
-constexpr int WAVES = NR == 1 ? 8 : 4;
-template <int NR>
+// Workers of W waves per KV head: as many as are on the chip at a time (NR: 16-row groups of a tile; 8: chunks).
+template <int NR, int W>
 static int n_workers(int hkv) {
-  return std::max(1, N_CU * (NR == 8 ? 2 : 1) / hkv);
+  return std::max(1, N_CU * (NR == 2 ? 4 : 8) / W / hkv);
 }
-template <int D, int NR>
+template <int D, int NR, int W>
 static size_t attend_bytes(int hkv) {
-  const size_t workers = size_t(n_workers<NR>(hkv));
+  const size_t workers = size_t(n_workers<NR, W>(hkv));
   return workers * hkv * sizeof(int4) + workers * 2 * hkv * (16 * NR * (D + 2)) * 4;
 }
-static size_t attend_bytes(const ca_cache *c) {
-  const int hkv = c->n_kv_heads;
-  return c->head_dim == 128 ? std::max({attend_bytes<128, 1>(hkv), attend_bytes<128, 2>(hkv), attend_bytes<128, 8>(hkv)})
-                            : std::max({attend_bytes<64, 1>(hkv), attend_bytes<64, 2>(hkv), attend_bytes<64, 8>(hkv)});
+template <int D>
+static size_t attend_bytes(int hkv) {
+  return std::max({attend_bytes<D, 1, 2>(hkv), attend_bytes<D, 2, 2>(hkv), attend_bytes<D, 8, 4>(hkv)});
 }
+static size_t attend_bytes(const ca_cache *c) { return c->head_dim == 128 ? attend_bytes<128>(c->n_kv_heads) : attend_bytes<64>(c->n_kv_heads); }
 
-template <int D, int NR>
+template <int D, int NR, int W>
 static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
-  constexpr int W = WAVES<NR>;
-  const int workers = n_workers<NR>(a.hkv);
+  const int workers = n_workers<NR, W>(a.hkv);
   a.by_workers = 1.0001f / float(workers);
   a.heads = static_cast<int4 *>(ws);
   a.parts = reinterpret_cast<float *>(a.heads + size_t(workers) * a.hkv);
@@ -1064,6 +1061,22 @@ static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
   // (no tile has more pages than the table is wide, and none of up to CUT pages is cut)
   if (a.s.width > CUT) hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(a.hkv), unsigned(workers), NR == 8 ? 8 : 4 * NR), dim3(256), 0, st, a);
   return launched("cache attention", hipSuccess);
+}
+
+// Rows per tile from the average sequence: up to 32 rows a page is converted by the wave that reads it; with more it is converted once
+// per 128 rows, through LDS.
+// Waves per worker.  With two or more tiles per CU pairs of waves (four workers per CU, two with 32 rows): while one worker looks its tile up or its waves'
+// sums meet, others read (200 sequences of 500 tokens, 8 KV heads of 128: 67 us with eight waves, 48 with four, 41 with two, 41 with one; 64 of 500: 27, 24, 19,
+// 25; 32 rows a tile, 200 of 500: 87 with four, 72 with two; contexts of thousands: level).  With fewer tiles a CU has one of its own, which its waves share: four
+// where contexts are short (32 sequences of 500: 17.3, 13.5, 15.8, 18.6; one of 901: 12.2, 11.6, 13.6, 20), eight otherwise (16 of 4000: 33, 36, 37, 38).  More
+// sequences than fit LDS four times leave pairs to themselves on a CU.
+template <int D>
+static int attend_by_rows(const AttendArgs &a, void *ws, hipStream_t st) {
+  const int64_t rows = int64_t(a.s.total) * a.G / a.s.n_seqs, tiles = int64_t(a.s.n_seqs) * a.hkv;
+  if (rows > 32) return launch_attend<D, 8, 4>(a, ws, st);
+  const bool pairs = tiles >= 2 * N_CU && 4 * (AttendShape<D, 1, 2>::MERGE + seq_table_bytes(a.s.n_seqs)) <= 160 * 1024;
+  if (rows > 16) return pairs ? launch_attend<D, 2, 2>(a, ws, st) : launch_attend<D, 2, 4>(a, ws, st);
+  return pairs ? launch_attend<D, 1, 2>(a, ws, st) : a.s.width <= 2 * CUT ? launch_attend<D, 1, 4>(a, ws, st) : launch_attend<D, 1, 8>(a, ws, st);
 }
 
 }  // namespace ca
@@ -1108,11 +1121,7 @@ int ca_cache_attend(const ca_cache *c, const ca_cache_batch *b, int32_t n_q_head
   a.sinks = window == 0 ? 0 : int(std::min<int64_t>(sinks, 1 << 30));
   a.c = (softmax_scale > 0.f ? softmax_scale : c->head_dim == 128 ? 0.08838834764831845f : 0.125f) * 1.4426950408889634f;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  // Rows per tile from the average sequence: up to 32 rows a page is converted by the wave that reads it; with more it is converted once
-  // per 128 rows, through LDS.
-  const int64_t rows = b->total_rows * g / b->n_seqs;
-  if (c->head_dim == 128) return rows <= 16 ? launch_attend<128, 1>(a, ws, st) : rows <= 32 ? launch_attend<128, 2>(a, ws, st) : launch_attend<128, 8>(a, ws, st);
-  return rows <= 16 ? launch_attend<64, 1>(a, ws, st) : rows <= 32 ? launch_attend<64, 2>(a, ws, st) : launch_attend<64, 8>(a, ws, st);
+  return c->head_dim == 128 ? attend_by_rows<128>(a, ws, st) : attend_by_rows<64>(a, ws, st);
 }
 
 int ca_cache_append(const ca_cache *c, const ca_cache_batch *b, const void *k, const void *v, void *hip_stream) {

@@ -162,6 +162,22 @@ def test_scales_far_from_one(rows):
     U.check(o, lse, want)
 
 
+@pytest.mark.parametrize("seqs,hq,hkv,d", [(70, 16, 8, 128), (70, 16, 8, 64), (520, 4, 1, 64), (1100, 1, 1, 128)])
+@pytest.mark.parametrize("rows", [1, 6, 20])
+@pytest.mark.parametrize("window,sinks", [(None, 0), (90, 5)])
+def test_more_tiles_than_the_chip_has_room_for(seqs, hq, hkv, d, rows, window, sinks):
+    """Two and more tiles per CU, of sequences from no token to thousands, most of them short; up to 1, 6 and 20 rows of each."""
+    rng = np.random.default_rng(seqs + rows)
+    lens = (rng.integers(0, 260, seqs)).tolist()
+    lens[3], lens[seqs - 2], lens[seqs // 2] = 5000, 2900, 0
+    n = [rows] * seqs if rows == 1 else rng.integers(rows - 1, rows + 1, seqs).tolist()
+    table, pages = U.layout(lens, seed=31)
+    c = filled(pages, hkv, d)
+    poison(c, lens, table)
+    q = queries(sum(n), hq, d)
+    U.check(*attend(c, q, n, lens, table, window, sinks), U.attend(c, q, n, lens, table, window, sinks))
+
+
 def test_as_many_sequences_as_there_may_be():
     n, lens = [1] * 4096, (np.arange(4096) % 3 + 1).tolist()
     table, pages = U.layout(lens, seed=22)
