@@ -152,6 +152,7 @@ struct AttendArgs {
   uint32_t by_g;  // 2^32 / G, rounded up: x / G is the high word of x * by_g for x < 2^32 / G (G > 1)
   float c;        // softmax_scale * log2(e)
   float by_workers;  // a little more than 1 / (workers per KV head)
+  int stream;        // codes pass the caches by
 
   __device__ __forceinline__ int token_of(int row) const { return G == 1 ? row : int(__umulhi(uint32_t(row), by_g)); }
 };
@@ -321,13 +322,27 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kerne
       u32x4 kr[4 * NH], vr[NB];
       auto load_k = [&](int i) __attribute__((always_inline)) {
         const uint8_t *const p = a.k + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
+        if (a.stream) {
+          asm volatile("" ::: "memory");  // (two branches, or the loads become one kind)
 #pragma unroll
-        for (int f = 0; f < 4 * NH; ++f) kr[f] = *reinterpret_cast<const u32x4 *>(p + k_lane + 4 * (f / NH) * D + 64 * (f % NH));
+          for (int f = 0; f < 4 * NH; ++f) kr[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + k_lane + 4 * (f / NH) * D + 64 * (f % NH)));
+          asm volatile("" ::: "memory");
+        } else {
+#pragma unroll
+          for (int f = 0; f < 4 * NH; ++f) kr[f] = *reinterpret_cast<const u32x4 *>(p + k_lane + 4 * (f / NH) * D + 64 * (f % NH));
+        }
       };
       auto load_v = [&](int i) __attribute__((always_inline)) {
         const uint8_t *const p = a.v + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
+        if (a.stream) {
+          asm volatile("" ::: "memory");
 #pragma unroll
-        for (int b = 0; b < NB; ++b) vr[b] = *reinterpret_cast<const u32x4 *>(p + v_lane + 16 * PAGE * b);
+          for (int b = 0; b < NB; ++b) vr[b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + v_lane + 16 * PAGE * b));
+          asm volatile("" ::: "memory");
+        } else {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) vr[b] = *reinterpret_cast<const u32x4 *>(p + v_lane + 16 * PAGE * b);
+        }
       };
       int cur = pop(), next;
       if (cur >= 0) load_k(cur), load_v(cur);
@@ -965,7 +980,8 @@ __global__ __launch_bounds__(256) void ca_cache_append_kernel(const AppendArgs a
 }
 
 // ------------------------------------------------------------------------------------------------ copies
-// 16 KiB of a page's keys, then of its values, per workgroup, all loads before the stores.  At the rate of a large copy; 16 pages take 3.4 us.
+// 16 KiB of a page's keys, then of its values, per workgroup, all loads before the stores, which pass the caches by (4000 pages of 128 KiB 202 -> 198 us,
+// 1400 pages 69 -> 55).  At the rate of a large copy; 16 pages take 3.4 us.
 constexpr int COPY_BYTES = 16384;
 __global__ __launch_bounds__(256) void ca_cache_copy_kernel(uint8_t *__restrict__ k, uint8_t *__restrict__ v, float *__restrict__ k_scale,
                                                             float *__restrict__ v_scale, const int32_t *__restrict__ src,
@@ -984,7 +1000,7 @@ __global__ __launch_bounds__(256) void ca_cache_copy_kernel(uint8_t *__restrict_
     if (256 * i + int(threadIdx.x) < n) r[i] = x[256 * i + threadIdx.x];
 #pragma unroll
   for (int i = 0; i < COPY_BYTES / 4096; ++i)
-    if (256 * i + int(threadIdx.x) < n) y[256 * i + threadIdx.x] = r[i];
+    if (256 * i + int(threadIdx.x) < n) __builtin_nontemporal_store(r[i], y + 256 * i + threadIdx.x);
   if (at == 0) {
     float *const scale = rest < chunks ? k_scale : v_scale;
     for (int h = threadIdx.x; h < hkv; h += 256) scale[size_t(to) * hkv + h] = scale[size_t(from) * hkv + h];
@@ -1120,6 +1136,11 @@ int ca_cache_attend(const ca_cache *c, const ca_cache_batch *b, int32_t n_q_head
   a.window = window == 0 ? 1 << 30 : int(std::min<int64_t>(window, 1 << 30));
   a.sinks = window == 0 ? 0 : int(std::min<int64_t>(sinks, 1 << 30));
   a.c = (softmax_scale > 0.f ? softmax_scale : c->head_dim == 128 ? 0.08838834764831845f : 0.125f) * 1.4426950408889634f;
+  // Codes that the last cache (256 MiB) does not hold until the next call pass it by: 64 sequences of about 4096 tokens, 8 KV heads of 128 (0.9 GB)
+  // 166 -> 150 us, 48 of 4096 (0.4 GB) 80 -> 76; those that it holds are read from there (36 of 4096, 0.3 GB: 57 against 60 us; 28: 42, 49).
+  // (As many as there may be: what the device's lengths say, the host does not know.)
+  const int64_t pages = std::min<int64_t>(int64_t(b->n_seqs) * std::min<int64_t>(b->table_width, (int64_t(a.window) + a.sinks) / PAGE + 3), c->n_pages);
+  a.stream = pages * c->n_kv_heads * (2 * PAGE * c->head_dim) > int64_t(384) << 20;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   return c->head_dim == 128 ? attend_by_rows<128>(a, ws, st) : attend_by_rows<64>(a, ws, st);
 }

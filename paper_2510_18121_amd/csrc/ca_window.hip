@@ -31,7 +31,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_fwd_window_kernel(
 
 // -Delta = -<dO, O> and log2(e) * LSE of 64 slots and a head, by (head, slot) for dQ and in the order of dK/dV's tiles; rows of padding get
 // probabilities of 0.  D / 8 lanes per row; the statistics leave through LDS as whole lines.  Bound by memory: 220 us, 5.1 TB/s, on the 64K tokens
-// above (a workgroup per 64 slots and all heads, with the statistics stored as they came: 257 us).
+// above (a workgroup per 64 slots and all heads, with the statistics stored as they came: 257 us).  O, which nothing else of the pass
+// reads, passes the caches by (210 -> 200 us).
 // O is the caller's, in bf16 (with shards of a merged row it is the whole row's), and Delta is what <dO, O> is with that: off by up to 2^-9 |dO| |O|.
 // Where a row sees a few keys alone that is the largest of the roundings (relative error of dQ and dK: 0.0025 from windows of 16 keys
 // on, 0.0027 with 6, 0.0036 with 2; 0.0017 is what rounding them to bf16 costs).
@@ -50,7 +51,7 @@ __global__ __launch_bounds__(256) void ca_window_prep_kernel(const int32_t *__re
   for (int n = 0; n < N; ++n) {
     const int row = max(0, rows[i0 + ROWS * n]);
     const size_t off = (size_t(row) * Hq + h) * D + 8 * c;
-    a[n] = *reinterpret_cast<const bf16x8 *>(O + off), b[n] = *reinterpret_cast<const bf16x8 *>(dO + off);
+    a[n] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8 *>(O + off)), b[n] = *reinterpret_cast<const bf16x8 *>(dO + off);
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) {

@@ -178,6 +178,30 @@ def test_more_tiles_than_the_chip_has_room_for(seqs, hq, hkv, d, rows, window, s
     U.check(*attend(c, q, n, lens, table, window, sinks), U.attend(c, q, n, lens, table, window, sinks))
 
 
+@pytest.mark.parametrize("d,pages", [(128, 3200), (64, 6300)])
+@pytest.mark.parametrize("rows", [[1] * 4, [1] * 70, [5] * 70])
+def test_a_large_pool_gives_the_bits_of_a_small_one(d, pages, rows):
+    """Of a pool of 400 MiB codes pass the caches by; the same tokens in a small one do not."""
+    rng = np.random.default_rng(32)
+    lens = rng.integers(1, 1500, len(rows)).tolist()
+    lens[1] = 100000 if len(rows) == 4 else 6000
+    table, n = U.layout(lens, seed=33)
+    small, large = filled(n, 8, d), KVCache.empty(pages, 8, d, DEV)
+    assert n * 8 * 128 * d <= 256 << 20 and large.n_pages * 8 * 128 * d > 384 << 20 and len(lens) * table.shape[1] >= large.n_pages
+    ids = torch.from_numpy(rng.permutation(large.n_pages)[:n]).to(DEV)
+    for x, y in ((small.k, large.k), (small.v, large.v)):
+        y.view(torch.uint8).fill_(0x7F)
+        y.view(torch.uint8)[ids] = x.view(torch.uint8)
+    for x, y in ((small.k_scale, large.k_scale), (small.v_scale, large.v_scale)):
+        y.fill_(float("nan"))
+        y[ids] = x
+    moved = np.where(table >= 0, ids.cpu().numpy()[np.maximum(table, 0)], -1).astype(np.int32)
+    q = queries(sum(rows), 32, d)
+    for window, sinks in ((None, 0), (90000, 3)):
+        for a, b in zip(attend(small, q, rows, lens, table, window, sinks), attend(large, q, rows, lens, moved, window, sinks)):
+            assert torch.equal(a, b)
+
+
 def test_as_many_sequences_as_there_may_be():
     n, lens = [1] * 4096, (np.arange(4096) % 3 + 1).tolist()
     table, pages = U.layout(lens, seed=22)
