@@ -184,7 +184,7 @@ def test_a_large_pool_gives_the_bits_of_a_small_one(d, pages, rows):
     """Of a pool of 400 MiB codes pass the caches by; the same tokens in a small one do not."""
     rng = np.random.default_rng(32)
     lens = rng.integers(1, 1500, len(rows)).tolist()
-    lens[1] = 100000 if len(rows) == 4 else 6000
+    lens[1] = 101000 if len(rows) == 4 else 6000
     table, n = U.layout(lens, seed=33)
     small, large = filled(n, 8, d), KVCache.empty(pages, 8, d, DEV)
     assert n * 8 * 128 * d <= 256 << 20 and large.n_pages * 8 * 128 * d > 384 << 20 and len(lens) * table.shape[1] >= large.n_pages
