@@ -11,14 +11,14 @@
 //
 // O = softmax(scale Q K^T) V and LSE need the codes once, 2 D bytes per (token, KV head): reading them bounds single tokens, and
 // matrix products bound chunks.  Measured (kernel times, 8 KV heads of 128 unless noted):
-//   attend   64 sequences of about 4096 tokens, 32 heads      164 us, 5.4 TB/s (a large copy: 4.97 read and written)
-//            4 sequences of 130K tokens, 64 heads             184 us, 5.7 TB/s
-//            32 sequences, window 4096, 16/16 heads of 64      50 us, 5.3 TB/s
-//            one sequence of 901 tokens                      11.5 us (14 bytes per cycle and CU, 8 CUs)
-//   chunk    4 chunks of 500 rows behind 8192 tokens          225 us, 0.92 PFLOP/s executed
-//   combine  of these                                         4 to 5 us, 14 us
+//   attend   64 sequences of about 4096 tokens, 32 heads      144 us, 6.2 TB/s (a large copy: 4.97 read and written)
+//            4 sequences of 130K tokens, 64 heads             168 us, 6.3 TB/s
+//            32 sequences, window 4096, 16/16 heads of 64      47 us, 5.7 TB/s
+//            one sequence of 901 tokens                      11.3 us (14 bytes per cycle and CU, 8 CUs)
+//   chunk    4 chunks of 500 rows behind 8192 tokens          221 us, 0.94 PFLOP/s executed
+//   combine  of these                                         4 to 5 us, 13 us
 //   append   128 tokens; 16 prompts of 2048                   6.6 us; 31 us, 4.4 TB/s
-//   copy     4000 pages of 128 KiB                            215 us, 4.9 TB/s
+//   copy     4000 pages of 128 KiB                            209 us, 5.0 TB/s
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -252,8 +252,8 @@ struct AttendShape {
 };
 
 // Single tokens and the like: tiles of 16 NR rows.  A wave has pages of its own, every W-th of the worker's run: codes come to registers
-// in 16-byte runs, the next page's K while this one's scores are multiplied, its V behind this one's (a page further ahead: 167 -> 175 us on 64 sequences
-// of about 4096 tokens, 184 -> 197 on 4 of 130K).  No barrier before the waves' sums meet.
+// in 16-byte runs, the next page's K while this one's scores are multiplied, its V behind this one's (a page further ahead took 5 % longer on 64 sequences
+// of about 4096 tokens, 7 % on 4 of 130K).  No barrier before the waves' sums meet.
 template <int D, int NR, int W>
 __global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kernel(const AttendArgs a) {
   using S = AttendShape<D, NR, W>;
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kerne
 // next one is written to the other stage while this one is multiplied; one barrier per page.  K's rows stand in the order of
 // the four tiles' rows, V^T's chunks of 8 keys in the order of its fragments, both swizzled as the other kernels' tiles are.
 // (4 chunks of 500 rows behind 8192 tokens, 32/8 heads of 128, the whole call: 412 us with 64 rows to a wave of the kernel above, 305 through
-// LDS, 258 with fragments fetched ahead and exponentials between MFMAs, 236 now.  MFMAs 38 % busy, vector instructions issue 46 %: conversions,
+// LDS, 258 with fragments fetched ahead and exponentials between MFMAs, 232 now.  MFMAs 38 % busy, vector instructions issue 46 %: conversions,
 // exponentials and packing beside them bound it.)  P is one bf16 operand here (its rounding is as large as O's own), not two as above.
 template <int D>
 struct ChunkSmem {
@@ -744,11 +744,11 @@ __global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs
 }
 
 // Adds up the parts of the tiles that were cut, in their order: a wave takes RW rows, and two (four) parts of each at a time.  4 to 5 us, of which
-// most is the way to the first load (14 us for chunks: 29 MB of parts); a worker adding them up in the first kernel would need counters that
+// most is the way to the first load (13 us for chunks: 29 MB of parts; of those a wave takes two rows, one or four: +1 %); a worker adding them up in the first kernel would need counters that
 // somebody clears.
 template <int D, int NR>
 __global__ __launch_bounds__(256) void ca_cache_combine_kernel(const AttendArgs a) {
-  constexpr int R = 16 * NR, LANES = D / 4, AT_A_TIME = 64 / LANES, RW = NR == 8 ? 4 : 1;
+  constexpr int R = 16 * NR, LANES = D / 4, AT_A_TIME = 64 / LANES, RW = NR == 8 ? 2 : 1;
   const int hk = blockIdx.x, worker = blockIdx.y;
   int4 head = a.heads[worker * a.hkv + hk];  // {parts, first row of the sequence, first row of the tile, last row of the tile}
   head.x = min(head.x, int(gridDim.y) - worker);  // (sequences that overlap, against their description, may have more units than are counted)
@@ -1075,7 +1075,7 @@ static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
   if (e != hipSuccess) return launched("cache attention", e);
   hipLaunchKernelGGL(kern, dim3(unsigned(a.hkv), unsigned(workers)), dim3(64 * W), bytes + seq_table_bytes(a.s.n_seqs), st, a);
   // (no tile has more pages than the table is wide, and none of up to CUT pages is cut)
-  if (a.s.width > CUT) hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(a.hkv), unsigned(workers), NR == 8 ? 8 : 4 * NR), dim3(256), 0, st, a);
+  if (a.s.width > CUT) hipLaunchKernelGGL((ca_cache_combine_kernel<D, NR>), dim3(unsigned(a.hkv), unsigned(workers), NR == 8 ? 16 : 4 * NR), dim3(256), 0, st, a);
   return launched("cache attention", hipSuccess);
 }
 

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_fwd_window_kernel(
 }
 
 // -Delta = -<dO, O> and log2(e) * LSE of 64 slots and a head, by (head, slot) for dQ and in the order of dK/dV's tiles; rows of padding get
-// probabilities of 0.  D / 8 lanes per row; the statistics leave through LDS as whole lines.  Bound by memory: 220 us, 5.1 TB/s, on the 64K tokens
+// probabilities of 0.  D / 8 lanes per row; the statistics leave through LDS as whole lines.  Bound by memory: 203 us, 5.4 TB/s, on the 64K tokens
 // above (a workgroup per 64 slots and all heads, with the statistics stored as they came: 257 us).  O, which nothing else of the pass
 // reads, passes the caches by (210 -> 200 us).
 // O is the caller's, in bf16 (with shards of a merged row it is the whole row's), and Delta is what <dO, O> is with that: off by up to 2^-9 |dO| |O|.
