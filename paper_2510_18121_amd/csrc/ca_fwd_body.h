@@ -36,7 +36,7 @@ namespace ca {
 
 template <int D, bool WINDOW = false>
 struct FwdSmem {
-  static constexpr int NST = D == 128 ? 2 : 3;  // stages of a K and a V tile
+  static constexpr int NST = D == 128 || WINDOW ? 2 : 3;  // stages of a K and a V tile (WINDOW: four workgroups share a CU at head_dim 64)
   static constexpr int TILE = FWD_BN * 2 * D;   // one K or V tile
   static constexpr int K_OFF = 0;
   static constexpr int V_OFF = TILE;
@@ -287,7 +287,7 @@ __device__ __forceinline__ void fwd_workgroup(const FwdUnit *__restrict__ units,
   // koff and voff): mask, row maximum, lazy rescaling, nothing interleaved
   auto general_block = [&](int k0, auto residue) __attribute__((always_inline)) {
     constexpr bool RESIDUE = decltype(residue)::value;
-    constexpr int GS = D == 64 && !RESIDUE ? NR : 2;  // row groups at a time: with more the registers do not hold all of it
+    constexpr int GS = D == 64 && WINDOW ? 1 : D == 64 && !RESIDUE ? NR : 2;  // row groups at a time: with more the registers do not hold all of it
     if (WINDOW ? !seen(k0, 32) : k0 > wmax64) return;
     // Lazy rescaling: the running reference m only moves when some row's maximum has grown by more than
     // 2^RESCALE_LOG2; until then probabilities are taken relative to the stale m (they stay below

@@ -18,10 +18,11 @@ namespace ca {
 // Workgroups are always halves of units (128 rows, 32 positions of 4 heads of a group where it has so many): the registers do not
 // hold whole units' four row groups and a mask of two bounds (328 spilled at head_dim 128), and a half spans the fewer keys.
 // 64K tokens, window 1024, 4 sinks, 32/8 heads of 128: 1.27 to 1.31 ms, 0.84 PFLOP/s of 4 D per (pair, head); 16K tokens, window 512, 16/16
-// heads of 64: 82 us, 0.37.  Bound by vector instructions beside the MFMAs (at head_dim 128 the matrix pipe is busy 44 % of the time and vector
-// instructions issue 50 %; 22 and 54 % at 64): 18 tiles per unit are few, and 2 to 4 of them are masked.
+// heads of 64: 75 us, 0.41.  Bound by vector instructions beside the MFMAs (at head_dim 128 the matrix pipe is busy 44 % of the time and vector
+// instructions issue 50 %; 25 and 61 % at 64): 18 tiles per unit are few, and 2 to 4 of them are masked.
+// At head_dim 64 four workgroups share a CU, with two stages of tiles and 128 registers a wave: 82 -> 75 us against three with three stages.
 template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_fwd_window_kernel(
+__global__ __launch_bounds__(256, D == 64 ? 4 : 2) void ca_fwd_window_kernel(
     const FwdUnit *__restrict__ units, int n_units, const int32_t *__restrict__ slot_row, const int32_t *__restrict__ slot_pos,
     const int32_t *__restrict__ slot_lo, int sinks, int short_rows, const bf16_t *__restrict__ Q, const bf16_t *__restrict__ K,
     const bf16_t *__restrict__ V, bf16_t *__restrict__ O, float *__restrict__ LSE, int Hq, int Hkv, int64_t total_q, float c) {
