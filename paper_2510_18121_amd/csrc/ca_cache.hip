@@ -255,7 +255,7 @@ struct AttendShape {
 // in 16-byte runs, the next page's K while this one's scores are multiplied, its V behind this one's (a page further ahead took 5 % longer on 64 sequences
 // of about 4096 tokens, 7 % on 4 of 130K).  No barrier before the waves' sums meet.
 template <int D, int NR, int W>
-__global__ __launch_bounds__(64 * W, NR == 1 ? 2 : 1) void ca_cache_attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * W, NR == 1 || D == 64 ? 2 : 1) void ca_cache_attend_kernel(const AttendArgs a) {
   using S = AttendShape<D, NR, W>;
   constexpr int R = S::R, NH = D / 64, NB = D / 16;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -1042,14 +1042,16 @@ static int launched(const char *what, hipError_t e) {
   return fail(CA_ERR_HIP, std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")");
 }
 
-// Workers of W waves per KV head: as many as are on the chip at a time (NR: 16-row groups of a tile; 8: chunks).
-template <int NR, int W>
+// Workers of W waves per KV head: as many as are on the chip at a time (NR: 16-row groups of a tile; 8: chunks), eight waves to a CU.  Of tiles of
+// 32 rows at head_dim 128 four (352 registers: in 256, 23 of them spill, and 64 sequences of about 4096 tokens with 8 rows each take 204 us, not 197;
+// at head_dim 64 eight waves take 110, four 176).
+template <int D, int NR, int W>
 static int n_workers(int hkv) {
-  return std::max(1, N_CU * (NR == 2 ? 4 : 8) / W / hkv);
+  return std::max(1, N_CU * (NR == 2 && D == 128 ? 4 : 8) / W / hkv);
 }
 template <int D, int NR, int W>
 static size_t attend_bytes(int hkv) {
-  const size_t workers = size_t(n_workers<NR, W>(hkv));
+  const size_t workers = size_t(n_workers<D, NR, W>(hkv));
   return workers * hkv * sizeof(int4) + workers * 2 * hkv * (16 * NR * (D + 2)) * 4;
 }
 template <int D>
@@ -1060,7 +1062,7 @@ static size_t attend_bytes(const ca_cache *c) { return c->head_dim == 128 ? atte
 
 template <int D, int NR, int W>
 static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
-  const int workers = n_workers<NR, W>(a.hkv);
+  const int workers = n_workers<D, NR, W>(a.hkv);
   a.by_workers = 1.0001f / float(workers);
   a.heads = static_cast<int4 *>(ws);
   a.parts = reinterpret_cast<float *>(a.heads + size_t(workers) * a.hkv);
