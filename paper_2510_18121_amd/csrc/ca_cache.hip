@@ -490,7 +490,7 @@ struct ChunkSmem {
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void ca_cache_chunk_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_cache_chunk_kernel(const AttendArgs a) {
   using S = ChunkSmem<D>;
   constexpr int R = 128, NK = D / 32, NB = D / 16, ROWB = 2 * D, NL = D / 64;  // NL: loads of K, and of V, of a wave per page
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -1044,10 +1044,11 @@ static int launched(const char *what, hipError_t e) {
 
 // Workers of W waves per KV head: as many as are on the chip at a time (NR: 16-row groups of a tile; 8: chunks), eight waves to a CU.  Of tiles of
 // 32 rows at head_dim 128 four (352 registers: in 256, 23 of them spill, and 64 sequences of about 4096 tokens with 8 rows each take 204 us, not 197;
-// at head_dim 64 eight waves take 110, four 176).
+// at head_dim 64 eight waves take 110, four 176).  Of chunks at head_dim 64 twelve, where tiles are long (4 chunks of 500 rows behind 8192 tokens, 32/8 heads: 261 us
+// with eight, 241 with twelve; 8 prompts of 512: 37, 41).
 template <int D, int NR, int W>
-static int n_workers(int hkv) {
-  return std::max(1, N_CU * (NR == 2 && D == 128 ? 4 : 8) / W / hkv);
+static int n_workers(int hkv, bool long_tiles = true) {
+  return std::max(1, N_CU * (NR == 2 && D == 128 ? 4 : NR == 8 && D == 64 && long_tiles ? 12 : 8) / W / hkv);
 }
 template <int D, int NR, int W>
 static size_t attend_bytes(int hkv) {
@@ -1062,7 +1063,7 @@ static size_t attend_bytes(const ca_cache *c) { return c->head_dim == 128 ? atte
 
 template <int D, int NR, int W>
 static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
-  const int workers = n_workers<D, NR, W>(a.hkv);
+  const int workers = n_workers<D, NR, W>(a.hkv, a.s.width > CUT);
   a.by_workers = 1.0001f / float(workers);
   a.heads = static_cast<int4 *>(ws);
   a.parts = reinterpret_cast<float *>(a.heads + size_t(workers) * a.hkv);
