@@ -64,7 +64,7 @@ class KVCache:
 
 
 class OutOfPages(RuntimeError):
-    """The pool has fewer free pages than a call needs; nothing has changed."""
+    """The pool has fewer free pages than a call needs."""
 
 
 class Sequences:
@@ -111,7 +111,7 @@ class Sequences:
 
     def extend(self, seqs, rows, device=None):
         """Room for rows[i] more tokens of seqs[i], and the call's arrays: q_start, kv_len and page_table on the device.  A last page that
-        other sequences hold too is copied for each of them first.  On the current stream."""
+        other sequences hold too is copied for each of them first.  On the current stream.  Where it raises, nothing has changed."""
         seqs, rows = list(seqs), [operator.index(n) for n in rows]
         if len(seqs) != len(rows) or len(set(seqs)) != len(seqs) or any(n < 0 for n in rows):
             raise ValueError("extend: one count of rows, not negative, for each of the sequences, and each of them once")
@@ -128,29 +128,39 @@ class Sequences:
                     copies.append(s)
         if need + len(copies) > len(self.free_pages):
             raise OutOfPages(f"{need + len(copies)} pages needed, {len(self.free_pages)} free")
-        src, dst = [], []
+        # what may fail comes before what changes
+        free = iter(self.free_pages[::-1])
+        pages = {s: list(self.pages[s]) for s in seqs}
+        src = [pages[s][-1] for s in copies]
         for s in copies:
-            src.append(self.pages[s][-1])
-            self._let_go(src[-1])
-            self.pages[s][-1] = self._take()
-            dst.append(self.pages[s][-1])
+            pages[s][-1] = next(free)
+        dst = [pages[s][-1] for s in copies]
         for s, n in zip(seqs, rows):
-            self.lengths[s] += n
-            while len(self.pages[s]) * PAGE_TOKENS < self.lengths[s]:
-                self.pages[s].append(self._take())
+            pages[s] += [next(free) for _ in range(-(-(self.lengths[s] + n) // PAGE_TOKENS) - len(pages[s]))]
         self._copy(src, dst)
-        return self.arrays(seqs, rows, device)
+        out = self._arrays([pages[s] for s in seqs], [self.lengths[s] + n for s, n in zip(seqs, rows)], rows, device)
+        for _ in range(need + len(copies)):
+            self.uses[self.free_pages.pop()] = 1
+        for p in src:
+            self._let_go(p)
+        for s, n in zip(seqs, rows):
+            self.pages[s] = pages[s]
+            self.lengths[s] += n
+        return out
 
     def arrays(self, seqs, rows, device=None):
         """q_start, kv_len and page_table (int32) of a call with the last rows[i] tokens of seqs[i]."""
+        return self._arrays([self.pages[s] for s in seqs], [self.lengths[s] for s in seqs], rows, device)
+
+    def _arrays(self, pages, lengths, rows, device):
         import torch
-        table = np.full((len(seqs), max([len(self.pages[s]) for s in seqs], default=0)), -1, np.int32)
-        for i, s in enumerate(seqs):
-            table[i, :len(self.pages[s])] = self.pages[s]
+        table = np.full((len(pages), max([len(x) for x in pages], default=0)), -1, np.int32)
+        for i, x in enumerate(pages):
+            table[i, :len(x)] = x
         start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
         if device is None:
             device = self.caches[0].device if self.caches else "cpu"
-        return tuple(torch.from_numpy(x).to(device) for x in (start, np.array([self.lengths[s] for s in seqs], np.int32), table))
+        return tuple(torch.from_numpy(x).to(device) for x in (start, np.array(lengths, np.int32), table))
 
     def compact(self):
         """Moves the pages in use to the front of the pool, on the current stream; returns how many are in use.  Page tables made before are
@@ -165,11 +175,6 @@ class Sequences:
             self.uses[to], self.uses[p] = self.uses[p], 0
         self.free_pages = list(range(len(self.uses) - 1, n - 1, -1))
         return n
-
-    def _take(self):
-        p = self.free_pages.pop()
-        self.uses[p] = 1
-        return p
 
     def _let_go(self, p):
         if p >= 0:
