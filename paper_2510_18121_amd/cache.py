@@ -68,12 +68,15 @@ class OutOfPages(RuntimeError):
 
 
 class Sequences:
-    """The pages of sequences in a pool of n_pages (of `caches`, or given: without caches nothing is copied on a device)."""
+    """The pages of sequences in a pool of n_pages (the fewest that one of `caches` has, unless fewer are given; without caches nothing is
+    copied on a device)."""
 
     def __init__(self, caches=(), n_pages=None):
         self.caches = list(caches)
         if n_pages is None:
             n_pages = min(c.n_pages for c in self.caches)
+        if operator.index(n_pages) < 0 or any(c.n_pages < n_pages for c in self.caches):
+            raise ValueError(f"n_pages {n_pages}: not negative, and no more than each of the caches has")
         self.free_pages = list(range(n_pages - 1, -1, -1))  # the lowest is handed out first
         self.uses = [0] * n_pages                           # sequences that hold the page
         self.pages, self.lengths = {}, {}                   # of each sequence; a page that was let go is -1

@@ -3,7 +3,7 @@ import copy
 
 import pytest
 
-from paper_2510_18121_amd.cache import Sequences
+from paper_2510_18121_amd.cache import KVCache, Sequences
 
 
 def state(s):
@@ -59,3 +59,14 @@ def test_a_copy_that_fails_leaves_the_pool_as_it_was_before_a_compaction():
     with pytest.raises(RuntimeError):
         s.compact()
     assert state(s) == before
+
+
+def test_a_pool_larger_than_a_cache_is_refused():
+    """Tokens of pages that a cache does not have would be dropped without a word."""
+    small, large = (KVCache.empty(n, 1, 64, "cpu") for n in (4, 6))
+    assert len(Sequences([large, small]).free_pages) == 4 and len(Sequences([large, small], n_pages=3).free_pages) == 3
+    for caches, n in (([small], 5), ([large, small], 6), ([], -1), ([small], -1)):
+        with pytest.raises(ValueError):
+            Sequences(caches, n_pages=n)
+    with pytest.raises(TypeError):
+        Sequences([small], n_pages=2.5)
