@@ -233,6 +233,11 @@ class Plan:
             pass
 
 
+def _count(x) -> int:
+    """An integer for an int64 argument, where ctypes would take it modulo 2^64; beyond 2^63 - 1 one is as good as another."""
+    return max(-1, min(operator.index(x), (1 << 63) - 1))
+
+
 def _planned(batch, window, sinks, plain, windowed) -> Plan:
     keep = []
     d = make_desc(batch, keep)
@@ -240,7 +245,7 @@ def _planned(batch, window, sinks, plain, windowed) -> Plan:
     if window is None:
         _check(plain(ctypes.byref(d), ctypes.byref(h)))
     else:
-        _check(windowed(ctypes.byref(d), operator.index(window), operator.index(sinks), ctypes.byref(h)))
+        _check(windowed(ctypes.byref(d), _count(window), _count(sinks), ctypes.byref(h)))
     return Plan(h.value, batch)
 
 
@@ -439,7 +444,7 @@ def ca_cache_attend(cache, q, o, lse, q_start, kv_len, page_table, ws, window=No
     lp = None if lse is None else _on_cache(cache, lse, (hq, rows), cache.f32, "lse")
     b = _cache_batch(cache, rows, q_start, kv_len, page_table)
     wp, n = (None, 0) if ws is None else (_on_cache(cache, ws, ws.shape, ws.dtype, "ws"), ws.numel() * ws.element_size())
-    _check(lib().ca_cache_attend(cache.desc_ref, ctypes.byref(b), hq, softmax_scale, operator.index(window), operator.index(sinks), qp, op, lp, wp,
+    _check(lib().ca_cache_attend(cache.desc_ref, ctypes.byref(b), hq, softmax_scale, _count(window), _count(sinks), qp, op, lp, wp,
                                  n, _cache_stream(cache, stream)))
 
 
