@@ -29,7 +29,10 @@ class _CoreAttention(torch.autograd.Function):
         q, k, v, o, lse = ctx.saved_tensors
         s = ctx.server
         dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
-        B.ca_backward(s.plan, q, k, v, o, d_o.contiguous(), lse, dq, dk, dv, s.ws)
+        d_o = d_o.contiguous()
+        if d_o.data_ptr() % 16 != 0:  # (where autograd's tensors lie is not the caller's choice)
+            d_o = d_o.clone()
+        B.ca_backward(s.plan, q, k, v, o, d_o, lse, dq, dk, dv, s.ws)
         return dq, dk, dv, None
 
 
