@@ -10,15 +10,17 @@
 // e4m3 is exact in bf16; the scales go into the exponent's factor (K) and into the probabilities (V).
 //
 // O = softmax(scale Q K^T) V and LSE need the codes once, 2 D bytes per (token, KV head): reading them bounds single tokens, and
-// matrix products bound chunks.  Measured (kernel times, 8 KV heads of 128 unless noted):
+// matrix products bound chunks.  Measured (kernel times under rocprofv3, medians over four sets of inputs in turn, of which the last cache holds none
+// of the large ones; 8 KV heads of 128 unless noted):
 //   attend   64 sequences of about 4096 tokens, 32 heads      144 us, 6.2 TB/s (a large copy: 4.97 read and written)
-//            4 sequences of 130K tokens, 64 heads             168 us, 6.3 TB/s
-//            32 sequences, window 4096, 16/16 heads of 64      47 us, 5.7 TB/s
-//            one sequence of 901 tokens                      11.3 us (14 bytes per cycle and CU, 8 CUs)
-//   chunk    4 chunks of 500 rows behind 8192 tokens          221 us, 0.94 PFLOP/s executed
+//            4 sequences of 130K tokens, 64 heads             173 us, 6.2 TB/s
+//            32 sequences, window 4096, 16/16 heads of 64      54 us, 4.9 TB/s (47 us on one set of inputs)
+//            one sequence of 901 tokens                      11.6 us (15 pages of 16 KiB, one CU per KV head: 9 bytes per cycle and
+//                                                             CU; 15 from the first page to the last, the rest is the way there and back)
+//   chunk    4 chunks of 500 rows behind 8192 tokens          246 us, 0.78 PFLOP/s (222 and 0.87 in a call without the profiler)
 //   combine  of these                                         4 to 5 us, 13 us
-//   append   128 tokens; 16 prompts of 2048                   6.6 us; 31 us, 4.4 TB/s
-//   copy     4000 pages of 128 KiB                            209 us, 5.0 TB/s
+//   append   128 tokens; 16 prompts of up to 2048             6.6 us; 41 us, 3.4 TB/s (32 us on one set of inputs)
+//   copy     4000 pages of 128 KiB                            212 us, 4.9 TB/s
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -161,6 +163,9 @@ struct AttendArgs {
 // of a tile.  The units of all sequences, in order, are dealt to the workers in equal runs, whatever the sequences' lengths
 // are; a run that ends inside a tile of at most CUT pages is moved to the tile's nearer end, longer tiles are cut.  (A CU takes 1100
 // cycles per page that it reads alone, of head_dim 128, and what adding up the parts takes 10 thousand, most of it between launches.)
+// Every tile of a sequence counts as many units as the sequence has pages (or the window spans), also where its rows sit early and do not see the
+// later ones, which are passed over: a prompt from its first token is dealt unevenly (32/8 heads of 128: one of 2048 rows 91 us, sixteen 1010; their flops
+// need 25 and 407), one behind a long context is not.
 constexpr int CUT = 16;
 __device__ __forceinline__ int tile_pages(int len, int R, int G, int window, int sinks) {
   const int pages = (len + PAGE - 1) / PAGE;
@@ -480,7 +485,7 @@ __global__ __launch_bounds__(64 * W, NR == 1 || D == 64 ? 2 : 1) void ca_cache_a
 // next one is written to the other stage while this one is multiplied; one barrier per page.  K's rows stand in the order of
 // the four tiles' rows, V^T's chunks of 8 keys in the order of its fragments, both swizzled as the other kernels' tiles are.
 // (4 chunks of 500 rows behind 8192 tokens, 32/8 heads of 128, the whole call: 412 us with 64 rows to a wave of the kernel above, 305 through
-// LDS, 258 with fragments fetched ahead and exponentials between MFMAs, 232 now.  MFMAs 38 % busy, vector instructions issue 46 %: conversions,
+// LDS, 258 with fragments fetched ahead and exponentials between MFMAs, 235 now.  MFMAs 38 % busy, vector instructions issue 46 %: conversions,
 // exponentials and packing beside them bound it.)  P is one bf16 operand here (its rounding is as large as O's own), not two as above.
 template <int D>
 struct ChunkSmem {
@@ -841,7 +846,7 @@ __device__ __forceinline__ float wave_top(uint32_t top) { return __builtin_bit_c
 // that leave the normal range.
 // K: D / 8 lanes per token, 8 columns each.  V: a lane has two columns; at head_dim 64 the wave's halves take tokens of their own.
 // (128 single tokens: 22 us with a workgroup per page, K and V one after the other; 8.6 with a wave each; 6.8 with the sequences in lanes or LDS.
-// 16 prompts of 2048 tokens: 47, 40.7 and 31 us.)
+// 16 prompts of up to 2048 tokens: 47, 40.7 and 32 us on one set of inputs, which the last cache holds; 41 where it does not.)
 template <int D>
 __global__ __launch_bounds__(256) void ca_cache_append_kernel(const AppendArgs a) {
   constexpr int LPT = D / 8, TPI = 64 / LPT, NI = PAGE / TPI;  // K: lanes per token, tokens per load, loads per page
@@ -1089,6 +1094,8 @@ static int launch_attend(AttendArgs a, void *ws, hipStream_t st) {
 // 25; 32 rows a tile, 200 of 500: 87 with four, 72 with two; contexts of thousands: level).  With fewer tiles a CU has one of its own, which its waves share: four
 // where contexts are short (32 sequences of 500: 17.3, 13.5, 15.8, 18.6; one of 901: 12.2, 11.6, 13.6, 20), eight otherwise (16 of 4000: 33, 36, 37, 38).  More
 // sequences than fit LDS four times leave pairs to themselves on a CU.
+// One kernel serves a call, by this average, also where single tokens and a chunk come together: 32/8 heads of 128, 63 tokens at 4096 (alone 93 us) with a
+// chunk of 400 rows (59) take 172 us, with one of 512 (61) 178; 127 tokens (172) with one of 500 (61) 278; 200 tokens at 1000 (81) with one of 500 (40) 107.
 template <int D>
 static int attend_by_rows(const AttendArgs &a, void *ws, hipStream_t st) {
   const int64_t rows = int64_t(a.s.total) * a.G / a.s.n_seqs, tiles = int64_t(a.s.n_seqs) * a.hkv;

@@ -294,8 +294,8 @@ __device__ __forceinline__ void fwd_workgroup(const FwdUnit *__restrict__ units,
     // 2^RESCALE_LOG2, harmless in fp32 and bf16) and the accumulators need no multiply.
     // (a row that sees none of these keys, having seen none before (in a piece that lies beyond its position), keeps
     // m = M_NONE and gets probabilities 0)
-    // The first rows of a document see a handful of keys, their output is as large as a single V row, and the 2^-9 relative
-    // rounding of P to bf16 would show up at the 1e-2 level next to the output's own bf16 rounding.  So the rounding residue of
+    // The first rows of a document see a handful of keys, their output is as large as a single V row, and the
+    // rounding of P to bf16 (up to 2^-8 of it) would show up at the 1e-2 level next to the output's own bf16 rounding.  So the rounding residue of
     // P goes through the matrix pipe too (P = hi + lo), which makes P V as good as fp32.  Later tiles go without: with it, and 16 keys
     // at a time, a forward that repeats all of its 16K tokens took 700 us instead of 493 (16/16 heads, head_dim 64) and 1600
     // instead of 1310 (32/8, 128).

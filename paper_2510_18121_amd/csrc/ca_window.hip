@@ -18,7 +18,7 @@ namespace ca {
 // Workgroups are always halves of units (128 rows, 32 positions of 4 heads of a group where it has so many): the registers do not
 // hold whole units' four row groups and a mask of two bounds (328 spilled at head_dim 128), and a half spans the fewer keys.
 // 64K tokens, window 1024, 4 sinks, 32/8 heads of 128: 1.27 to 1.31 ms, 0.84 PFLOP/s of 4 D per (pair, head); 16K tokens, window 512, 16/16
-// heads of 64: 75 us, 0.41.  Bound by vector instructions beside the MFMAs (at head_dim 128 the matrix pipe is busy 44 % of the time and vector
+// heads of 64: 75 us (80 with inputs that the last cache does not hold), 0.41.  Bound by vector instructions beside the MFMAs (at head_dim 128 the matrix pipe is busy 44 % of the time and vector
 // instructions issue 50 %; 25 and 61 % at 64): 18 tiles per unit are few, and 2 to 4 of them are masked.
 // At head_dim 64 four workgroups share a CU, with two stages of tiles and 128 registers a wave: 82 -> 75 us against three with three stages.
 template <int D>
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void ca_fwd_window_kernel(
 // probabilities of 0.  D / 8 lanes per row; the statistics leave through LDS as whole lines.  Bound by memory: 203 us, 5.4 TB/s, on the 64K tokens
 // above (a workgroup per 64 slots and all heads, with the statistics stored as they came: 257 us).  O, which nothing else of the pass
 // reads, passes the caches by (210 -> 200 us).
-// O is the caller's, in bf16 (with shards of a merged row it is the whole row's), and Delta is what <dO, O> is with that: off by up to 2^-9 |dO| |O|.
+// O is the caller's, in bf16 (with shards of a merged row it is the whole row's), and Delta is what <dO, O> is with that: off by up to 2^-8 |dO| |O|.
 // Where a row sees a few keys alone that is the largest of the roundings (relative error of dQ and dK: 0.0025 from windows of 16 keys
 // on, 0.0027 with 6, 0.0036 with 2; 0.0017 is what rounding them to bf16 costs).
 template <int D>

@@ -248,6 +248,9 @@ def split_kv(b: Batch, window: int):
     Returns (partial batch, gather, part_rows): gather [total_q'] = original packed-Q row of every row of the
     partial batch (to build its Q and dO, and to scatter results back); part_rows [n_parts, total_q] int32 = for every
     original row its rows in the partial batch, window by window, -1 where it has fewer windows.
+
+    In a plan of the partial batch for layers with a sliding window (binding.ca_plan) sinks count from every key window's first key:
+    results merge to the whole's without sinks only.
     """
     assert window >= 1
     doc_start, doc_len, win_of_doc = [], [], []
