@@ -1,5 +1,5 @@
 """The bound of two bf16 operands of P, on the CPU: a model of the kernels' roundings keeps it, and with one operand, or a wrong second one,
-does not: in the batches of tests/test_gpu_accuracy.py, so that these would find such a kernel."""
+does not, on rows of as few keys as those of tests/test_gpu_accuracy.py: that test would find such a kernel."""
 import pytest
 import torch
 
