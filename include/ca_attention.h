@@ -276,6 +276,51 @@ int ca_cache_attend_workspace_bytes(const ca_cache *cache, int32_t n_q_heads, si
 int ca_cache_copy_pages(const ca_cache *cache, const int32_t *src, const int32_t *dst, int64_t n, void *hip_stream);
 
 /*
+ * Queries and keys on their way to attention: the norm of each head, and the turn by the position of the row, in one pass.
+ * Of a head x of head_dim columns at position p, with a gain g [head_dim]:
+ *   u = g x / sqrt(mean(x^2) + eps)  (without a gain u = x);   y = R(p) u
+ * where R(p) turns the pairs of the first rot_dim columns, (i, i + rot_dim / 2), or interleaved (2 i, 2 i + 1), by p times the frequency of
+ * pair i and multiplies them by `factor`, and leaves the other columns as they are.  Statistics and turns are computed in fp32, y is rounded
+ * once.  rot_dim 0: the norm alone (a layer without positions).  A frequency is a turn per position in units of 2^-64 (round(f / (2 pi) * 2^64) modulo 2^64 for f radians
+ * per position): the fraction of a turn at a position is exact, however far that lies.  ca_rotation is a description in host memory.
+ */
+typedef struct {
+  int32_t head_dim, rot_dim; /* head_dim 64 or 128; rot_dim even, 0 .. head_dim */
+  int32_t interleaved;
+  float factor;              /* of the turned columns, 1 for none */
+  const uint64_t *turns;     /* DEVICE [rot_dim / 2] */
+} ca_rotation;
+
+/* One tensor of a call, queries or keys: rows of `heads` heads side by side, from one row to the next the given number of elements, a
+ * multiple of 8 (so that the queries and keys of a joint projection are taken from where they are); x, y, dy, 16-byte aligned, bf16. */
+typedef struct {
+  const void *x;      /* not read by ca_rotate_backward where gain is NULL */
+  const void *dy;     /* ca_rotate_backward */
+  void *y;            /* the result: y of ca_rotate, dx of ca_rotate_backward; it may be x, or dy, itself (same stride), and otherwise
+                         overlaps no input */
+  const float *gain;  /* DEVICE fp32 [head_dim], or NULL: no norm */
+  float *dgain;       /* ca_rotate_backward with a gain: fp32 [head_dim], written */
+  const int32_t *pos; /* DEVICE [rows]: the position of each row, of any sign; not read where the call has sequences */
+  int64_t rows, x_stride, dy_stride, y_stride;
+  int32_t heads;
+} ca_rotate_tensor;
+
+/*
+ * ca_rotate: y of one or two tensors (queries and keys, which may have different rows and positions) in one launch.
+ * where: NULL, or the sequences of the rows (n_seqs, q_start and kv_len of a ca_cache_batch are read, on the device): row r of sequence s is
+ * at position kv_len[s] - (q_start[s + 1] - r), and rows of no sequence are left as they are.
+ * ca_rotate_backward: dx, and dgain (the sum over all rows and heads, in a fixed order), of the same y: all but y and dy as in the forward call.  ws: device
+ * workspace of ca_rotate_backward_workspace_bytes, 16-byte aligned, needed where there is a gain; calls that may overlap in time need one
+ * each.  One launch, or two with gains.  dx rows of no sequence are left as they are.
+ * Both: asynchronous on hip_stream, allocate nothing, bit-reproducible.
+ */
+int ca_rotate(const ca_rotation *rotation, const ca_rotate_tensor *tensors, int32_t n_tensors, const ca_cache_batch *where, float eps,
+              void *hip_stream);
+int ca_rotate_backward(const ca_rotation *rotation, const ca_rotate_tensor *tensors, int32_t n_tensors, const ca_cache_batch *where,
+                       float eps, void *ws, size_t ws_bytes, void *hip_stream);
+size_t ca_rotate_backward_workspace_bytes(void);
+
+/*
  * Per-kernel timing for profilers and cost models (Section 4.2's profiler benchmarks core attention over
  * a grid of shapes; this is the hook it reads).  After ca_profile_enable(plan, 1) every ca_forward /
  * ca_backward on that plan records HIP events on the caller's stream around its kernels.

@@ -6,6 +6,7 @@ Plumbing only: forward() calls ca_forward, backward() calls ca_backward; nothing
 Q, K, V, O and the per-row log-sum-exp and recomputes P in backward (Section 2.1)."""
 from __future__ import annotations
 
+import numpy as np
 import torch
 
 from . import binding as B
@@ -36,6 +37,16 @@ class _CoreAttention(torch.autograd.Function):
         return dq, dk, dv, None
 
 
+def row_positions(batch):
+    """Document position of every row of the packed Q, and of the packed K (int32; 0 for rows of no task, keys of no document)."""
+    q, kv = np.zeros(batch.total_q, np.int32), np.zeros(batch.total_kv, np.int32)
+    for rows, starts, lens, first in ((q, batch.task_q_start, batch.task_q_len, batch.task_q_pos),
+                                      (kv, batch.doc_kv_start, batch.doc_kv_len, np.zeros(len(batch.doc_kv_len), np.int64))):
+        for a, n, p in zip(*(np.asarray(x).tolist() for x in (starts, lens, first))):
+            rows[a:a + n] = np.arange(p, p + n)
+    return q, kv
+
+
 class AttentionServer:
     """One fused batch of CA-tasks planned once and run as a differentiable op:
 
@@ -45,12 +56,23 @@ class AttentionServer:
 
     `batch` is any object with the descriptor's fields (e.g. workloads.Batch).  Rows of q that belong to no task
     have undefined output and zero gradient.  one_pass: see binding.alloc_workspace.  window, sinks: every row attends the last
-    `window` keys of its context, itself among them, and the context's first `sinks` (None: all of it); see binding.ca_plan."""
+    `window` keys of its context, itself among them, and the context's first `sinks` (None: all of it); see binding.ca_plan.
+    rotation (rotary.Rotation): q and k are turned by the positions of their rows in their documents first, and, with gains, each head of
+    them is normed before: o = server(q, k, v, q_gain, k_gain)."""
 
-    def __init__(self, batch, device="cuda", one_pass=None, window=None, sinks=0):
+    def __init__(self, batch, device="cuda", one_pass=None, window=None, sinks=0, rotation=None, eps=1e-6):
+        if rotation is not None and rotation.head_dim != batch.head_dim:
+            raise ValueError(f"the rotation's head_dim is {rotation.head_dim}, the batch's {batch.head_dim}")
         self.plan = B.ca_plan(batch, window, sinks)
         self.ws = B.alloc_workspace(self.plan, device, one_pass)
         self.fwd_ws_bytes = self.plan.workspace_bytes_split()[0]
+        self.rotation, self.eps = rotation, eps
+        if rotation is not None:
+            self.q_pos, self.kv_pos = (torch.from_numpy(x).to(device) for x in row_positions(batch))
 
-    def __call__(self, q, k, v):
+    def __call__(self, q, k, v, q_gain=None, k_gain=None):
+        if self.rotation is not None:
+            q, k = self.rotation(q, k, self.q_pos, self.kv_pos, q_gain=q_gain, k_gain=k_gain, eps=self.eps)
+        elif q_gain is not None or k_gain is not None:
+            raise ValueError("gains without a rotation (one of no frequencies turns nothing)")
         return _CoreAttention.apply(q, k, v, self)

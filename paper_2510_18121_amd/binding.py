@@ -49,6 +49,14 @@ class CacheBatch(ctypes.Structure):
                 ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
 
 
+class RotateTensor(ctypes.Structure):
+    """ca_rotate_tensor of include/ca_attention.h."""
+
+    _fields_ = [("x", ctypes.c_void_p), ("dy", ctypes.c_void_p), ("y", ctypes.c_void_p), ("gain", ctypes.c_void_p), ("dgain", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p), ("rows", ctypes.c_int64), ("x_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64), ("heads", ctypes.c_int32)]
+
+
 def lib() -> ctypes.CDLL:
     """The loaded C-ABI library; raises if it has not been built (python -m paper_2510_18121_amd.build)."""
     global _lib
@@ -96,6 +104,9 @@ def lib() -> ctypes.CDLL:
         L.ca_cache_attend.argtypes = [vp, vp, i32, ctypes.c_float, i64, i64, vp, vp, vp, vp, sz, vp]
         L.ca_cache_attend_workspace_bytes.argtypes = [vp, i32, ctypes.POINTER(sz)]
         L.ca_cache_copy_pages.argtypes = [vp, vp, vp, i64, vp]
+        L.ca_rotate.argtypes = [vp, vp, i32, vp, ctypes.c_float, vp]
+        L.ca_rotate_backward.argtypes = [vp, vp, i32, vp, ctypes.c_float, vp, sz, vp]
+        L.ca_rotate_backward_workspace_bytes.restype = sz
         L.ca_mfma_stream.argtypes = L.ca_mfma_stream16.argtypes = [vp, i64, i32, i32, vp, vp]
         L.ca_xcd_map.argtypes = [i32, i32, vp, vp]
         L.ca_atomic_stream.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp]
@@ -461,6 +472,109 @@ def alloc_cache_workspace(cache, n_q_heads, device=None):
     n = ctypes.c_size_t()
     _check(lib().ca_cache_attend_workspace_bytes(cache.desc_ref, operator.index(n_q_heads), ctypes.byref(n)))
     return torch.empty(n.value, dtype=torch.uint8, device=cache.device if device is None else device)
+
+
+def rows_in_line(t):
+    """t [rows, heads, head_dim] itself where its rows are 16-byte aligned and each of them is one run of memory, otherwise a copy."""
+    import torch
+    rows, heads, d = t.shape
+    s = t.stride()
+    if s[2] == 1 and (heads == 1 or s[1] == d) and (rows == 1 or (s[0] % 8 == 0 and s[0] >= heads * d)) and t.data_ptr() % 16 == 0:
+        return t
+    return t.clone(memory_format=torch.contiguous_format)
+
+
+def _rows(t, shape, index, name):
+    """Address and row stride of a bf16 tensor [rows, heads, head_dim] on that device, each of whose rows is one run of memory."""
+    import torch
+    rows, heads, d = shape
+    s = t.stride()
+    if (t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != index or s[2] != 1 or (heads != 1 and s[1] != d)
+            or (rows > 1 and (s[0] < heads * d or s[0] % 8))):
+        raise ValueError(f"{name}: expected bf16 tensor {tuple(shape)} on device {index}, whose rows are runs of memory a multiple of 8 elements apart, "
+                         f"got {tuple(t.shape)} {t.dtype} on {t.device} with strides {s}")
+    return (t.data_ptr() if rows else None), (s[0] if rows > 1 else heads * d)
+
+
+def _flat(t, shape, dtype, index, name):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous tensor {shape} {dtype} on device {index}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _rotate_tensor(rotation, x, dy, y, pos, by_sequences, gain, dgain, name):
+    """A ca_rotate_tensor; x None: of a gradient without a gain."""
+    import torch
+    index, f32 = rotation.index, torch.float32
+    shape = y.shape
+    if len(shape) != 3 or shape[2] != rotation.head_dim:
+        raise ValueError(f"{name}: expected [rows, heads, {rotation.head_dim}], got {tuple(shape)}")
+    d = (rotation.head_dim,)
+    t = RotateTensor()
+    t.rows, t.heads = shape[0], shape[1]
+    t.y, t.y_stride = _rows(y, shape, index, name + " (out)")
+    if x is not None:
+        t.x, t.x_stride = _rows(x, shape, index, name)
+    if dy is not None:
+        t.dy, t.dy_stride = _rows(dy, shape, index, f"gradient of {name}")
+    if gain is not None:
+        t.gain = _flat(gain, d, f32, index, f"gain of {name}")
+        if dy is not None:
+            t.dgain = _flat(dgain, d, f32, index, f"gradient of the gain of {name}")
+    if not by_sequences:
+        if pos is None:
+            raise ValueError(f"{name}: neither positions nor sequences are given")
+        t.pos = _flat(pos, shape[:1], torch.int32, index, f"positions of {name}")
+    return t
+
+
+def _rotate_call(rotation, tensors, where):
+    """The tensors as an array, their number, and the sequences as a ca_cache_batch (or None)."""
+    import torch
+    index, current = rotation.index, torch.cuda.current_device()
+    if index != current:
+        raise ValueError(f"the rotation is on {rotation.device}, the current device is {current}")
+    batch = None
+    if where is not None:
+        start, lens = where[0], where[1]
+        n = lens.shape[0]
+        batch = CacheBatch(n, 0, tensors[0].rows, _flat(start, (n + 1,), torch.int32, index, "q_start"), _flat(lens, (n,), torch.int32, index, "kv_len"), None)
+    return (RotateTensor * len(tensors))(*tensors), len(tensors), None if batch is None else ctypes.byref(batch)
+
+
+def ca_rotate(rotation, q, k, q_out, k_out, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, eps=1e-6, stream=None):
+    """Norm (with a gain) and turn of the rows of q, and of k unless it is None, in one launch on torch's current stream, or `stream`
+    (rotation: rotary.Rotation).  q, k and the outputs: bf16 [rows, heads, head_dim], each row a run of memory, so that views of a joint projection
+    will do; an output may be its input.  Positions: q_pos and k_pos (device int32 [rows]; k_pos None: those of q), or where = (q_start, kv_len, ..) of
+    the sequences of a call on a cache: rows are their last ones, and rows of no sequence are left as they are.  Gains: fp32 [head_dim]."""
+    tensors = [_rotate_tensor(rotation, q, None, q_out, q_pos, where is not None, q_gain, None, "q")]
+    if k is not None:
+        tensors.append(_rotate_tensor(rotation, k, None, k_out, q_pos if k_pos is None else k_pos, where is not None, k_gain, None, "k"))
+    array, n, batch = _rotate_call(rotation, tensors, where)
+    _check(lib().ca_rotate(rotation.desc_ref, array, n, batch, eps, _stream_ptr(stream)))
+
+
+def ca_rotate_backward(rotation, q, k, dq_out, dk_out, dq, dk, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, dq_gain=None,
+                       dk_gain=None, eps=1e-6, ws=None, stream=None):
+    """Gradients of ca_rotate: dq and dk (may be dq_out and dk_out) and, with gains, dq_gain and dk_gain (fp32 [head_dim]), from dq_out and dk_out
+    (dk_out None: of q alone).  q and k are needed where there is a gain, as is ws (alloc_rotate_workspace)."""
+    tensors = []
+    for x, dy, dx, pos, gain, dgain, name in ((q, dq_out, dq, q_pos, q_gain, dq_gain, "q"),
+                                              (k, dk_out, dk, q_pos if k_pos is None else k_pos, k_gain, dk_gain, "k")):
+        if dy is None:
+            continue
+        if gain is not None and (x is None or dgain is None):
+            raise ValueError(f"{name}: with a gain the gradient needs the input, and a tensor for that of the gain")
+        tensors.append(_rotate_tensor(rotation, x if gain is not None else None, dy, dx, pos, where is not None, gain, dgain, name))
+    array, n, batch = _rotate_call(rotation, tensors, where)
+    wp, wn = (None, 0) if ws is None else (_flat(ws, ws.shape, ws.dtype, rotation.index, "ws"), ws.numel() * ws.element_size())
+    _check(lib().ca_rotate_backward(rotation.desc_ref, array, n, batch, eps, wp, wn, _stream_ptr(stream)))
+
+
+def alloc_rotate_workspace(device="cuda"):
+    """A torch uint8 buffer big enough for ca_rotate_backward.  Calls that may overlap in time need one each."""
+    import torch
+    return torch.empty(lib().ca_rotate_backward_workspace_bytes(), dtype=torch.uint8, device=device)
 
 
 def ca_mfma_stream(operands, n_mfma_per_wave, sums, side_work=0, stream=None, shape=32):

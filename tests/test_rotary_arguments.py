@@ -1,0 +1,129 @@
+"""Turned queries and keys without a GPU: frequencies, the definition's gradients, and what the calls refuse."""
+import ctypes
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+import torch
+
+import rotary_util as U
+from paper_2510_18121_amd import binding as B
+from paper_2510_18121_amd import rotary as R
+from paper_2510_18121_amd.autograd import row_positions
+
+
+def test_frequencies():
+    f = R.frequencies(8, 10000.0)
+    assert np.allclose(f, [1, 0.1, 0.01, 0.001], rtol=1e-15)
+    assert np.array_equal(R.interpolated(f, 4), f / 4)
+    g = R.by_parts(f, 4, 1000, slow=1.0, fast=100.0)  # turns in 1000 positions: 159, 15.9, 1.59, 0.159
+    assert g[0] == f[0] and g[3] == f[3] / 4 and f[1] / 4 < g[1] < f[1] and f[2] / 4 < g[2] < f[2]
+    kept = (1000 * 0.1 / (2 * np.pi) - 1) / 99
+    assert np.isclose(g[1], 0.1 * (kept + (1 - kept) / 4), rtol=1e-14)
+
+
+def test_turns_are_fractions_of_a_turn():
+    f = np.array([1.0, 0.37, 1e-9, -0.25, 7.0])
+    r = R.Rotation(64, frequencies=f, device="cpu")
+    turns = r.turns.numpy().view(np.uint64)
+    for x, t in zip(f, turns.tolist()):
+        for p in (1, 12345, 10 ** 6, -7):
+            got = (p * t % 2 ** 64) / 2 ** 64 * 2 * np.pi
+            d = (got - p * x + np.pi) % (2 * np.pi) - np.pi
+            assert abs(d) < 1e-9, (x, p)
+    assert r.rot_dim == 10 and r.head_dim == 64
+
+
+@pytest.mark.parametrize("rot,interleaved", [(8, False), (6, True), (0, False)])
+def test_the_definitions_gradients_against_differences(rot, interleaved):
+    g = torch.Generator().manual_seed(rot)
+    x, dy = (torch.randn(3, 2, 8, generator=g, dtype=U.F64) for _ in range(2))
+    gain, pos, freq = torch.randn(8, generator=g, dtype=U.F64), torch.tensor([0, 5, 70001]), R.frequencies(rot, 100.0)
+    dx, dg, _, _ = U.backward(x, dy, pos, freq, interleaved, 1.3, gain)
+    f = lambda x, gain: (U.forward(x, pos, freq, interleaved, 1.3, gain)[0] * dy).sum()  # noqa: E731
+    for t, grad in ((x, dx), (gain, dg)):
+        for i in range(t.numel()):
+            h = torch.zeros_like(t)
+            h.view(-1)[i] = 1e-6
+            a, b = (f(t + s * h, gain) if t is x else f(x, t + s * h) for s in (1, -1))
+            assert abs((a - b) / 2e-6 - grad.reshape(-1)[i]) < 1e-7
+
+
+def test_row_positions():
+    b = SimpleNamespace(total_q=7, total_kv=9, task_q_start=np.array([4, 0]), task_q_len=np.array([3, 2]), task_q_pos=np.array([2, 10]),
+                        doc_kv_start=np.array([0, 5]), doc_kv_len=np.array([5, 3]))
+    q, kv = row_positions(b)
+    assert q.tolist() == [10, 11, 0, 0, 2, 3, 4] and kv.tolist() == [0, 1, 2, 3, 4, 0, 1, 2, 0] and q.dtype == kv.dtype == np.int32
+
+
+@pytest.mark.parametrize("kw", [{"head_dim": 96}, {"head_dim": 64, "rot_dim": 66}, {"head_dim": 64, "rot_dim": 7}, {"head_dim": 64, "base": 0.0},
+                                {"head_dim": 64, "frequencies": [float("nan")]}, {"head_dim": 64, "frequencies": [1.0] * 33},
+                                {"head_dim": 64, "frequencies": [1.0], "rot_dim": 4}, {"head_dim": 64, "factor": float("inf")}])
+def test_rotations_that_are_refused(kw):
+    with pytest.raises(ValueError):
+        R.Rotation(device="cpu", **kw)
+
+
+@pytest.mark.parametrize("bad", [lambda: R.interpolated([1.0], 0), lambda: R.by_parts([1.0], 2, 100, 5, 5), lambda: R.by_parts([1.0], -1, 100)])
+def test_frequency_arguments_that_are_refused(bad):
+    with pytest.raises(ValueError):
+        bad()
+
+
+PTR = 1 << 20  # an address that no check reads
+
+
+def call(rotation=None, tensor=None, n=1, where=None, eps=1e-6, backward=False, ws=PTR, ws_bytes=1 << 30):
+    r = R.RotationDesc(128, 128, 0, 1.0, PTR)
+    for k, v in (rotation or {}).items():
+        setattr(r, k, v)
+    t = B.RotateTensor(x=PTR, dy=PTR, y=PTR, gain=PTR, dgain=PTR, pos=PTR, rows=5, x_stride=1024, dy_stride=1024, y_stride=1024, heads=8)
+    for k, v in (tensor or {}).items():
+        setattr(t, k, v)
+    batch = None if where is None else ctypes.byref(B.CacheBatch(*where))
+    arr = (B.RotateTensor * 2)(t, t)
+    if backward:
+        return B.lib().ca_rotate_backward(ctypes.byref(r), arr, n, batch, eps, ws, ws_bytes, None)
+    return B.lib().ca_rotate(ctypes.byref(r), arr, n, batch, eps, None)
+
+
+BAD, NOT, ROOM = B.CA_ERR_INVALID_ARG, B.CA_ERR_UNSUPPORTED, B.CA_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("want,kw", [
+    (NOT, {"rotation": {"head_dim": 96}}), (BAD, {"rotation": {"rot_dim": 130}}), (BAD, {"rotation": {"rot_dim": -2}}), (BAD, {"rotation": {"rot_dim": 7}}),
+    (BAD, {"rotation": {"turns": None}}), (BAD, {"n": 0}), (BAD, {"n": 3}), (BAD, {"eps": -1.0}), (BAD, {"eps": float("nan")}),
+    (BAD, {"tensor": {"rows": -1}}), (BAD, {"tensor": {"heads": 0}}), (NOT, {"tensor": {"rows": 1 << 31}}), (BAD, {"tensor": {"x": None}}),
+    (BAD, {"tensor": {"x": PTR + 8}}), (BAD, {"tensor": {"x_stride": 1020}}), (BAD, {"tensor": {"x_stride": 1028}}), (BAD, {"tensor": {"x_stride": 1016}}),
+    (BAD, {"tensor": {"y": None}}), (BAD, {"tensor": {"y": PTR + 2}}), (BAD, {"tensor": {"y_stride": 0}}), (BAD, {"tensor": {"pos": None}}),
+    (BAD, {"tensor": {"dy": None}, "backward": True}), (BAD, {"tensor": {"dy_stride": 1}, "backward": True}),
+    (BAD, {"tensor": {"dgain": None}, "backward": True}), (ROOM, {"backward": True, "ws": None}), (ROOM, {"backward": True, "ws_bytes": 64}),
+    (ROOM, {"backward": True, "ws": PTR + 4}), (BAD, {"tensor": {"x": None}, "backward": True}),
+    (NOT, {"where": (4097, 0, 5, PTR, PTR, None)}), (NOT, {"where": (-1, 0, 5, PTR, PTR, None)}), (BAD, {"where": (3, 0, 5, None, PTR, None)}),
+    (BAD, {"where": (3, 0, 5, PTR, None, None)})])
+def test_calls_that_are_refused(want, kw):
+    assert call(**kw) == want
+    assert B.lib().ca_last_error()
+
+
+def test_null_rotation_and_tensors():
+    assert B.lib().ca_rotate(None, None, 1, None, 0.0, None) == BAD
+    r = R.RotationDesc(128, 0, 0, 1.0, None)
+    assert B.lib().ca_rotate(ctypes.byref(r), None, 1, None, 0.0, None) == BAD
+
+
+def test_nothing_to_do_is_no_launch():
+    assert call(tensor={"rows": 0, "x": None, "y": None, "gain": None}) == B.CA_OK
+    assert call(where=(0, 0, 5, None, None, None)) == B.CA_OK
+
+
+def test_gains_without_a_rotation_are_refused():
+    from paper_2510_18121_amd.autograd import AttentionServer
+    s = object.__new__(AttentionServer)
+    s.rotation = None
+    with pytest.raises(ValueError):
+        s(None, None, None, q_gain=torch.ones(64))
+
+
+def test_workspace_does_not_depend_on_the_call():
+    assert B.lib().ca_rotate_backward_workspace_bytes() == 2 * 2048 * 128 * 4
