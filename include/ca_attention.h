@@ -269,6 +269,14 @@ int ca_cache_attend(const ca_cache *cache, const ca_cache_batch *batch, int32_t 
 int ca_cache_attend_workspace_bytes(const ca_cache *cache, int32_t n_q_heads, size_t *bytes);
 
 /*
+ * ca_cache_read: the rows of the batch back out of the pages of their sequences: k and v (device bf16 [total_rows][n_kv_heads][head_dim], 16-byte aligned; one of them may be
+ * NULL) receive code * scale, rounded once (NaN where the code is; exact, but for values below bf16's normal range, where scales are powers of two, as ca_cache_append makes them).
+ * A token whose page_table entry is no page reads as zeros.  Rows of no sequence, of tokens before a sequence's first and of those beyond the table are left as
+ * they are.  One launch on hip_stream; allocates nothing, never synchronises.
+ */
+int ca_cache_read(const ca_cache *cache, const ca_cache_batch *batch, void *k, void *v, void *hip_stream);
+
+/*
  * ca_cache_copy_pages: copies page src[i] to page dst[i] (DEVICE int32 [n]; all heads, keys, values and scales), for i < n: the shared last
  * page of a forked sequence, or the pages that a compaction moves.  No page is written twice, and none that is written is read by
  * another pair.  Pairs with an id outside [0, n_pages) are skipped.  One launch on hip_stream; allocates nothing, never synchronises.

@@ -101,6 +101,7 @@ def lib() -> ctypes.CDLL:
         L.ca_merge_partials.argtypes = [vp, i64, i32, vp, vp, i64, vp, vp, vp, vp, i32, i32, vp]
         L.ca_sum_partial_dq.argtypes = [vp, i64, i32, vp, i64, vp, i32, i32, vp]
         L.ca_cache_append.argtypes = [vp] * 5
+        L.ca_cache_read.argtypes = [vp] * 5
         L.ca_cache_attend.argtypes = [vp, vp, i32, ctypes.c_float, i64, i64, vp, vp, vp, vp, sz, vp]
         L.ca_cache_attend_workspace_bytes.argtypes = [vp, i32, ctypes.POINTER(sz)]
         L.ca_cache_copy_pages.argtypes = [vp, vp, vp, i64, vp]
@@ -457,6 +458,17 @@ def ca_cache_attend(cache, q, o, lse, q_start, kv_len, page_table, ws, window=No
     wp, n = (None, 0) if ws is None else (_on_cache(cache, ws, ws.shape, ws.dtype, "ws"), ws.numel() * ws.element_size())
     _check(lib().ca_cache_attend(cache.desc_ref, ctypes.byref(b), hq, softmax_scale, _count(window), _count(sinks), qp, op, lp, wp,
                                  n, _cache_stream(cache, stream)))
+
+
+def ca_cache_read(cache, k, v, q_start, kv_len, page_table, stream=None):
+    """The rows of the batch out of the cache: k and v (bf16 [rows, n_kv_heads, head_dim]; one of them may be None) are written."""
+    if k is None and v is None:
+        raise ValueError("k and v: one of them at least")
+    rows = (v if k is None else k).shape[0]
+    shape = (rows, cache.n_kv_heads, cache.head_dim)
+    kp, vp = (None if x is None else _on_cache(cache, x, shape, cache.bf16, name) for x, name in ((k, "k"), (v, "v")))
+    b = _cache_batch(cache, rows, q_start, kv_len, page_table)
+    _check(lib().ca_cache_read(cache.desc_ref, ctypes.byref(b), kp, vp, _cache_stream(cache, stream)))
 
 
 def ca_cache_copy_pages(cache, src, dst, stream=None):
