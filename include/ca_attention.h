@@ -269,6 +269,25 @@ int ca_cache_attend(const ca_cache *cache, const ca_cache_batch *batch, int32_t 
 int ca_cache_attend_workspace_bytes(const ca_cache *cache, int32_t n_q_heads, size_t *bytes);
 
 /*
+ * ca_cache_attend_shared: ca_cache_attend (without a window) where sequences have their first pages in common, as forks of one prompt have: those are attended once
+ * for all rows of a group.  Group g: sequences group_start[g] .. group_start[g + 1] - 1, the first prefix_pages[g] entries of whose page_table
+ * rows are the same (those of the group's first sequence are taken for all); sequences of no group, and groups of 0 pages, share nothing.  The arrays are DEVICE
+ * memory, read when the kernels run.  What is shared are whole pages that every row of a sequence sees: a sequence of which kv_len - (its
+ * rows) is less than 64 prefix_pages is attended by itself, from its own entries.  Results are those of ca_cache_attend but for the order of sums and the rounding of P, which goes
+ * by the rows per group here and there by the rows per sequence: of the shared tokens bf16 where a group has more than 32 rows on average (queries times heads of a KV head).
+ * ws: device workspace of ca_cache_attend_shared_workspace_bytes (of this many rows or fewer), 256-byte aligned, written; calls that may overlap in time need one each.
+ * Two launches on hip_stream; allocates nothing, never synchronises, bit-reproducible.
+ */
+typedef struct {
+  int32_t n_groups;            /* at most n_seqs */
+  const int32_t *group_start;  /* [n_groups + 1], not descending */
+  const int32_t *prefix_pages; /* [n_groups] */
+} ca_cache_groups;
+int ca_cache_attend_shared(const ca_cache *cache, const ca_cache_batch *batch, const ca_cache_groups *groups, int32_t n_q_heads,
+                           float softmax_scale, const void *q, void *o, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+int ca_cache_attend_shared_workspace_bytes(const ca_cache *cache, int32_t n_q_heads, int64_t total_rows, size_t *bytes);
+
+/*
  * ca_cache_read: the rows of the batch back out of the pages of their sequences: k and v (device bf16 [total_rows][n_kv_heads][head_dim], 16-byte aligned; one of them may be
  * NULL) receive code * scale, rounded once (NaN where the code is; exact, but for values below bf16's normal range, where scales are powers of two, as ca_cache_append makes them).
  * A token whose page_table entry is no page reads as zeros.  Rows of no sequence, of tokens before a sequence's first and of those beyond the table are left as

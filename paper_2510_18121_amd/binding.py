@@ -49,6 +49,12 @@ class CacheBatch(ctypes.Structure):
                 ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
 
 
+class CacheGroups(ctypes.Structure):
+    """ca_cache_groups of include/ca_attention.h."""
+
+    _fields_ = [("n_groups", ctypes.c_int32), ("group_start", ctypes.c_void_p), ("prefix_pages", ctypes.c_void_p)]
+
+
 class RotateTensor(ctypes.Structure):
     """ca_rotate_tensor of include/ca_attention.h."""
 
@@ -102,6 +108,8 @@ def lib() -> ctypes.CDLL:
         L.ca_sum_partial_dq.argtypes = [vp, i64, i32, vp, i64, vp, i32, i32, vp]
         L.ca_cache_append.argtypes = [vp] * 5
         L.ca_cache_read.argtypes = [vp] * 5
+        L.ca_cache_attend_shared.argtypes = [vp, vp, vp, i32, ctypes.c_float, vp, vp, vp, vp, sz, vp]
+        L.ca_cache_attend_shared_workspace_bytes.argtypes = [vp, i32, i64, ctypes.POINTER(sz)]
         L.ca_cache_attend.argtypes = [vp, vp, i32, ctypes.c_float, i64, i64, vp, vp, vp, vp, sz, vp]
         L.ca_cache_attend_workspace_bytes.argtypes = [vp, i32, ctypes.POINTER(sz)]
         L.ca_cache_copy_pages.argtypes = [vp, vp, vp, i64, vp]
@@ -458,6 +466,31 @@ def ca_cache_attend(cache, q, o, lse, q_start, kv_len, page_table, ws, window=No
     wp, n = (None, 0) if ws is None else (_on_cache(cache, ws, ws.shape, ws.dtype, "ws"), ws.numel() * ws.element_size())
     _check(lib().ca_cache_attend(cache.desc_ref, ctypes.byref(b), hq, softmax_scale, _count(window), _count(sinks), qp, op, lp, wp,
                                  n, _cache_stream(cache, stream)))
+
+
+def ca_cache_attend_shared(cache, q, o, lse, q_start, kv_len, page_table, group_start, prefix_pages, ws, softmax_scale=0.0, stream=None):
+    """ca_cache_attend where groups of sequences share their first pages, which are attended once for all rows of a group: group g has the sequences
+    group_start[g] .. group_start[g + 1] - 1, and their first prefix_pages[g] pages are the same (device int32; cache.Sequences.groups).
+    ws: alloc_shared_workspace."""
+    rows, hq, _ = shape = q.shape
+    qp = _on_cache(cache, q, (rows, hq, cache.head_dim), cache.bf16, "q")
+    op = _on_cache(cache, o, shape, cache.bf16, "o")
+    lp = None if lse is None else _on_cache(cache, lse, (hq, rows), cache.f32, "lse")
+    b = _cache_batch(cache, rows, q_start, kv_len, page_table)
+    n = prefix_pages.shape[0]
+    g = CacheGroups(n, _on_cache(cache, group_start, (n + 1,), cache.i32, "group_start"), _on_cache(cache, prefix_pages, (n,), cache.i32, "prefix_pages"))
+    wp, wn = (None, 0) if ws is None else (_on_cache(cache, ws, ws.shape, ws.dtype, "ws"), ws.numel() * ws.element_size())
+    _check(lib().ca_cache_attend_shared(cache.desc_ref, ctypes.byref(b), ctypes.byref(g), hq, softmax_scale, qp, op, lp, wp, wn,
+                                        _cache_stream(cache, stream)))
+
+
+def alloc_shared_workspace(cache, n_q_heads, rows, device=None):
+    """A torch uint8 buffer big enough for ca_cache_attend_shared on that cache with up to that many rows.  Calls that may overlap in time need one
+    each."""
+    import torch
+    n = ctypes.c_size_t()
+    _check(lib().ca_cache_attend_shared_workspace_bytes(cache.desc_ref, operator.index(n_q_heads), operator.index(rows), ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=cache.device if device is None else device)
 
 
 def ca_cache_read(cache, k, v, q_start, kv_len, page_table, stream=None):

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libca_attention.so")
 SOURCES = ["ca_plan.cpp", "ca_api.hip", "ca_fwd.hip", "ca_bwd.hip", "ca_bwd_fused.hip", "ca_window.hip", "ca_cache.hip", "ca_cache_read.hip",
-           "ca_merge.hip", "ca_rotate.hip", "ca_calib.hip"]
+           "ca_cache_shared.hip", "ca_merge.hip", "ca_rotate.hip", "ca_calib.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # packed fp32 VALU forms are kept out of the generated code on purpose

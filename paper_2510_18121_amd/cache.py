@@ -155,15 +155,58 @@ class Sequences:
         """q_start, kv_len and page_table (int32) of a call with the last rows[i] tokens of seqs[i]."""
         return self._arrays([self.pages[s] for s in seqs], [self.lengths[s] for s in seqs], rows, device)
 
-    def _arrays(self, pages, lengths, rows, device):
+    def groups(self, seqs, rows, device=None):
+        """group_start and prefix_pages (int32) of binding.ca_cache_attend_shared, for a call with the last rows[i] tokens of seqs[i]: neighbours in `seqs`
+        that share their first pages make up groups, so that the most pages are read once instead of again.  (The arrays stay right
+        as long as the same sequences grow: they are made when sequences come and go.)"""
+        seqs, rows = list(seqs), [operator.index(n) for n in rows]
+        if len(seqs) != len(rows):
+            raise ValueError("groups: one count of rows for each of the sequences")
+        n = len(seqs)
+        whole = [max(0, self.lengths[s] - r) // PAGE_TOKENS for s, r in zip(seqs, rows)]  # pages that all rows see
+        common = [0]  # of each sequence with the one before it
+        for i in range(1, n):
+            a, b, m = self.pages[seqs[i - 1]], self.pages[seqs[i]], 0
+            top = min(whole[i - 1], whole[i])
+            if a[:top] == b[:top]:
+                m = top
+            else:
+                while a[m] == b[m]:
+                    m += 1
+            # (a page that a window has left is in nobody's hands)
+            common.append(next((j for j in range(m) if a[j] < 0), m))
+        # best[i]: pages saved among the first i sequences, the last group of which begins at at[i]; a group of m saves m - 1 times its least common run
+        common = np.array(common, np.int64)
+        best, at, least = np.zeros(n + 1, np.int64), list(range(-1, n)), [0] * (n + 1)
+        nothing = 0  # the last sequence that shares nothing with the one before it
+        for i in range(1, n + 1):
+            best[i] = best[i - 1]
+            if common[i - 1] == 0:
+                nothing = i - 1
+            run = np.minimum.accumulate(common[i - 1:nothing:-1])  # of groups that begin at i - 2, i - 3, ..
+            if run.size:
+                saved = best[nothing:i - 1][::-1] + np.arange(1, run.size + 1) * run
+                k = int(saved.argmax())
+                if saved[k] > best[i]:
+                    best[i], at[i], least[i] = saved[k], i - 2 - k, int(run[k])
+        starts, pages, i = [n], [], n
+        while i > 0:
+            starts.append(at[i]), pages.append(least[i])
+            i = at[i]
+        return self._on(device, np.array(starts[::-1], np.int32), np.array(pages[::-1], np.int32))
+
+    def _on(self, device, *arrays):
         import torch
+        if device is None:
+            device = self.caches[0].device if self.caches else "cpu"
+        return tuple(torch.from_numpy(x).to(device) for x in arrays)
+
+    def _arrays(self, pages, lengths, rows, device):
         table = np.full((len(pages), max([len(x) for x in pages], default=0)), -1, np.int32)
         for i, x in enumerate(pages):
             table[i, :len(x)] = x
         start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
-        if device is None:
-            device = self.caches[0].device if self.caches else "cpu"
-        return tuple(torch.from_numpy(x).to(device) for x in (start, np.array(lengths, np.int32), table))
+        return self._on(device, start, np.array(lengths, np.int32), table)
 
     def compact(self):
         """Moves the pages in use to the front of the pool, on the current stream; returns how many are in use.  Page tables made before are

@@ -25,12 +25,49 @@ struct SeqArgs {
 };
 struct Seq {
   int row0, n, len;  // rows row0 .. row0 + n - 1, at positions len - n .. len - 1
+  int more;          // PREFIX: whose row of the table has the pages; TAIL: pages that are left out
 };
-__device__ __forceinline__ Seq seq_of(const SeqArgs &a, int s) {
+// Where groups of sequences share their first pages, attention runs over two kinds of sequences in place of the batch's (WHOLE) own.  PREFIX: each
+// group's rows, all of which see all of the shared pages.  TAIL: each sequence's rows over the tokens behind them, counted from there.  A sequence of
+// which some row would see less than all of the shared pages takes no part: its tail is all of it, and what PREFIX makes of its rows is left.
+enum Part { WHOLE, PREFIX, TAIL };
+struct GroupedSeqs : SeqArgs {
+  const int32_t *group_start, *prefix_pages;
+  int n_groups;
+};
+template <Part P, class A>
+__device__ __forceinline__ int n_entries(const A &a) {
+  if constexpr (P == PREFIX) return a.n_groups;
+  else return a.n_seqs;
+}
+template <Part P = WHOLE, class A>
+__device__ __forceinline__ Seq seq_of(const A &a, int s) {
   Seq q;
+  if constexpr (P == PREFIX) {
+    q.more = min(max(a.group_start[s], 0), a.n_seqs);
+    const int end = min(max(a.group_start[s + 1], q.more), a.n_seqs);
+    q.row0 = min(max(a.q_start[q.more], 0), a.total);
+    q.n = min(max(a.q_start[end], q.row0), a.total) - q.row0;
+    q.len = min(max(a.prefix_pages[s], 0), a.width) * PAGE;
+    if (q.len == 0 || end == q.more) q.n = 0;
+    return q;
+  }
   q.row0 = min(max(a.q_start[s], 0), a.total);
   q.n = min(max(a.q_start[s + 1], q.row0), a.total) - q.row0;
   q.len = min(max(a.kv_len[s], 0), a.width * PAGE);
+  q.more = 0;
+  if constexpr (P == TAIL) {
+    if (a.n_groups > 0) {
+      int lo = 0, hi = a.n_groups;  // the last group that begins at s or before
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.group_start[mid] <= s) lo = mid;
+        else hi = mid;
+      }
+      const int shared = a.group_start[lo] <= s && s < a.group_start[lo + 1] ? min(max(a.prefix_pages[lo], 0), a.width) : 0;
+      if (q.len - q.n >= shared * PAGE) q.more = shared, q.len -= shared * PAGE;
+    }
+  }
   return q;
 }
 
@@ -51,32 +88,42 @@ __device__ __forceinline__ int wave_prefix(int x) {  // inclusive
   x = add_lanes<0x142, 0xA>(x);         // the last lane of the 16 before
   return add_lanes<0x143, 0xC>(x);      // ... and of the 32 before
 }
-constexpr size_t seq_table_bytes(int n_seqs) { return n_seqs <= 64 ? 0 : 64 + size_t(n_seqs + 4) / 4 * 16 * 4; }
-struct SeqTable {
+constexpr size_t seq_table_bytes(int n_seqs, Part part = WHOLE) {
+  return n_seqs <= 64 ? 0 : 64 + size_t(n_seqs + 4) / 4 * 16 * (part == TAIL ? 5 : 4);
+}
+template <Part P>
+struct SeqTableOf {
   int n_seqs;
   Seq mine;         // up to 64 sequences: of this lane,
   int upto;         // and the units up to it and with it
-  int *wave_sums, *pre, *row0, *n, *len;  // more
+  int *wave_sums, *pre, *row0, *n, *len, *more;  // more than 64
+  const int32_t *group_start;
+  int last;
 
   // for all threads of the workgroup (T); returns the sum of all units
-  template <int T, class F>
-  __device__ __forceinline__ int fill(void *lds, const SeqArgs &a, F units) {
+  template <int T, class A, class F>
+  __device__ __forceinline__ int fill(void *lds, const A &a, F units) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    n_seqs = a.n_seqs;
+    n_seqs = n_entries<P>(a);
+    if constexpr (P == PREFIX) {
+      if (n_seqs == 0) return 0;
+      group_start = a.group_start, last = a.n_seqs;
+    }
     if (n_seqs <= 64) {
-      mine = seq_of(a, min(lane, n_seqs - 1));
+      mine = seq_of<P>(a, min(lane, n_seqs - 1));
       upto = wave_prefix(lane < n_seqs ? units(mine) : 0);
       return __builtin_amdgcn_readlane(upto, 63);
     }
     const int stride = (n_seqs + 4) / 4 * 4;
-    wave_sums = static_cast<int *>(lds), pre = wave_sums + 16, row0 = pre + stride, n = row0 + stride, len = n + stride;
+    wave_sums = static_cast<int *>(lds), pre = wave_sums + 16, row0 = pre + stride, n = row0 + stride, len = n + stride, more = len + stride;
     int carry = 0;
     for (int base = 0; base < n_seqs; base += T) {
       const int i = base + int(threadIdx.x);
       int x = 0;
       if (i < n_seqs) {
-        const Seq q = seq_of(a, i);
+        const Seq q = seq_of<P>(a, i);
         row0[i] = q.row0, n[i] = q.n, len[i] = q.len;
+        if (P == TAIL) more[i] = q.more;
         x = units(q);
       }
       x = wave_prefix(x);
@@ -96,8 +143,11 @@ struct SeqTable {
     return __builtin_amdgcn_readfirstlane(carry);
   }
   __device__ __forceinline__ Seq at(int s) const {
-    if (n_seqs <= 64) return {__builtin_amdgcn_readlane(mine.row0, s), __builtin_amdgcn_readlane(mine.n, s), __builtin_amdgcn_readlane(mine.len, s)};
-    return {__builtin_amdgcn_readfirstlane(row0[s]), __builtin_amdgcn_readfirstlane(n[s]), __builtin_amdgcn_readfirstlane(len[s])};
+    if (n_seqs <= 64)
+      return {__builtin_amdgcn_readlane(mine.row0, s), __builtin_amdgcn_readlane(mine.n, s), __builtin_amdgcn_readlane(mine.len, s),
+              P == WHOLE ? 0 : __builtin_amdgcn_readlane(mine.more, s)};
+    return {__builtin_amdgcn_readfirstlane(row0[s]), __builtin_amdgcn_readfirstlane(n[s]), __builtin_amdgcn_readfirstlane(len[s]),
+            P == WHOLE ? 0 : __builtin_amdgcn_readfirstlane(P == TAIL ? more[s] : min(max(group_start[s], 0), last))};
   }
   __device__ __forceinline__ int before(int s) const {  // units of the sequences before s
     if (n_seqs <= 64) return s == 0 ? 0 : __builtin_amdgcn_readlane(upto, s - 1);
@@ -113,7 +163,19 @@ struct SeqTable {
     }
     return __builtin_amdgcn_readfirstlane(lo);
   }
+  __device__ __forceinline__ int find_row(int row) const {  // the last one that begins at the row or before, or -1
+    if (n_seqs <= 64) return __builtin_popcountll(__ballot(int(threadIdx.x & 63) < n_seqs && mine.row0 <= row)) - 1;
+    if (row0[0] > row) return -1;
+    int lo = 0, hi = n_seqs;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (row0[mid] <= row) lo = mid;
+      else hi = mid;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+  }
 };
+using SeqTable = SeqTableOf<WHOLE>;
 
 // ------------------------------------------------------------------------------------------------ calls
 inline int fail(int code, const std::string &msg) {

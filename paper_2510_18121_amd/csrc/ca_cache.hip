@@ -40,13 +40,13 @@ namespace ca {
 template <int D, int NR, int W>
 __global__ __launch_bounds__(64 * W, NR == 1 || D == 64 ? 2 : 1) void ca_cache_attend_kernel(const AttendArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  attend_workgroup<D, NR, W>(a, smem, blockIdx.x, blockIdx.y, gridDim.y);
+  attend_workgroup<WHOLE, D, NR, W>(a, smem, blockIdx.x, blockIdx.y, gridDim.y, a.parts, a.by_workers);
 }
 
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_cache_chunk_kernel(const AttendArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  chunk_workgroup<D>(a, smem, blockIdx.x, blockIdx.y, gridDim.y);
+  chunk_workgroup<WHOLE, D>(a, smem, blockIdx.x, blockIdx.y, gridDim.y, a.parts, a.by_workers);
 }
 
 // Adds up the parts of the tiles that were cut, in their order: a wave takes RW rows, and two (four) parts of each at a time.  4 to 5 us, of which

@@ -7,8 +7,9 @@
 namespace ca {
 
 // ------------------------------------------------------------------------------------------------ attention
-struct AttendArgs {
-  SeqArgs s;
+template <class S>
+struct AttendArgsOf {
+  S s;
   const uint8_t *k, *v;
   const float *k_scale, *v_scale;
   const bf16_t *q;
@@ -25,6 +26,11 @@ struct AttendArgs {
 
   __device__ __forceinline__ int token_of(int row) const { return G == 1 ? row : int(__umulhi(uint32_t(row), by_g)); }
 };
+using AttendArgs = AttendArgsOf<SeqArgs>;
+// PREFIX and TAIL: sums of a row and head, {m, l} behind them, of tiles that one worker had from their first page to their last.
+struct SharedArgs : AttendArgsOf<GroupedSeqs> {
+  float *row_sums[2], *row_ml[2];  // [total_rows][n_q_heads][D], [..][2]
+};
 
 // Rows of a sequence and KV head, token by token and then by head of the group, make up tiles of R = 16 NR; a unit of work is a page
 // of a tile.  The units of all sequences, in order, are dealt to the workers in equal runs, whatever the sequences' lengths
@@ -34,6 +40,7 @@ struct AttendArgs {
 // later ones, which are passed over: a prompt from its first token is dealt unevenly (32/8 heads of 128: one of 2048 rows 91 us, sixteen 1010; their flops
 // need 25 and 407), one behind a long context is not.
 constexpr int CUT = 16;
+constexpr int FAR = 1 << 29;  // the position of rows that see every token there is
 __device__ __forceinline__ int tile_pages(int len, int R, int G, int window, int sinks) {
   const int pages = (len + PAGE - 1) / PAGE;
   if (window >= len) return max(1, pages);
@@ -57,14 +64,15 @@ __device__ __forceinline__ int quotient(int x, int y) {
 }
 
 // The workers' shares of the units: worker w has units bound(w) .. bound(w + 1) - 1.
+template <Part P>
 struct WorkSplit {
-  SeqTable tab;
+  SeqTableOf<P> tab;
   int total, run, R, G, window, sinks;
-  template <int T>
-  __device__ __forceinline__ void make(void *lds, const AttendArgs &a, int rows, int n_workers, int least) {
+  template <int T, class A>
+  __device__ __forceinline__ void make(void *lds, const A &a, int rows, int n_workers, float by_workers, int least) {
     R = rows, G = a.G, window = a.window, sinks = a.sinks;
-    total = tab.fill<T>(lds, a.s, [&](const Seq &q) { return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, window, sinks); });
-    run = max(least, n_workers == 1 ? total : __builtin_amdgcn_readfirstlane(int(float(total) * a.by_workers)) + 1);
+    total = tab.template fill<T>(lds, a.s, [&](const Seq &q) { return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, window, sinks); });
+    run = max(least, n_workers == 1 ? total : __builtin_amdgcn_readfirstlane(int(float(total) * by_workers)) + 1);
   }
   __device__ __forceinline__ int bound(int w) const {
     const int u = min(w * run, total);
@@ -126,17 +134,17 @@ struct AttendShape {
 // Single tokens and the like: tiles of 16 NR rows.  A wave has pages of its own, every W-th of the worker's run: codes come to registers
 // in 16-byte runs, the next page's K while this one's scores are multiplied, its V behind this one's (a page further ahead took 5 % longer on 64 sequences
 // of about 4096 tokens, 7 % on 4 of 130K).  No barrier before the waves' sums meet.
-template <int D, int NR, int W>
-__device__ __forceinline__ void attend_workgroup(const AttendArgs &a, char *smem, int hk, int worker, int n_workers) {
+template <Part P, int D, int NR, int W, class A>
+__device__ __forceinline__ void attend_workgroup(const A &a, char *smem, int hk, int worker, int n_workers, float *parts, float by_workers) {
   using S = AttendShape<D, NR, W>;
   constexpr int R = S::R, NH = D / 64, NB = D / 16;
   float *const merge = reinterpret_cast<float *>(smem), *const merge_ml = merge + W * R * S::ROW;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j4 = lane >> 4, li = lane & 15;
   const int G = a.G;
-  WorkSplit split;
-  split.make<64 * W>(smem + S::MERGE, a, R, n_workers, W);
-  const SeqTable &tab = split.tab;
+  WorkSplit<P> split;
+  split.template make<64 * W>(smem + S::MERGE, a, R, n_workers, by_workers, W);
+  const SeqTableOf<P> &tab = split.tab;
   const int begin = split.bound(worker), end = split.bound(worker + 1);
   int4 head = {0, 0, 0, 0};
   const uint32_t k_lane = uint32_t(16 * (li >> 2) + (li & 3)) * D + 16 * j4, v_lane = uint32_t(li) * PAGE + 16 * j4;
@@ -149,7 +157,7 @@ __device__ __forceinline__ void attend_workgroup(const AttendArgs &a, char *smem
     const int n = min(end - u, per_tile - first);
     u += n;
     // the rows
-    const int last_row = min((tile + 1) * R, q.n * G) - 1, pos0 = q.len - q.n;
+    const int last_row = min((tile + 1) * R, q.n * G) - 1, pos0 = P == PREFIX ? FAR : q.len - q.n;
     const int p0 = pos0 + a.token_of(tile * R), p1 = pos0 + a.token_of(last_row);  // of the tile's first and last row
     const int from = max(0, p0 - a.window + 1);                                    // the first key of a window that some row has
     const int n_sink = min((a.sinks + PAGE - 1) / PAGE, from / PAGE);
@@ -170,7 +178,7 @@ __device__ __forceinline__ void attend_workgroup(const AttendArgs &a, char *smem
       if (base + lane < n_mine) {
         const int i = first + wave + W * (base + lane);
         at = i < n_sink ? i : from / PAGE + i - n_sink;
-        if (at * PAGE <= p1) id = a.s.table[size_t(s) * a.s.width + at];
+        if (at * PAGE <= p1) id = a.s.table[size_t(P == PREFIX ? q.more : s) * a.s.width + (P == TAIL ? q.more : 0) + at];
         if (id >= a.s.n_pages) id = -1;
       }
       if (base == 0) {
@@ -293,7 +301,7 @@ __device__ __forceinline__ void attend_workgroup(const AttendArgs &a, char *smem
     __syncthreads();
     const bool whole = n == per_tile;
     const int slot = first == 0 ? 1 : 0;
-    float *const part = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2));
+    float *const part = parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2));
     if (!whole && slot == 1) head = int4{(u - n + per_tile - 1) / split.run - worker + 1, q.row0, tile * R, last_row};
     float factor[NR];
 #pragma unroll
@@ -334,6 +342,14 @@ __device__ __forceinline__ void attend_workgroup(const AttendArgs &a, char *smem
           continue;
         }
         const int token = a.token_of(at), h = hk * G + at - token * G;
+        if constexpr (P != WHOLE) {
+          if (P == PREFIX || q.more > 0) {
+            const size_t i = size_t(q.row0 + token) * a.hq + h;
+            *reinterpret_cast<f32x4 *>(a.row_sums[P == TAIL] + i * D + c0 + col) = y;
+            if (stats) a.row_ml[P == TAIL][2 * i] = top, a.row_ml[P == TAIL][2 * i + 1] = all;
+            continue;
+          }
+        }
         const float inv = all == 0.f ? 0.f : 1.0f / all;  // (a row that sees nothing: O = 0, LSE = -inf)
         *reinterpret_cast<u32x2 *>(a.o + (size_t(q.row0 + token) * a.hq + h) * D + c0 + col) =
             u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
@@ -342,7 +358,7 @@ __device__ __forceinline__ void attend_workgroup(const AttendArgs &a, char *smem
       if (c0 + S::CW < D || u < end) __syncthreads();
     }
   }
-  if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
+  if (P == WHOLE && threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
 }
 
 // ------------------------------------------------------------------------------------------------ attention of chunks
@@ -360,17 +376,17 @@ struct ChunkSmem {
   static_assert(4 * PATCH_BYTES <= TOTAL, "patches fit in the stages");
 };
 
-template <int D>
-__device__ __forceinline__ void chunk_workgroup(const AttendArgs &a, char *smem, int hk, int worker, int n_workers) {
+template <Part P, int D, class A>
+__device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, int hk, int worker, int n_workers, float *parts, float by_workers) {
   using S = ChunkSmem<D>;
   constexpr int R = 128, NK = D / 32, NB = D / 16, ROWB = 2 * D, NL = D / 64;  // NL: loads of K, and of V, of a wave per page
   const uint32_t lds0 = (uint32_t)(uintptr_t)(CA_LDS char *)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j4 = lane >> 4, li = lane & 15;
   const int G = a.G;
-  WorkSplit split;
-  split.make<256>(smem + S::TOTAL, a, R, n_workers, 4);
-  const SeqTable &tab = split.tab;
+  WorkSplit<P> split;
+  split.template make<256>(smem + S::TOTAL, a, R, n_workers, by_workers, 4);
+  const SeqTableOf<P> &tab = split.tab;
   const int begin = split.bound(worker), end = split.bound(worker + 1);
   int4 head = {0, 0, 0, 0};
   // where the wave's codes come from in a page, and where they go: K row i of tile `wave` is key 16 (i / 4) + 4 wave + i % 4
@@ -394,7 +410,7 @@ __device__ __forceinline__ void chunk_workgroup(const AttendArgs &a, char *smem,
     const int n = min(end - u, per_tile - first);
     u += n;
     // the rows: of the tile, and of the wave (w..)
-    const int last_row = min((tile + 1) * R, q.n * G) - 1, pos0 = q.len - q.n, row_w = tile * R + 32 * wave;
+    const int last_row = min((tile + 1) * R, q.n * G) - 1, pos0 = P == PREFIX ? FAR : q.len - q.n, row_w = tile * R + 32 * wave;
     const int p0 = pos0 + a.token_of(tile * R), p1 = pos0 + a.token_of(last_row);
     const int from = max(0, p0 - a.window + 1), n_sink = min((a.sinks + PAGE - 1) / PAGE, from / PAGE);
     const int p0w = pos0 + a.token_of(row_w), p1w = row_w <= last_row ? pos0 + a.token_of(min(row_w + 31, last_row)) : -1;
@@ -423,7 +439,7 @@ __device__ __forceinline__ void chunk_workgroup(const AttendArgs &a, char *smem,
       if (base + lane < n) {
         const int i = first + base + lane;
         at = i < n_sink ? i : from / PAGE + i - n_sink;
-        if (at * PAGE <= p1) id = a.s.table[size_t(s) * a.s.width + at];
+        if (at * PAGE <= p1) id = a.s.table[size_t(P == PREFIX ? q.more : s) * a.s.width + (P == TAIL ? q.more : 0) + at];
         if (id >= a.s.n_pages) id = -1;
         if (id >= 0) ks = fmaxf(a.k_scale[size_t(id) * a.hkv + hk] * a.c, LEAST_SCALE), vs = a.v_scale[size_t(id) * a.hkv + hk];
         // The scale of V goes into the exponent: exp2(x - m + lv) = P vs, and their sum times iv is that of P.  Not where that could
@@ -588,7 +604,23 @@ __device__ __forceinline__ void chunk_workgroup(const AttendArgs &a, char *smem,
       }
     }
     const float sum[2] = {quad_sum(l[0]), quad_sum(l[1])};
-    if (n == per_tile) {
+    bool joined = false;  // (with the other part of what its rows see)
+    if constexpr (P != WHOLE) {
+      joined = n == per_tile && (P == PREFIX || q.more > 0);
+      if (joined) {
+#pragma unroll
+        for (int rg = 0; rg < 2; ++rg) {
+          const int r = row_w + 16 * rg + li, i = a.token_of(r);
+          if (r > last_row) continue;
+          const size_t at = size_t(q.row0 + i) * a.hq + hk * G + r - i * G;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4 *>(a.row_sums[P == TAIL] + at * D + 16 * b + 4 * j4) = acc[b][rg];
+          if (j4 == 0) a.row_ml[P == TAIL][2 * at] = m[rg], a.row_ml[P == TAIL][2 * at + 1] = sum[rg];
+        }
+      }
+    }
+    if (joined) {
+    } else if (n == per_tile) {
       const float f0 = sum[0] == 0.f ? 0.f : 1.0f / sum[0], f1 = sum[1] == 0.f ? 0.f : 1.0f / sum[1];
       store_tile16_as_lines<0>(lds0 + wave * PATCH_BYTES, acc, f0, f1, lane, [&](int p) __attribute__((always_inline)) -> bf16_t * {
         const int r = row_w + p, i = a.token_of(r);
@@ -600,17 +632,17 @@ __device__ __forceinline__ void chunk_workgroup(const AttendArgs &a, char *smem,
     } else {
       const int slot = first == 0 ? 1 : 0;
       if (slot == 1) head = int4{(u - n + per_tile - 1) / split.run - worker + 1, q.row0, tile * R, last_row};
-      float *const part = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2)) + 32 * wave * D;
+      float *const part = parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2)) + 32 * wave * D;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int rg = 0; rg < 2; ++rg) *reinterpret_cast<f32x4 *>(part + (16 * rg + li) * D + 16 * b + 4 * j4) = acc[b][rg];
-      float *const ml = a.parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2)) + R * D + 64 * wave;
+      float *const ml = parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2)) + R * D + 64 * wave;
       if (lane < 32) ml[2 * lane] = lane < 16 ? m[0] : m[1], ml[2 * lane + 1] = lane < 16 ? sum[0] : sum[1];
     }
     if (u < end) __syncthreads();  // the patches lie in the stages
   }
-  if (threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
+  if (P == WHOLE && threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
 }
 
 // ------------------------------------------------------------------------------------------------ launches

@@ -1,0 +1,239 @@
+// Attention over the cache where groups of sequences share their first pages (forks of one prompt): those are attended once for all rows of
+// a group, the tokens behind them sequence by sequence, and a row's two results are joined.
+//
+// Of a row the keys are split into the shared ones (P) and the others (T): with L the log-sum-exp over each,
+//   O = (exp(L_P) O_P + exp(L_T) O_T) / (exp(L_P) + exp(L_T)).
+// Without sharing the codes of the prefix are read once per sequence, 2 D bytes per (token, KV head) each time, and that is what single tokens cost.
+// Here the rows of the whole group make up tiles of 128 rows (or 16, 32 where there are few), to which a page is fetched once: the prefix is
+// bound by the matrix products, 4 D flops per (row, head, token), and the tails by reading them.  Both go on side by side, in one launch of
+// workgroups of either kind (ca_cache_attend.h); a second one joins the results and the parts of the tiles that were cut.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <sstream>
+
+#include "ca_cache.h"
+#include "ca_cache_attend.h"
+#include "ca_device.h"
+#include "ca_internal.h"
+#include "ca_launch.h"
+
+namespace ca {
+
+struct SharedLaunch {
+  SharedArgs a;
+  float *parts[2];      // PREFIX, TAIL
+  int workers[2];       // per KV head
+  float by_workers[2];
+};
+
+template <Part P, int D, int NR, class A>
+__device__ __forceinline__ void tile_workgroup(const A &a, char *smem, int hk, int worker, int n_workers, float *parts, float by_workers) {
+  if constexpr (NR == 8) chunk_workgroup<P, D>(a, smem, hk, worker, n_workers, parts, by_workers);
+  else attend_workgroup<P, D, NR, 4>(a, smem, hk, worker, n_workers, parts, by_workers);
+}
+template <int D, int NR>
+constexpr int tile_bytes() {
+  if constexpr (NR == 8) return ChunkSmem<D>::TOTAL;
+  else return AttendShape<D, NR, 4>::MERGE;
+}
+
+// NP, NT: 16-row groups of a tile of the prefix and of the tails.
+template <int D, int NP, int NT>
+__global__ __launch_bounds__(256, (NP == 2 || NT == 2) && D == 128 ? 1 : 2) void ca_cache_shared_kernel(const SharedLaunch x) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int worker = blockIdx.y;
+  if (worker < x.workers[0]) tile_workgroup<PREFIX, D, NP>(x.a, smem, blockIdx.x, worker, x.workers[0], x.parts[0], x.by_workers[0]);
+  else tile_workgroup<TAIL, D, NT>(x.a, smem, blockIdx.x, worker - x.workers[0], x.workers[1], x.parts[1], x.by_workers[1]);
+}
+
+// What there is of a row's tile: the parts of the workers that had a run of its pages each, or one sum of the row.
+template <int D>
+struct RowParts {
+  const float *first, *others, *first_ml, *others_ml;
+  size_t stride;  // from a worker's part to the next one's
+  int n;
+  template <Part P, class A>
+  __device__ __forceinline__ void of(const A &a, const WorkSplit<P> &split, const float *parts, int n_workers, int entry, const Seq &q, int row, int h, int hk) {
+    const int R = split.R, G = a.G, r = (row - q.row0) * G + h - hk * G, tile = r / R, in_tile = r - tile * R;
+    const int per = tile_pages(q.len, R, G, a.window, a.sinks), u0 = split.tab.before(entry) + tile * per;
+    // (sequences that overlap, against their description, may have more units than are counted)
+    const int w0 = min(quotient(u0, split.run), n_workers - 1), w1 = min(quotient(u0 + per - 1, split.run), n_workers - 1);
+    if (per <= CUT || w0 == w1) {
+      const size_t i = size_t(row) * a.hq + h;
+      n = 1, first = a.row_sums[P == TAIL] + i * D, first_ml = a.row_ml[P == TAIL] + 2 * i;
+      return;
+    }
+    const size_t size = size_t(R) * (D + 2);
+    n = w1 - w0 + 1, stride = 2 * a.hkv * size;
+    const float *const p = parts + (size_t(2 * w0 + 1) * a.hkv + hk) * size;  // (the part of a tile that begins in a worker's run is its second)
+    first = p + in_tile * D, first_ml = p + R * D + 2 * in_tile;
+    const float *const o = parts + (size_t(2 * w0 + 2) * a.hkv + hk) * size;
+    others = o + in_tile * D, others_ml = o + R * D + 2 * in_tile;
+  }
+  __device__ __forceinline__ const float *sum(int i) const { return i == 0 ? first : others + (i - 1) * stride; }
+  __device__ __forceinline__ const float *ml(int i) const { return i == 0 ? first_ml : others_ml + (i - 1) * stride; }
+};
+
+// A wave takes a row and head at a time: D / 4 lanes to a part.
+template <int D, int NP, int NT>
+__global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x, int rows_of_wave) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  constexpr int LANES = D / 4, AT_A_TIME = 64 / LANES;
+  const SharedArgs &a = x.a;
+  WorkSplit<PREFIX> prefix;
+  WorkSplit<TAIL> tail;
+  prefix.template make<256>(smem, a, 16 * NP, x.workers[0], x.by_workers[0], 4);
+  tail.template make<256>(smem + seq_table_bytes(a.s.n_groups, PREFIX), a, 16 * NT, x.workers[1], x.by_workers[1], 4);
+  const int lane = threadIdx.x & 63, mine = lane / LANES, col = 4 * (lane % LANES);
+  const int64_t wave = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = int64_t(a.s.total) * a.hq;
+  for (int64_t at = wave * rows_of_wave; at < min(n, (wave + 1) * rows_of_wave); ++at) {
+    const int row = int(at / a.hq), h = int(at - int64_t(row) * a.hq), hk = h / a.G;
+    const int s = tail.tab.find_row(row);
+    if (s < 0) continue;
+    const Seq q = tail.tab.at(s);
+    if (row < q.row0 || row >= q.row0 + q.n) continue;
+    RowParts<D> t, p;
+    t.template of<TAIL>(a, tail, x.parts[1], x.workers[1], s, q, row, h, hk);
+    p.n = 0;
+    if (q.more > 0) {
+      const int g = prefix.tab.find_row(row);
+      const Seq of_group = prefix.tab.at(max(g, 0));
+      if (g >= 0 && row >= of_group.row0 && row < of_group.row0 + of_group.n)
+        p.template of<PREFIX>(a, prefix, x.parts[0], x.workers[0], g, of_group, row, h, hk);
+    } else if (t.n == 1) {
+      continue;  // it is done
+    }
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    float top = NO_MAX, sum = 0.f;
+    auto add = [&](float m, float l, const f32x4 &z) __attribute__((always_inline)) {
+      const float grown = fmaxf(top, m), old = fast_exp2(top - grown), w = fast_exp2(m - grown);
+      top = grown, sum = sum * old + w * l;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = y[e] * old + w * z[e];
+    };
+#pragma unroll 4
+    for (int i = mine; i < p.n + t.n; i += AT_A_TIME) {
+      const bool in_prefix = i < p.n;
+      const float *const z = in_prefix ? p.sum(i) : t.sum(i - p.n), *const ml = in_prefix ? p.ml(i) : t.ml(i - p.n);
+      add(ml[0], ml[1], *reinterpret_cast<const f32x4 *>(z + col));
+    }
+#pragma unroll
+    for (int o = LANES; o < 64; o <<= 1) {
+      f32x4 z;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[e] = __shfl_xor(y[e], o);
+      add(__shfl_xor(top, o), __shfl_xor(sum, o), z);
+    }
+    if (mine != 0) continue;
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    *reinterpret_cast<u32x2 *>(a.o + (size_t(row) * a.hq + h) * D + col) =
+        u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
+    if (col == 0 && a.lse) a.lse[size_t(h) * a.s.total + row] = 0.6931471805599453f * (top + fast_log2(sum));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ calls
+// Workers of both kinds together, per KV head: two workgroups of four waves to a CU.
+static int shared_workers(int hkv) { return std::max(2, N_CU * 2 / hkv); }
+static size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
+struct SharedBytes {
+  size_t parts, sums, ml;  // sums, ml: of each kind
+  size_t all() const { return parts + 2 * (sums + ml); }
+};
+static SharedBytes shared_bytes(int d, int hkv, int hq, int64_t rows) {
+  return {round_up(size_t(shared_workers(hkv)) * 2 * hkv * (128 * (d + 2)) * 4), round_up(size_t(rows) * hq * d * 4), round_up(size_t(rows) * hq * 2 * 4)};
+}
+
+template <int D, int NP, int NT>
+static int launch_shared(SharedLaunch &x, hipStream_t st) {
+  SharedArgs &a = x.a;
+  const int all = shared_workers(a.hkv);
+  x.workers[0] = a.s.n_groups > 0 ? all / 2 : 0, x.workers[1] = all - x.workers[0];
+  for (int i = 0; i < 2; ++i) x.by_workers[i] = 1.0001f / float(std::max(1, x.workers[i]));
+  x.parts[1] = x.parts[0] + size_t(x.workers[0]) * 2 * a.hkv * (16 * NP * (D + 2));
+  const size_t tables[2] = {seq_table_bytes(a.s.n_groups, PREFIX), seq_table_bytes(a.s.n_seqs, TAIL)};
+  const size_t bytes = std::max(tile_bytes<D, NP>() + tables[0], tile_bytes<D, NT>() + tables[1]);
+  auto kern = ca_cache_shared_kernel<D, NP, NT>;
+  auto join = ca_cache_join_kernel<D, NP, NT>;
+  int device = 0;
+  hipError_t e = hipGetDevice(&device);
+  static std::atomic<bool> done[2][16];
+  if (e == hipSuccess) e = set_smem(kern, int(std::max(tile_bytes<D, NP>(), tile_bytes<D, NT>()) + seq_table_bytes(MAX_SEQS, TAIL)), device, done[0]);
+  if (e == hipSuccess) e = set_smem(join, int(seq_table_bytes(MAX_SEQS, PREFIX) + seq_table_bytes(MAX_SEQS, TAIL)), device, done[1]);
+  if (e != hipSuccess) return launched("cache attention of groups", e);
+  hipLaunchKernelGGL(kern, dim3(unsigned(a.hkv), unsigned(all)), dim3(256), bytes, st, x);
+  const int64_t n = int64_t(a.s.total) * a.hq;
+  const int per = int(std::max<int64_t>(1, n / (N_CU * 64)));
+  hipLaunchKernelGGL(join, dim3(unsigned((n + 4 * per - 1) / (4 * per))), dim3(256), tables[0] + tables[1], st, x, per);
+  return launched("cache attention of groups", hipSuccess);
+}
+
+// Rows per tile, as in ca_cache_attend, from the average group and the average sequence.
+template <int D>
+static int shared_by_rows(SharedLaunch &x, hipStream_t st) {
+  const SharedArgs &a = x.a;
+  const int64_t rows = int64_t(a.s.total) * a.G, of_group = rows / std::max(1, a.s.n_groups), of_seq = rows / a.s.n_seqs;
+  if (of_seq > 32) return launch_shared<D, 8, 8>(x, st);
+  if (of_group > 32) return of_seq > 16 ? launch_shared<D, 8, 2>(x, st) : launch_shared<D, 8, 1>(x, st);
+  if (of_group > 16) return of_seq > 16 ? launch_shared<D, 2, 2>(x, st) : launch_shared<D, 2, 1>(x, st);
+  return launch_shared<D, 1, 1>(x, st);
+}
+
+}  // namespace ca
+
+extern "C" {
+
+int ca_cache_attend_shared_workspace_bytes(const ca_cache *c, int32_t n_q_heads, int64_t total_rows, size_t *bytes) {
+  using namespace ca;
+  if (const int rc = check_cache(c); rc != CA_OK) return rc;
+  if (!bytes) return fail(CA_ERR_INVALID_ARG, "output is null");
+  if (n_q_heads < 1 || n_q_heads % c->n_kv_heads != 0) return fail(CA_ERR_UNSUPPORTED, "n_q_heads is not a multiple of n_kv_heads");
+  if (total_rows < 0 || total_rows >= (int64_t(1) << 30)) return fail(CA_ERR_INVALID_ARG, "total_rows: not negative, below 2^30");
+  *bytes = shared_bytes(c->head_dim, c->n_kv_heads, n_q_heads, total_rows).all();
+  return CA_OK;
+}
+
+int ca_cache_attend_shared(const ca_cache *c, const ca_cache_batch *b, const ca_cache_groups *groups, int32_t n_q_heads, float softmax_scale,
+                           const void *q, void *o, float *lse, void *ws, size_t ws_bytes, void *hip_stream) {
+  using namespace ca;
+  if (const int rc = check_cache(c); rc != CA_OK) return rc;
+  if (const int rc = check_batch(b); rc != CA_OK) return rc;
+  if (!groups) return fail(CA_ERR_INVALID_ARG, "groups is null");
+  if (groups->n_groups < 0 || groups->n_groups > b->n_seqs) return fail(CA_ERR_INVALID_ARG, "groups: none, or up to as many as there are sequences");
+  if (groups->n_groups > 0 && (!groups->group_start || !groups->prefix_pages)) return fail(CA_ERR_INVALID_ARG, "groups: group_start or prefix_pages is null");
+  if (n_q_heads < 1 || n_q_heads % c->n_kv_heads != 0) return fail(CA_ERR_UNSUPPORTED, "n_q_heads is not a multiple of n_kv_heads");
+  if (b->n_seqs == 0 || b->total_rows == 0) return CA_OK;
+  if (!q || !o) return fail(CA_ERR_INVALID_ARG, "q or o is null");
+  if (!aligned(q) || !aligned(o)) return fail(CA_ERR_INVALID_ARG, "q or o is not 16-byte aligned");
+  const SharedBytes need = shared_bytes(c->head_dim, c->n_kv_heads, n_q_heads, b->total_rows);
+  if (!ws || ws_bytes < need.all() || reinterpret_cast<uintptr_t>(ws) % 256 != 0) {
+    std::ostringstream os;
+    os << "workspace of " << (ws ? ws_bytes : 0) << " bytes given, " << need.all() << " needed, 256-byte aligned";
+    return fail(CA_ERR_WORKSPACE, os.str());
+  }
+  const int64_t g = n_q_heads / c->n_kv_heads;
+  if ((b->total_rows * g / 16 + b->n_seqs) * std::max(1, b->table_width) >= int64_t(1) << 30)
+    return fail(CA_ERR_UNSUPPORTED, "batch: rows times pages beyond 2^30");
+  if ((b->total_rows * g + 128) * g >= int64_t(1) << 32) return fail(CA_ERR_UNSUPPORTED, "batch: rows times the square of the heads per KV head beyond 2^32");
+  SharedLaunch x = {};
+  SharedArgs &a = x.a;
+  static_cast<SeqArgs &>(a.s) = seq_args(c, b);
+  a.s.group_start = groups->group_start, a.s.prefix_pages = groups->prefix_pages, a.s.n_groups = groups->n_groups;
+  a.k = static_cast<const uint8_t *>(c->k), a.v = static_cast<const uint8_t *>(c->v), a.k_scale = c->k_scale, a.v_scale = c->v_scale;
+  a.q = static_cast<const bf16_t *>(q), a.o = static_cast<bf16_t *>(o), a.lse = lse;
+  a.hq = n_q_heads, a.hkv = c->n_kv_heads, a.G = int(g), a.by_g = uint32_t(((uint64_t(1) << 32) + uint64_t(g) - 1) / uint64_t(g));
+  a.window = 1 << 30, a.sinks = 0;
+  a.c = (softmax_scale > 0.f ? softmax_scale : c->head_dim == 128 ? 0.08838834764831845f : 0.125f) * 1.4426950408889634f;
+  char *at = static_cast<char *>(ws);
+  x.parts[0] = reinterpret_cast<float *>(at), at += need.parts;
+  for (int i = 0; i < 2; ++i) {
+    a.row_sums[i] = reinterpret_cast<float *>(at), at += need.sums;
+    a.row_ml[i] = reinterpret_cast<float *>(at), at += need.ml;
+  }
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  return c->head_dim == 128 ? shared_by_rows<128>(x, st) : shared_by_rows<64>(x, st);
+}
+
+}  // extern "C"
