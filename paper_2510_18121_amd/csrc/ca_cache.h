@@ -40,34 +40,66 @@ __device__ __forceinline__ int n_entries(const A &a) {
   if constexpr (P == PREFIX) return a.n_groups;
   else return a.n_seqs;
 }
-template <Part P = WHOLE, class A>
-__device__ __forceinline__ Seq seq_of(const A &a, int s) {
+__device__ __forceinline__ Seq seq_from(const SeqArgs &a, int start, int end, int len) {
   Seq q;
-  if constexpr (P == PREFIX) {
-    q.more = min(max(a.group_start[s], 0), a.n_seqs);
-    const int end = min(max(a.group_start[s + 1], q.more), a.n_seqs);
-    q.row0 = min(max(a.q_start[q.more], 0), a.total);
-    q.n = min(max(a.q_start[end], q.row0), a.total) - q.row0;
-    q.len = min(max(a.prefix_pages[s], 0), a.width) * PAGE;
-    if (q.len == 0 || end == q.more) q.n = 0;
-    return q;
-  }
-  q.row0 = min(max(a.q_start[s], 0), a.total);
-  q.n = min(max(a.q_start[s + 1], q.row0), a.total) - q.row0;
-  q.len = min(max(a.kv_len[s], 0), a.width * PAGE);
+  q.row0 = min(max(start, 0), a.total);
+  q.n = min(max(end, q.row0), a.total) - q.row0;
+  q.len = min(max(len, 0), a.width * PAGE);
   q.more = 0;
-  if constexpr (P == TAIL) {
-    if (a.n_groups > 0) {
-      int lo = 0, hi = a.n_groups;  // the last group that begins at s or before
+  return q;
+}
+__device__ __forceinline__ Seq seq_of(const SeqArgs &a, int s) { return seq_from(a, a.q_start[s], a.q_start[s + 1], a.kv_len[s]); }
+// What the groups' arrays say, and the first 64 entries of q_start, one per lane, so that what is looked up in them costs no further trips to memory.
+struct GroupLanes {
+  int start, end, pages;  // of this lane's group
+  int row;                // q_start of this lane
+  int n;                  // groups
+  __device__ __forceinline__ void load(const GroupedSeqs &a) {
+    const int lane = threadIdx.x & 63, g = min(lane, max(a.n_groups - 1, 0));
+    n = a.n_groups, start = end = pages = 0;
+    if (n > 0) start = a.group_start[g], end = a.group_start[g + 1], pages = a.prefix_pages[g];
+    row = a.q_start[min(lane, a.n_seqs)];
+  }
+  __device__ __forceinline__ int row_of(const GroupedSeqs &a, int i) const {  // q_start[i], of any lane's own i
+    if (a.n_seqs < 64) return __shfl(row, i);
+    return a.q_start[i];
+  }
+  // the pages that sequence s shares (for all lanes of a wave together)
+  __device__ __forceinline__ int shared_by(const GroupedSeqs &a, int s) const {
+    if (n == 0) return 0;
+    int lo = 0, hi = n;  // the last group that begins at s or before
+    int first, last, p;
+    if (n <= 64) {
+      for (int step = 32; step > 0; step >>= 1) {
+        if (step >= n) continue;
+        const int mid = min(lo + step, n - 1);
+        if (__shfl(start, mid) <= s) lo = mid;
+      }
+      first = __shfl(start, lo), last = __shfl(end, lo), p = __shfl(pages, lo);
+    } else {
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (a.group_start[mid] <= s) lo = mid;
         else hi = mid;
       }
-      const int shared = a.group_start[lo] <= s && s < a.group_start[lo + 1] ? min(max(a.prefix_pages[lo], 0), a.width) : 0;
-      if (q.len - q.n >= shared * PAGE) q.more = shared, q.len -= shared * PAGE;
+      first = a.group_start[lo], last = a.group_start[lo + 1], p = a.prefix_pages[lo];
     }
+    return first <= s && s < last ? min(max(p, 0), a.width) : 0;
   }
+};
+__device__ __forceinline__ Seq group_as_seq(const GroupedSeqs &a, const GroupLanes &l, int g) {
+  int start = l.start, end = l.end, pages = l.pages;
+  if (a.n_groups > 64) start = a.group_start[g], end = a.group_start[g + 1], pages = a.prefix_pages[g];
+  const int first = min(max(start, 0), a.n_seqs), last = min(max(end, first), a.n_seqs);
+  Seq q = seq_from(a, l.row_of(a, first), l.row_of(a, last), 0);
+  q.more = first, q.len = min(max(pages, 0), a.width) * PAGE;
+  if (q.len == 0 || last == first) q.n = 0;
+  return q;
+}
+__device__ __forceinline__ Seq tail_of(const GroupedSeqs &a, const GroupLanes &l, int s) {
+  Seq q = seq_of(a, s);
+  const int shared = l.shared_by(a, s);
+  if (q.len - q.n >= shared * PAGE) q.more = shared, q.len -= shared * PAGE;
   return q;
 }
 
@@ -99,7 +131,14 @@ struct SeqTableOf {
   int *wave_sums, *pre, *row0, *n, *len, *more;  // more than 64
   const int32_t *group_start;
   int last;
+  GroupLanes lanes;  // PREFIX and TAIL: loaded before
 
+  template <class A>
+  __device__ __forceinline__ Seq entry(const A &a, int i) const {
+    if constexpr (P == WHOLE) return seq_of(a, i);
+    else if constexpr (P == PREFIX) return group_as_seq(a, lanes, i);
+    else return tail_of(a, lanes, i);
+  }
   // for all threads of the workgroup (T); returns the sum of all units
   template <int T, class A, class F>
   __device__ __forceinline__ int fill(void *lds, const A &a, F units) {
@@ -110,7 +149,7 @@ struct SeqTableOf {
       group_start = a.group_start, last = a.n_seqs;
     }
     if (n_seqs <= 64) {
-      mine = seq_of<P>(a, min(lane, n_seqs - 1));
+      mine = entry(a, min(lane, n_seqs - 1));
       upto = wave_prefix(lane < n_seqs ? units(mine) : 0);
       return __builtin_amdgcn_readlane(upto, 63);
     }
@@ -120,8 +159,10 @@ struct SeqTableOf {
     for (int base = 0; base < n_seqs; base += T) {
       const int i = base + int(threadIdx.x);
       int x = 0;
+      Seq q;
+      if (P != WHOLE) q = entry(a, min(i, n_seqs - 1));  // (by all lanes)
       if (i < n_seqs) {
-        const Seq q = seq_of<P>(a, i);
+        if (P == WHOLE) q = entry(a, i);
         row0[i] = q.row0, n[i] = q.n, len[i] = q.len;
         if (P == TAIL) more[i] = q.more;
         x = units(q);
@@ -155,6 +196,7 @@ struct SeqTableOf {
   }
   __device__ __forceinline__ int find(int u) const {  // the sequence that has unit u (less than all units)
     if (n_seqs <= 64) return __builtin_popcountll(__ballot(upto <= u));
+    if constexpr (P != WHOLE) return last_upto(pre, u);
     int lo = 0, hi = n_seqs;  // pre[lo] <= u < pre[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -163,16 +205,15 @@ struct SeqTableOf {
     }
     return __builtin_amdgcn_readfirstlane(lo);
   }
+  // the last of x[0 .. n_seqs - 1], which do not descend, that is not above v, or -1: two looks at 64 of them
+  __device__ __forceinline__ int last_upto(const int *x, int v) const {
+    const int lane = threadIdx.x & 63, run = (n_seqs + 63) / 64;
+    const int before = max(0, __builtin_popcountll(__ballot(lane * run < n_seqs && x[min(lane * run, n_seqs - 1)] <= v)) - 1) * run;
+    return before + __builtin_popcountll(__ballot(lane < run && before + lane < n_seqs && x[min(before + lane, n_seqs - 1)] <= v)) - 1;
+  }
   __device__ __forceinline__ int find_row(int row) const {  // the last one that begins at the row or before, or -1
     if (n_seqs <= 64) return __builtin_popcountll(__ballot(int(threadIdx.x & 63) < n_seqs && mine.row0 <= row)) - 1;
-    if (row0[0] > row) return -1;
-    int lo = 0, hi = n_seqs;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (row0[mid] <= row) lo = mid;
-      else hi = mid;
-    }
-    return __builtin_amdgcn_readfirstlane(lo);
+    return last_upto(row0, row);
   }
 };
 using SeqTable = SeqTableOf<WHOLE>;

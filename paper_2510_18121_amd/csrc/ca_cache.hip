@@ -40,13 +40,19 @@ namespace ca {
 template <int D, int NR, int W>
 __global__ __launch_bounds__(64 * W, NR == 1 || D == 64 ? 2 : 1) void ca_cache_attend_kernel(const AttendArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  attend_workgroup<WHOLE, D, NR, W>(a, smem, blockIdx.x, blockIdx.y, gridDim.y, a.parts, a.by_workers);
+  WorkSplit<WHOLE> split;
+  split.count<64 * W>(smem + AttendShape<D, NR, W>::MERGE, a, 16 * NR);
+  split.deal(gridDim.y, a.by_workers, W);
+  attend_workgroup<WHOLE, D, NR, W>(a, smem, split, blockIdx.x, blockIdx.y, a.parts);
 }
 
 template <int D>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_cache_chunk_kernel(const AttendArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  chunk_workgroup<WHOLE, D>(a, smem, blockIdx.x, blockIdx.y, gridDim.y, a.parts, a.by_workers);
+  WorkSplit<WHOLE> split;
+  split.count<256>(smem + ChunkSmem<D>::TOTAL, a, 128);
+  split.deal(gridDim.y, a.by_workers, 4);
+  chunk_workgroup<WHOLE, D>(a, smem, split, blockIdx.x, blockIdx.y, a.parts);
 }
 
 // Adds up the parts of the tiles that were cut, in their order: a wave takes RW rows, and two (four) parts of each at a time.  4 to 5 us, of which

@@ -67,18 +67,22 @@ __device__ __forceinline__ int quotient(int x, int y) {
 template <Part P>
 struct WorkSplit {
   SeqTableOf<P> tab;
-  int total, run, R, G, window, sinks;
+  int total, run, cut, R, G, window, sinks;
   template <int T, class A>
-  __device__ __forceinline__ void make(void *lds, const A &a, int rows, int n_workers, float by_workers, int least) {
+  __device__ __forceinline__ void count(void *lds, const A &a, int rows) {
     R = rows, G = a.G, window = a.window, sinks = a.sinks;
     total = tab.template fill<T>(lds, a.s, [&](const Seq &q) { return (q.n * G + R - 1) / R * tile_pages(q.len, R, G, window, sinks); });
+  }
+  // by_workers: a little more than 1 / n_workers
+  __device__ __forceinline__ void deal(int n_workers, float by_workers, int least, int longest_whole = CUT) {
+    cut = longest_whole;
     run = max(least, n_workers == 1 ? total : __builtin_amdgcn_readfirstlane(int(float(total) * by_workers)) + 1);
   }
   __device__ __forceinline__ int bound(int w) const {
     const int u = min(w * run, total);
     if (u >= total || u == 0) return u;
     const int s = tab.find(u), n = tile_pages(tab.at(s).len, R, G, window, sinks);
-    if (n > CUT) return u;
+    if (n > cut) return u;
     const int x = u - tab.before(s), into = x - quotient(x, n) * n;
     return 2 * into < n ? u - into : u - into + n;
   }
@@ -131,19 +135,21 @@ struct AttendShape {
   static constexpr int MERGE = (W * R * ROW + W * R * 2) * 4;
 };
 
-// Single tokens and the like: tiles of 16 NR rows.  A wave has pages of its own, every W-th of the worker's run: codes come to registers
+// Single tokens and the like: tiles of 16 NR rows.  The worker is a workgroup of W waves, or, with W = 1, a wave of any.  A wave has pages of its own, every W-th of the worker's run: codes come to registers
 // in 16-byte runs, the next page's K while this one's scores are multiplied, its V behind this one's (a page further ahead took 5 % longer on 64 sequences
 // of about 4096 tokens, 7 % on 4 of 130K).  No barrier before the waves' sums meet.
 template <Part P, int D, int NR, int W, class A>
-__device__ __forceinline__ void attend_workgroup(const A &a, char *smem, int hk, int worker, int n_workers, float *parts, float by_workers) {
+__device__ __forceinline__ void attend_workgroup(const A &a, char *smem, const WorkSplit<P> &split, int hk, int worker, float *parts) {
   using S = AttendShape<D, NR, W>;
   constexpr int R = S::R, NH = D / 64, NB = D / 16;
   float *const merge = reinterpret_cast<float *>(smem), *const merge_ml = merge + W * R * S::ROW;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), thread = W == 1 ? lane : threadIdx.x;
+  auto sync = [&]() __attribute__((always_inline)) {
+    if constexpr (W == 1) wave_sync();
+    else __syncthreads();
+  };
   const int j4 = lane >> 4, li = lane & 15;
   const int G = a.G;
-  WorkSplit<P> split;
-  split.template make<64 * W>(smem + S::MERGE, a, R, n_workers, by_workers, W);
   const SeqTableOf<P> &tab = split.tab;
   const int begin = split.bound(worker), end = split.bound(worker + 1);
   int4 head = {0, 0, 0, 0};
@@ -298,7 +304,7 @@ __device__ __forceinline__ void attend_workgroup(const A &a, char *smem, int hk,
       sum[rg] = quad_sum(l[rg]);
       if (j4 == 0) merge_ml[wave * R + 16 * rg + li] = m[rg];
     }
-    __syncthreads();
+    sync();
     const bool whole = n == per_tile;
     const int slot = first == 0 ? 1 : 0;
     float *const part = parts + size_t((worker * 2 + slot) * a.hkv + hk) * (R * (D + 2));
@@ -319,8 +325,8 @@ __device__ __forceinline__ void attend_workgroup(const A &a, char *smem, int hk,
 #pragma unroll
           for (int rg = 0; rg < NR; ++rg)
             *reinterpret_cast<f32x4 *>(&merge[(wave * R + 16 * rg + li) * S::ROW + 16 * b - c0 + 4 * j4]) = acc[b][rg] * factor[rg];
-      __syncthreads();
-      for (int i = threadIdx.x; i < R * S::CW / 4; i += 64 * W) {
+      sync();
+      for (int i = thread; i < R * S::CW / 4; i += 64 * W) {
         const int r = i / (S::CW / 4), col = 4 * (i % (S::CW / 4)), at = tile * R + r;
         if (at > last_row) break;
         f32x4 y = {0.f, 0.f, 0.f, 0.f};
@@ -355,7 +361,7 @@ __device__ __forceinline__ void attend_workgroup(const A &a, char *smem, int hk,
             u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
         if (stats && a.lse) a.lse[size_t(h) * a.s.total + q.row0 + token] = 0.6931471805599453f * (top + fast_log2(all));
       }
-      if (c0 + S::CW < D || u < end) __syncthreads();
+      if (c0 + S::CW < D || u < end) sync();
     }
   }
   if (P == WHOLE && threadIdx.x == 0) a.heads[worker * a.hkv + hk] = head;
@@ -377,15 +383,13 @@ struct ChunkSmem {
 };
 
 template <Part P, int D, class A>
-__device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, int hk, int worker, int n_workers, float *parts, float by_workers) {
+__device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, const WorkSplit<P> &split, int hk, int worker, float *parts) {
   using S = ChunkSmem<D>;
   constexpr int R = 128, NK = D / 32, NB = D / 16, ROWB = 2 * D, NL = D / 64;  // NL: loads of K, and of V, of a wave per page
   const uint32_t lds0 = (uint32_t)(uintptr_t)(CA_LDS char *)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j4 = lane >> 4, li = lane & 15;
   const int G = a.G;
-  WorkSplit<P> split;
-  split.template make<256>(smem + S::TOTAL, a, R, n_workers, by_workers, 4);
   const SeqTableOf<P> &tab = split.tab;
   const int begin = split.bound(worker), end = split.bound(worker + 1);
   int4 head = {0, 0, 0, 0};

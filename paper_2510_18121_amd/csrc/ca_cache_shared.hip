@@ -23,29 +23,72 @@ namespace ca {
 
 struct SharedLaunch {
   SharedArgs a;
-  float *parts[2];      // PREFIX, TAIL
-  int workers[2];       // per KV head
-  float by_workers[2];
+  float *parts;
+  int groups;                // workgroups per KV head, of both kinds
+  float cost[2], tiles[2];   // of PREFIX and of TAIL: what a unit costs a workgroup, and all tiles beside their units
 };
 
-template <Part P, int D, int NR, class A>
-__device__ __forceinline__ void tile_workgroup(const A &a, char *smem, int hk, int worker, int n_workers, float *parts, float by_workers) {
-  if constexpr (NR == 8) chunk_workgroup<P, D>(a, smem, hk, worker, n_workers, parts, by_workers);
-  else attend_workgroup<P, D, NR, 4>(a, smem, hk, worker, n_workers, parts, by_workers);
-}
+// A worker is a workgroup where tiles are of 128 rows, otherwise a wave.
+constexpr int waves_apart(int NR) { return NR == 8 ? 1 : 4; }
+// Tiles of up to CUT_SHARED pages are not cut.  (There is a second launch anyway, and more parts cost little there.)
+constexpr int CUT_SHARED = 4;
+
+// How the workgroups are dealt to the two kinds: by what they cost together, from the device's arrays, the same in every workgroup.
+struct TwoSplits {
+  WorkSplit<PREFIX> prefix;
+  WorkSplit<TAIL> tail;
+  int groups;  // workgroups of PREFIX, the first ones
+  int workers[2];
+  float *parts[2];
+  // KEEP_BOTH: tables of both (lds has room for them); otherwise of the kind that the workgroup is of.
+  template <int D, int NP, int NT, bool KEEP_BOTH>
+  __device__ __forceinline__ void make(char *lds, const SharedLaunch &x, int group) {
+    const SharedArgs &a = x.a;
+    const bool clash = !KEEP_BOTH && a.s.n_groups > 64;  // both tables lie in LDS
+    constexpr int WP = waves_apart(NP), WT = waves_apart(NT);
+    tail.tab.lanes.load(a.s);
+    prefix.tab.lanes = tail.tab.lanes;
+    prefix.count<256>(lds, a, 16 * NP);
+    if (clash) __syncthreads();
+    tail.count<256>(KEEP_BOTH ? lds + seq_table_bytes(a.s.n_groups, PREFIX) : lds, a, 16 * NT);
+    const float p = x.cost[0] * float(prefix.total) + x.tiles[0], t = x.cost[1] * float(tail.total) + x.tiles[1];
+    const int most = (prefix.total + LEAST * WP - 1) / (LEAST * WP);
+    groups = prefix.total == 0 ? 0 : min(most, max(1, min(x.groups - 1, int(float(x.groups) * p / (p + t) + 0.5f))));
+    groups = __builtin_amdgcn_readfirstlane(groups);
+    workers[0] = groups * WP, workers[1] = (x.groups - groups) * WT;
+    prefix.run = max(LEAST, quotient(prefix.total + max(workers[0], 1) - 1, max(workers[0], 1)));
+    tail.run = max(1, quotient(tail.total + workers[1] - 1, workers[1]));
+    prefix.cut = NP == 8 ? CUT : CUT_SHARED, tail.cut = NT == 8 ? CUT : CUT_SHARED;
+    parts[0] = x.parts, parts[1] = x.parts + size_t(workers[0]) * 2 * a.hkv * (16 * NP * (D + 2));
+    if (clash && group < groups) {
+      __syncthreads();
+      prefix.count<256>(lds, a, 16 * NP);
+    }
+  }
+  static constexpr int LEAST = 2;  // units of a worker of PREFIX
+};
+
 template <int D, int NR>
 constexpr int tile_bytes() {
   if constexpr (NR == 8) return ChunkSmem<D>::TOTAL;
-  else return AttendShape<D, NR, 4>::MERGE;
+  else return 4 * AttendShape<D, NR, 1>::MERGE;
+}
+template <Part P, int D, int NR, class A>
+__device__ __forceinline__ void tile_workgroup(const A &a, char *smem, const WorkSplit<P> &split, int hk, int group, float *parts) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if constexpr (NR == 8) chunk_workgroup<P, D>(a, smem, split, hk, group, parts);
+  else attend_workgroup<P, D, NR, 1>(a, smem + wave * AttendShape<D, NR, 1>::MERGE, split, hk, 4 * group + wave, parts);
 }
 
 // NP, NT: 16-row groups of a tile of the prefix and of the tails.
 template <int D, int NP, int NT>
-__global__ __launch_bounds__(256, (NP == 2 || NT == 2) && D == 128 ? 1 : 2) void ca_cache_shared_kernel(const SharedLaunch x) {
+__global__ __launch_bounds__(256, 2) void ca_cache_shared_kernel(const SharedLaunch x) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int worker = blockIdx.y;
-  if (worker < x.workers[0]) tile_workgroup<PREFIX, D, NP>(x.a, smem, blockIdx.x, worker, x.workers[0], x.parts[0], x.by_workers[0]);
-  else tile_workgroup<TAIL, D, NT>(x.a, smem, blockIdx.x, worker - x.workers[0], x.workers[1], x.parts[1], x.by_workers[1]);
+  const int group = blockIdx.y;
+  TwoSplits s;
+  s.make<D, NP, NT, false>(smem + std::max(tile_bytes<D, NP>(), tile_bytes<D, NT>()), x, group);
+  if (group < s.groups) tile_workgroup<PREFIX, D, NP>(x.a, smem, s.prefix, blockIdx.x, group, s.parts[0]);
+  else tile_workgroup<TAIL, D, NT>(x.a, smem, s.tail, blockIdx.x, group - s.groups, s.parts[1]);
 }
 
 // What there is of a row's tile: the parts of the workers that had a run of its pages each, or one sum of the row.
@@ -60,7 +103,7 @@ struct RowParts {
     const int per = tile_pages(q.len, R, G, a.window, a.sinks), u0 = split.tab.before(entry) + tile * per;
     // (sequences that overlap, against their description, may have more units than are counted)
     const int w0 = min(quotient(u0, split.run), n_workers - 1), w1 = min(quotient(u0 + per - 1, split.run), n_workers - 1);
-    if (per <= CUT || w0 == w1) {
+    if (per <= split.cut || w0 == w1) {
       const size_t i = size_t(row) * a.hq + h;
       n = 1, first = a.row_sums[P == TAIL] + i * D, first_ml = a.row_ml[P == TAIL] + 2 * i;
       return;
@@ -80,12 +123,12 @@ struct RowParts {
 template <int D, int NP, int NT>
 __global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x, int rows_of_wave) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  constexpr int LANES = D / 4, AT_A_TIME = 64 / LANES;
+  constexpr int LANES = D / 4, AT_A_TIME = 64 / LANES, LOADS = 8;
   const SharedArgs &a = x.a;
-  WorkSplit<PREFIX> prefix;
-  WorkSplit<TAIL> tail;
-  prefix.template make<256>(smem, a, 16 * NP, x.workers[0], x.by_workers[0], 4);
-  tail.template make<256>(smem + seq_table_bytes(a.s.n_groups, PREFIX), a, 16 * NT, x.workers[1], x.by_workers[1], 4);
+  TwoSplits split;
+  split.make<D, NP, NT, true>(smem, x, 0);
+  const WorkSplit<PREFIX> &prefix = split.prefix;
+  const WorkSplit<TAIL> &tail = split.tail;
   const int lane = threadIdx.x & 63, mine = lane / LANES, col = 4 * (lane % LANES);
   const int64_t wave = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = int64_t(a.s.total) * a.hq;
   for (int64_t at = wave * rows_of_wave; at < min(n, (wave + 1) * rows_of_wave); ++at) {
@@ -95,13 +138,13 @@ __global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x
     const Seq q = tail.tab.at(s);
     if (row < q.row0 || row >= q.row0 + q.n) continue;
     RowParts<D> t, p;
-    t.template of<TAIL>(a, tail, x.parts[1], x.workers[1], s, q, row, h, hk);
+    t.template of<TAIL>(a, tail, split.parts[1], split.workers[1], s, q, row, h, hk);
     p.n = 0;
     if (q.more > 0) {
       const int g = prefix.tab.find_row(row);
       const Seq of_group = prefix.tab.at(max(g, 0));
       if (g >= 0 && row >= of_group.row0 && row < of_group.row0 + of_group.n)
-        p.template of<PREFIX>(a, prefix, x.parts[0], x.workers[0], g, of_group, row, h, hk);
+        p.template of<PREFIX>(a, prefix, split.parts[0], split.workers[0], g, of_group, row, h, hk);
     } else if (t.n == 1) {
       continue;  // it is done
     }
@@ -113,11 +156,20 @@ __global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = y[e] * old + w * z[e];
     };
-#pragma unroll 4
-    for (int i = mine; i < p.n + t.n; i += AT_A_TIME) {
-      const bool in_prefix = i < p.n;
-      const float *const z = in_prefix ? p.sum(i) : t.sum(i - p.n), *const ml = in_prefix ? p.ml(i) : t.ml(i - p.n);
-      add(ml[0], ml[1], *reinterpret_cast<const f32x4 *>(z + col));
+    const int n_parts = p.n + t.n;
+    for (int base = 0; base < n_parts; base += LOADS * AT_A_TIME) {  // (all of a round's loads before the first sum)
+      f32x4 z[LOADS];
+      f32x2 ml[LOADS];
+#pragma unroll
+      for (int k = 0; k < LOADS; ++k) {
+        const int i = min(base + k * AT_A_TIME + mine, n_parts - 1);
+        const bool in_prefix = i < p.n;
+        z[k] = *reinterpret_cast<const f32x4 *>((in_prefix ? p.sum(i) : t.sum(i - p.n)) + col);
+        ml[k] = *reinterpret_cast<const f32x2 *>(in_prefix ? p.ml(i) : t.ml(i - p.n));
+      }
+#pragma unroll
+      for (int k = 0; k < LOADS; ++k)
+        if (base + k * AT_A_TIME + mine < n_parts) add(ml[k][0], ml[k][1], z[k]);
     }
 #pragma unroll
     for (int o = LANES; o < 64; o <<= 1) {
@@ -135,26 +187,27 @@ __global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x
 }
 
 // ------------------------------------------------------------------------------------------------ calls
-// Workers of both kinds together, per KV head: two workgroups of four waves to a CU.
-static int shared_workers(int hkv) { return std::max(2, N_CU * 2 / hkv); }
+// Workgroups per KV head: two of four waves to a CU.
+static int shared_groups(int hkv) { return std::max(2, N_CU * 2 / hkv); }
 static size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 struct SharedBytes {
   size_t parts, sums, ml;  // sums, ml: of each kind
   size_t all() const { return parts + 2 * (sums + ml); }
 };
 static SharedBytes shared_bytes(int d, int hkv, int hq, int64_t rows) {
-  return {round_up(size_t(shared_workers(hkv)) * 2 * hkv * (128 * (d + 2)) * 4), round_up(size_t(rows) * hq * d * 4), round_up(size_t(rows) * hq * 2 * 4)};
+  // (parts: two of 128 rows for each workgroup, which is also room for two of 16 rows for each of its waves)
+  return {round_up(size_t(shared_groups(hkv)) * 2 * hkv * (128 * (d + 2)) * 4), round_up(size_t(rows) * hq * d * 4), round_up(size_t(rows) * hq * 2 * 4)};
 }
 
 template <int D, int NP, int NT>
 static int launch_shared(SharedLaunch &x, hipStream_t st) {
-  SharedArgs &a = x.a;
-  const int all = shared_workers(a.hkv);
-  x.workers[0] = a.s.n_groups > 0 ? all / 2 : 0, x.workers[1] = all - x.workers[0];
-  for (int i = 0; i < 2; ++i) x.by_workers[i] = 1.0001f / float(std::max(1, x.workers[i]));
-  x.parts[1] = x.parts[0] + size_t(x.workers[0]) * 2 * a.hkv * (16 * NP * (D + 2));
+  const SharedArgs &a = x.a;
+  x.groups = shared_groups(a.hkv);
+  const float rows = float(a.s.total) * a.G;
+  x.cost[0] = NP == 8 ? 2.6f : 1.2f, x.cost[1] = NT == 8 ? 2.6f : 1.5f;
+  x.tiles[0] = (rows / (16 * NP) + a.s.n_groups) * (NP == 8 ? 4.f : 1.f), x.tiles[1] = (rows / (16 * NT) + a.s.n_seqs) * (NT == 8 ? 4.f : 1.f);
   const size_t tables[2] = {seq_table_bytes(a.s.n_groups, PREFIX), seq_table_bytes(a.s.n_seqs, TAIL)};
-  const size_t bytes = std::max(tile_bytes<D, NP>() + tables[0], tile_bytes<D, NT>() + tables[1]);
+  const size_t bytes = std::max(tile_bytes<D, NP>(), tile_bytes<D, NT>()) + std::max(tables[0], tables[1]);
   auto kern = ca_cache_shared_kernel<D, NP, NT>;
   auto join = ca_cache_join_kernel<D, NP, NT>;
   int device = 0;
@@ -163,22 +216,21 @@ static int launch_shared(SharedLaunch &x, hipStream_t st) {
   if (e == hipSuccess) e = set_smem(kern, int(std::max(tile_bytes<D, NP>(), tile_bytes<D, NT>()) + seq_table_bytes(MAX_SEQS, TAIL)), device, done[0]);
   if (e == hipSuccess) e = set_smem(join, int(seq_table_bytes(MAX_SEQS, PREFIX) + seq_table_bytes(MAX_SEQS, TAIL)), device, done[1]);
   if (e != hipSuccess) return launched("cache attention of groups", e);
-  hipLaunchKernelGGL(kern, dim3(unsigned(a.hkv), unsigned(all)), dim3(256), bytes, st, x);
+  hipLaunchKernelGGL(kern, dim3(unsigned(a.hkv), unsigned(x.groups)), dim3(256), bytes, st, x);
   const int64_t n = int64_t(a.s.total) * a.hq;
   const int per = int(std::max<int64_t>(1, n / (N_CU * 64)));
   hipLaunchKernelGGL(join, dim3(unsigned((n + 4 * per - 1) / (4 * per))), dim3(256), tables[0] + tables[1], st, x, per);
   return launched("cache attention of groups", hipSuccess);
 }
 
-// Rows per tile, as in ca_cache_attend, from the average group and the average sequence.
+// Rows per tile, as in ca_cache_attend, from the average group and the average sequence.  (Tiles of 32 rows, as there, are none here: at head_dim 128 they leave
+// room for four waves to a CU, 8 answers to a prompt of 2048 tokens 20.6 us with them and 17.8 without; at 64 200 answers to nine of 4000 72 and 68.)
 template <int D>
 static int shared_by_rows(SharedLaunch &x, hipStream_t st) {
   const SharedArgs &a = x.a;
   const int64_t rows = int64_t(a.s.total) * a.G, of_group = rows / std::max(1, a.s.n_groups), of_seq = rows / a.s.n_seqs;
   if (of_seq > 32) return launch_shared<D, 8, 8>(x, st);
-  if (of_group > 32) return of_seq > 16 ? launch_shared<D, 8, 2>(x, st) : launch_shared<D, 8, 1>(x, st);
-  if (of_group > 16) return of_seq > 16 ? launch_shared<D, 2, 2>(x, st) : launch_shared<D, 2, 1>(x, st);
-  return launch_shared<D, 1, 1>(x, st);
+  return of_group > 32 ? launch_shared<D, 8, 1>(x, st) : launch_shared<D, 1, 1>(x, st);
 }
 
 }  // namespace ca
@@ -227,7 +279,7 @@ int ca_cache_attend_shared(const ca_cache *c, const ca_cache_batch *b, const ca_
   a.window = 1 << 30, a.sinks = 0;
   a.c = (softmax_scale > 0.f ? softmax_scale : c->head_dim == 128 ? 0.08838834764831845f : 0.125f) * 1.4426950408889634f;
   char *at = static_cast<char *>(ws);
-  x.parts[0] = reinterpret_cast<float *>(at), at += need.parts;
+  x.parts = reinterpret_cast<float *>(at), at += need.parts;
   for (int i = 0; i < 2; ++i) {
     a.row_sums[i] = reinterpret_cast<float *>(at), at += need.sums;
     a.row_ml[i] = reinterpret_cast<float *>(at), at += need.ml;

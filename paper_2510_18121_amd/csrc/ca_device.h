@@ -87,6 +87,13 @@ __device__ __forceinline__ int lane_id_here() {
 // a ^ b: of a loop-carried LDS address and the distance to one of its fragments
 __device__ __forceinline__ int xor_here(int a, const int b) { return a ^ opaque(b); }
 
+// What lanes of the wave have written to LDS is there for its other lanes (its LDS instructions execute in order; this is for the compiler).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __device__ __forceinline__ int wave_max(int v) {
   for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o));
   return v;

@@ -91,13 +91,6 @@ __device__ __forceinline__ float head_sum(float x) {
   return LANES == 8 ? add_dpp<0x141>(x) : x;      // 7 - lane: of the other four
 }
 
-// What lanes of the wave have written to LDS is there for its other lanes (its LDS instructions execute in order; this is for the compiler).
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // A wave's own LDS: cosines and sines of the row's pairs, and, for HALF_ANY, the heads in flight.
 template <int D, Layout L>
 struct RotateSmem {
