@@ -529,62 +529,65 @@ def rows_in_line(t):
     return t.clone(memory_format=torch.contiguous_format)
 
 
-def _rows(t, shape, index, name):
-    """Address and row stride of a bf16 tensor [rows, heads, head_dim] on that device, each of whose rows is one run of memory."""
-    import torch
+def _rows(rotation, t, shape, name):
+    """Address and row stride of a bf16 tensor [rows, heads, head_dim] on the rotation's device, each of whose rows is one run of memory."""
     rows, heads, d = shape
-    s = t.stride()
-    if (t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != index or s[2] != 1 or (heads != 1 and s[1] != d)
-            or (rows > 1 and (s[0] < heads * d or s[0] % 8))):
-        raise ValueError(f"{name}: expected bf16 tensor {tuple(shape)} on device {index}, whose rows are runs of memory a multiple of 8 elements apart, "
-                         f"got {tuple(t.shape)} {t.dtype} on {t.device} with strides {s}")
-    return (t.data_ptr() if rows else None), (s[0] if rows > 1 else heads * d)
+    if t.shape == shape and t.dtype is rotation.bf16 and t.get_device() == rotation.index:
+        if t.is_contiguous():
+            return t.data_ptr(), heads * d
+        s = t.stride()
+        if s[2] == 1 and (heads == 1 or s[1] == d) and (rows == 1 or (s[0] >= heads * d and s[0] % 8 == 0)):
+            return t.data_ptr(), s[0] if rows > 1 else heads * d
+    raise ValueError(f"{name}: expected bf16 tensor {tuple(shape)} on {rotation.device}, whose rows are runs of memory a multiple of 8 elements apart, "
+                     f"got {tuple(t.shape)} {t.dtype} on {t.device} with strides {t.stride()}")
 
 
-def _flat(t, shape, dtype, index, name):
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
-        raise ValueError(f"{name}: expected contiguous tensor {shape} {dtype} on device {index}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+def _line(rotation, t, shape, dtype, name):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != rotation.index or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous tensor {tuple(shape)} {dtype} on {rotation.device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
-def _rotate_tensor(rotation, x, dy, y, pos, by_sequences, gain, dgain, name):
-    """A ca_rotate_tensor; x None: of a gradient without a gain."""
-    import torch
-    index, f32 = rotation.index, torch.float32
+def _rotate_tensor(rotation, x, dy, y, pos, where, gain, dgain, name):
+    """The fields of a ca_rotate_tensor; x None: of a gradient without a gain."""
     shape = y.shape
     if len(shape) != 3 or shape[2] != rotation.head_dim:
         raise ValueError(f"{name}: expected [rows, heads, {rotation.head_dim}], got {tuple(shape)}")
-    d = (rotation.head_dim,)
-    t = RotateTensor()
-    t.rows, t.heads = shape[0], shape[1]
-    t.y, t.y_stride = _rows(y, shape, index, name + " (out)")
+    xp = xs = dp = ds = gp = dgp = pp = None
+    yp, ys = _rows(rotation, y, shape, name + " (out)")
     if x is not None:
-        t.x, t.x_stride = _rows(x, shape, index, name)
+        xp, xs = _rows(rotation, x, shape, name)
     if dy is not None:
-        t.dy, t.dy_stride = _rows(dy, shape, index, f"gradient of {name}")
+        dp, ds = _rows(rotation, dy, shape, "gradient of " + name)
     if gain is not None:
-        t.gain = _flat(gain, d, f32, index, f"gain of {name}")
+        gp = _line(rotation, gain, shape[2:], rotation.f32, "gain of " + name)
         if dy is not None:
-            t.dgain = _flat(dgain, d, f32, index, f"gradient of the gain of {name}")
-    if not by_sequences:
+            dgp = _line(rotation, dgain, shape[2:], rotation.f32, "gradient of the gain of " + name)
+    if where is None:
         if pos is None:
             raise ValueError(f"{name}: neither positions nor sequences are given")
-        t.pos = _flat(pos, shape[:1], torch.int32, index, f"positions of {name}")
-    return t
+        pp = _line(rotation, pos, shape[:1], rotation.i32, "positions of " + name)
+    return xp, dp, yp, gp, dgp, pp, shape[0], xs or 0, ds or 0, ys, shape[1]
 
 
-def _rotate_call(rotation, tensors, where):
-    """The tensors as an array, their number, and the sequences as a ca_cache_batch (or None)."""
-    import torch
-    index, current = rotation.index, torch.cuda.current_device()
-    if index != current:
+_RotateTensors = RotateTensor * 2
+
+
+def _rotate_where(rotation, where, rows):
+    """The sequences as a ca_cache_batch, or None."""
+    if where is None:
+        return None
+    n = where[1].shape[0]
+    return ctypes.byref(CacheBatch(n, 0, rows, _line(rotation, where[0], (n + 1,), rotation.i32, "q_start"),
+                                   _line(rotation, where[1], (n,), rotation.i32, "kv_len"), None))
+
+
+def _rotate_stream(rotation, stream):
+    """The stream's address; the tensors have to be on the current device, whose streams order the work on it."""
+    current = rotation.current_device()
+    if rotation.index != current:
         raise ValueError(f"the rotation is on {rotation.device}, the current device is {current}")
-    batch = None
-    if where is not None:
-        start, lens = where[0], where[1]
-        n = lens.shape[0]
-        batch = CacheBatch(n, 0, tensors[0].rows, _flat(start, (n + 1,), torch.int32, index, "q_start"), _flat(lens, (n,), torch.int32, index, "kv_len"), None)
-    return (RotateTensor * len(tensors))(*tensors), len(tensors), None if batch is None else ctypes.byref(batch)
+    return _stream_ptr(stream) if stream is not None or rotation.raw_stream is None else rotation.raw_stream(current)
 
 
 def ca_rotate(rotation, q, k, q_out, k_out, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, eps=1e-6, stream=None):
@@ -592,11 +595,12 @@ def ca_rotate(rotation, q, k, q_out, k_out, q_pos=None, k_pos=None, where=None, 
     (rotation: rotary.Rotation).  q, k and the outputs: bf16 [rows, heads, head_dim], each row a run of memory, so that views of a joint projection
     will do; an output may be its input.  Positions: q_pos and k_pos (device int32 [rows]; k_pos None: those of q), or where = (q_start, kv_len, ..) of
     the sequences of a call on a cache: rows are their last ones, and rows of no sequence are left as they are.  Gains: fp32 [head_dim]."""
-    tensors = [_rotate_tensor(rotation, q, None, q_out, q_pos, where is not None, q_gain, None, "q")]
-    if k is not None:
-        tensors.append(_rotate_tensor(rotation, k, None, k_out, q_pos if k_pos is None else k_pos, where is not None, k_gain, None, "k"))
-    array, n, batch = _rotate_call(rotation, tensors, where)
-    _check(lib().ca_rotate(rotation.desc_ref, array, n, batch, eps, _stream_ptr(stream)))
+    first = _rotate_tensor(rotation, q, None, q_out, q_pos, where, q_gain, None, "q")
+    if k is None:
+        n, tensors = 1, _RotateTensors(first)
+    else:
+        n, tensors = 2, _RotateTensors(first, _rotate_tensor(rotation, k, None, k_out, q_pos if k_pos is None else k_pos, where, k_gain, None, "k"))
+    _check(lib().ca_rotate(rotation.desc_ref, tensors, n, _rotate_where(rotation, where, first[6]), eps, _rotate_stream(rotation, stream)))
 
 
 def ca_rotate_backward(rotation, q, k, dq_out, dk_out, dq, dk, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, dq_gain=None,
@@ -610,10 +614,12 @@ def ca_rotate_backward(rotation, q, k, dq_out, dk_out, dq, dk, q_pos=None, k_pos
             continue
         if gain is not None and (x is None or dgain is None):
             raise ValueError(f"{name}: with a gain the gradient needs the input, and a tensor for that of the gain")
-        tensors.append(_rotate_tensor(rotation, x if gain is not None else None, dy, dx, pos, where is not None, gain, dgain, name))
-    array, n, batch = _rotate_call(rotation, tensors, where)
-    wp, wn = (None, 0) if ws is None else (_flat(ws, ws.shape, ws.dtype, rotation.index, "ws"), ws.numel() * ws.element_size())
-    _check(lib().ca_rotate_backward(rotation.desc_ref, array, n, batch, eps, wp, wn, _stream_ptr(stream)))
+        tensors.append(_rotate_tensor(rotation, x if gain is not None else None, dy, dx, pos, where, gain, dgain, name))
+    if not tensors:
+        raise ValueError("neither dq_out nor dk_out")
+    wp, wn = (None, 0) if ws is None else (_line(rotation, ws, ws.shape, ws.dtype, "ws"), ws.numel() * ws.element_size())
+    _check(lib().ca_rotate_backward(rotation.desc_ref, _RotateTensors(*tensors), len(tensors), _rotate_where(rotation, where, tensors[0][6]), eps, wp, wn,
+                                    _rotate_stream(rotation, stream)))
 
 
 def alloc_rotate_workspace(device="cuda"):

@@ -19,6 +19,9 @@
 
 namespace ca {
 
+constexpr int MOST_BLOCKS = N_CU * 4;  // workgroups of a tensor
+constexpr int64_t STREAM_BYTES = int64_t(384) << 20;
+
 enum Layout { HALF, INTERLEAVED, HALF_ANY };  // HALF: rot / 2 is a multiple of 8; HALF_ANY: of anything
 
 struct RotateTensor {
@@ -165,8 +168,9 @@ struct Turner {
   }
 };
 
-// A wave takes a row's heads, or a run of them, 1024 elements at a time, and then those of a row further on.
-template <int D, Layout L, bool BACKWARD>
+// A wave takes a row's heads, or a run of them, 1024 elements at a time, and then those of a row further on; the elements after the next are on their
+// way while it works.  STREAM: tensors that the last cache does not hold until somebody reads them pass it by.
+template <int D, Layout L, bool BACKWARD, bool STREAM>
 __global__ __launch_bounds__(256) void ca_rotate_kernel(const RotateArgs a) {
   constexpr int LANES = D / 16, SLOTS = 64 / LANES;  // of a head; heads at a time
   __shared__ RotateSmem<D, L> smem[4];
@@ -187,59 +191,98 @@ __global__ __launch_bounds__(256) void ca_rotate_kernel(const RotateArgs a) {
     ga[e] = t.gain ? t.gain[turner.col_a + e] : 1.f, gb[e] = t.gain ? t.gain[turner.col_b + e] : 1.f;
     da[e] = db[e] = 0.f;
   }
-  for (int64_t row = w / segments; row < t.rows && w / segments < stride; row += stride) {
-    int pos = 0;
-    if (t.pos) pos = t.pos[row];
-    else if (!position_in_sequence(a, t.rows, row, lane, pos)) continue;
-    if (lane < D / 2) mine.cs[lane] = cos_sin(pos, turns) * a.factor;
-    wave_sync();
-    turner.take(mine.cs);
-    wave_sync();
-    for (int h0 = first; h0 < end; h0 += SLOTS) {
-      const int h = h0 + turner.slot;
-      const bool there = h < end;
-      const int64_t at = int64_t(there ? h : h0) * D;
-      float xa[8], xb[8];
-      const bf16_t *const src = (BACKWARD ? t.dy + row * t.dy_stride : t.x + row * t.x_stride) + at;
-      unpack(*reinterpret_cast<const u32x4 *>(src + turner.col_a), xa);
-      unpack(*reinterpret_cast<const u32x4 *>(src + turner.col_b), xb);
-      bf16_t *const dst = t.y + row * t.y_stride + at;
-      if (!BACKWARD) {
-        if (t.gain) {
-          float sum = 0.f;
+  auto get = [&](const bf16_t *p) __attribute__((always_inline)) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+    else return *reinterpret_cast<const u32x4 *>(p);
+  };
+  auto put = [&](bf16_t *p, const u32x4 &v) __attribute__((always_inline)) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+    else *reinterpret_cast<u32x4 *>(p) = v;
+  };
+  struct Raw {
+    u32x4 a, b, xa, xb;  // x, or dy and with a gain x
+  };
+  auto load = [&](int64_t row, int h0) __attribute__((always_inline)) {
+    const int h = h0 + turner.slot;
+    const int64_t at = int64_t(h < end ? h : h0) * D;
+    const bf16_t *const src = (BACKWARD ? t.dy + row * t.dy_stride : t.x + row * t.x_stride) + at;
+    Raw r;
+    r.a = get(src + turner.col_a), r.b = get(src + turner.col_b);
+    if (BACKWARD && t.gain) {
+      const bf16_t *const xs = t.x + row * t.x_stride + at;
+      r.xa = get(xs + turner.col_a), r.xb = get(xs + turner.col_b);
+    }
+    return r;
+  };
+  int64_t row = w / segments;
+  int h0 = first;
+  bool more = row < t.rows && w / segments < stride && first < end, known = false;
+  Raw next = {};
+  int pos = 0, next_pos = 0;
+  if (more) {
+    next = load(row, h0);
+    if (t.pos) next_pos = t.pos[row];
+  }
+  while (more) {
+    const Raw now = next;
+    const int64_t this_row = row;
+    const int this_h0 = h0;
+    const bool new_row = h0 == first;
+    if (new_row) {
+      pos = next_pos, known = true;
+      if (!t.pos) known = position_in_sequence(a, t.rows, row, lane, pos);
+    }
+    h0 += SLOTS;
+    if (h0 >= end) h0 = first, row += stride;
+    more = row < t.rows;
+    if (more) {
+      next = load(row, h0);
+      if (t.pos && h0 == first) next_pos = t.pos[row];
+    }
+    if (!known) continue;  // a row of no sequence
+    if (new_row) {
+      if (lane < D / 2) mine.cs[lane] = cos_sin(pos, turns) * a.factor;
+      wave_sync();
+      turner.take(mine.cs);
+      wave_sync();
+    }
+    const int h = this_h0 + turner.slot;
+    const bool there = h < end;
+    float xa[8], xb[8];
+    unpack(now.a, xa), unpack(now.b, xb);
+    if (!BACKWARD) {
+      if (t.gain) {
+        float sum = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], sum));
-          const float r = rsqrtf(fmaf(head_sum<LANES>(sum), 1.f / D, a.eps));
+        for (int e = 0; e < 8; ++e) sum = fmaf(xa[e], xa[e], fmaf(xb[e], xb[e], sum));
+        const float r = rsqrtf(fmaf(head_sum<LANES>(sum), 1.f / D, a.eps));
 #pragma unroll
-          for (int e = 0; e < 8; ++e) xa[e] *= r * ga[e], xb[e] *= r * gb[e];
+        for (int e = 0; e < 8; ++e) xa[e] *= r * ga[e], xb[e] *= r * gb[e];
+      }
+      turner.template turn<1>(xa, xb, mine.x);
+    } else {
+      turner.template turn<-1>(xa, xb, mine.x);
+      if (t.gain) {
+        float va[8], vb[8];
+        unpack(now.xa, va), unpack(now.xb, vb);
+        float sum = 0.f, dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          sum = fmaf(va[e], va[e], fmaf(vb[e], vb[e], sum));
+          dot = fmaf(xa[e] * ga[e], va[e], fmaf(xb[e] * gb[e], vb[e], dot));
         }
-        turner.template turn<1>(xa, xb, mine.x);
-      } else {
-        turner.template turn<-1>(xa, xb, mine.x);
-        if (t.gain) {
-          float va[8], vb[8];
-          const bf16_t *const xs = t.x + row * t.x_stride + at;
-          unpack(*reinterpret_cast<const u32x4 *>(xs + turner.col_a), va);
-          unpack(*reinterpret_cast<const u32x4 *>(xs + turner.col_b), vb);
-          float sum = 0.f, dot = 0.f;
+        const float r = rsqrtf(fmaf(head_sum<LANES>(sum), 1.f / D, a.eps));
+        const float mean = head_sum<LANES>(dot) * (r * r) * (1.f / D);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            sum = fmaf(va[e], va[e], fmaf(vb[e], vb[e], sum));
-            dot = fmaf(xa[e] * ga[e], va[e], fmaf(xb[e] * gb[e], vb[e], dot));
-          }
-          const float r = rsqrtf(fmaf(head_sum<LANES>(sum), 1.f / D, a.eps));
-          const float mean = head_sum<LANES>(dot) * (r * r) * (1.f / D);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (there) da[e] = fmaf(xa[e] * r, va[e], da[e]), db[e] = fmaf(xb[e] * r, vb[e], db[e]);
-            xa[e] = r * fmaf(-mean, va[e], xa[e] * ga[e]), xb[e] = r * fmaf(-mean, vb[e], xb[e] * gb[e]);
-          }
+        for (int e = 0; e < 8; ++e) {
+          if (there) da[e] = fmaf(xa[e] * r, va[e], da[e]), db[e] = fmaf(xb[e] * r, vb[e], db[e]);
+          xa[e] = r * fmaf(-mean, va[e], xa[e] * ga[e]), xb[e] = r * fmaf(-mean, vb[e], xb[e] * gb[e]);
         }
       }
-      if (there) {
-        *reinterpret_cast<u32x4 *>(dst + turner.col_a) = packed(xa);
-        *reinterpret_cast<u32x4 *>(dst + turner.col_b) = packed(xb);
-      }
+    }
+    if (there) {
+      bf16_t *const dst = t.y + this_row * t.y_stride + int64_t(h) * D;
+      put(dst + turner.col_a, packed(xa)), put(dst + turner.col_b, packed(xb));
     }
   }
   if (!BACKWARD || !t.gain) return;
@@ -256,26 +299,30 @@ __global__ __launch_bounds__(256) void ca_rotate_kernel(const RotateArgs a) {
     t.dgain[size_t(block) * D + threadIdx.x] = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
 }
 
-// dg of each tensor from the workgroups' sums: 16 columns to a workgroup, 64 threads to a column, in a fixed order.
+// dg of each tensor from the workgroups' sums, four columns to a workgroup, in a fixed order.
 struct GainSums {
   const float *parts[2];
   float *out[2];
   int n[2];
 };
 template <int D>
-__global__ __launch_bounds__(1024) void ca_rotate_gain_kernel(const GainSums a) {
-  __shared__ float sums[64][17];
-  const int which = blockIdx.y, col = 16 * blockIdx.x + (threadIdx.x & 15), i0 = threadIdx.x >> 4;
+__global__ __launch_bounds__(256) void ca_rotate_gain_kernel(const GainSums a) {
+  __shared__ f32x4 sums[256];
+  const int which = blockIdx.y, i0 = threadIdx.x;
   if (!a.out[which]) return;
-  float sum = 0.f;
-  for (int i = i0; i < a.n[which]; i += 64) sum += a.parts[which][size_t(i) * D + col];
-  sums[i0][threadIdx.x & 15] = sum;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < MOST_BLOCKS / 256; ++k) {
+    const int i = i0 + 256 * k;
+    if (i < a.n[which]) sum += *reinterpret_cast<const f32x4 *>(a.parts[which] + size_t(i) * D + 4 * blockIdx.x);
+  }
+  sums[i0] = sum;
   __syncthreads();
-  for (int o = 32; o > 0; o >>= 1) {
-    if (i0 < o) sums[i0][threadIdx.x & 15] += sums[i0 + o][threadIdx.x & 15];
+  for (int o = 128; o > 0; o >>= 1) {
+    if (i0 < o) sums[i0] += sums[i0 + o];
     __syncthreads();
   }
-  if (i0 == 0) a.out[which][col] = sums[0][threadIdx.x & 15];
+  if (i0 < 4) a.out[which][4 * blockIdx.x + i0] = sums[0][i0];
 }
 
 // ------------------------------------------------------------------------------------------------ calls
@@ -283,8 +330,6 @@ static int refuse(int code, const std::string &msg) {
   set_error(msg);
   return code;
 }
-constexpr int MOST_BLOCKS = N_CU * 8;  // workgroups of a tensor: as many as are on the chip at a time
-
 static bool whole_lines(const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0; }
 
 static int check_rotation(const ca_rotation *r) {
@@ -342,6 +387,7 @@ static int rotate(const ca_rotation *r, const ca_rotate_tensor *tensors, int n, 
   GainSums g = {};
   float *parts = static_cast<float *>(ws);
   size_t need = 0;
+  int64_t bytes = 0;  // of what is read and written
   static const char *const names[] = {"first tensor", "second tensor"};
   for (int i = 0; i < n; ++i) {
     const ca_rotate_tensor &s = tensors[i];
@@ -351,6 +397,7 @@ static int rotate(const ca_rotation *r, const ca_rotate_tensor *tensors, int n, 
     t.gain = s.gain, t.pos = where ? nullptr : s.pos, t.rows = where && where->n_seqs == 0 ? 0 : s.rows;
     t.x_stride = s.x_stride, t.y_stride = s.y_stride, t.dy_stride = s.dy_stride, t.heads = s.heads;
     shape(t, d);
+    bytes += t.rows * t.heads * d * (backward && t.gain ? 6 : 4);
     if (backward && s.gain) {
       if (!s.dgain) return refuse(CA_ERR_INVALID_ARG, std::string(names[i]) + ": dgain is null");
       t.dgain = parts + need / 4, g.parts[i] = t.dgain, g.out[i] = s.dgain, g.n[i] = t.blocks;
@@ -367,19 +414,20 @@ static int rotate(const ca_rotation *r, const ca_rotate_tensor *tensors, int n, 
   if (blocks > 0) {
     const Layout l = r->interleaved ? INTERLEAVED : r->rot_dim % 16 == 0 ? HALF : HALF_ANY;
     auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, st, a); };
-    auto by_layout = [&](auto dim, auto back) {
+    auto by_layout = [&](auto dim, auto back, auto past) {
       constexpr int D = decltype(dim)::value;
-      constexpr bool B = decltype(back)::value;
-      if (l == INTERLEAVED) launch(ca_rotate_kernel<D, INTERLEAVED, B>);
-      else if (l == HALF) launch(ca_rotate_kernel<D, HALF, B>);
-      else launch(ca_rotate_kernel<D, HALF_ANY, B>);
+      constexpr bool B = decltype(back)::value, S = decltype(past)::value;
+      if (l == INTERLEAVED) launch(ca_rotate_kernel<D, INTERLEAVED, B, S>);
+      else if (l == HALF) launch(ca_rotate_kernel<D, HALF, B, S>);
+      else launch(ca_rotate_kernel<D, HALF_ANY, B, S>);
     };
-    auto by_direction = [&](auto dim) { backward ? by_layout(dim, std::true_type{}) : by_layout(dim, std::false_type{}); };
+    auto by_size = [&](auto dim, auto back) { bytes > STREAM_BYTES ? by_layout(dim, back, std::true_type{}) : by_layout(dim, back, std::false_type{}); };
+    auto by_direction = [&](auto dim) { backward ? by_size(dim, std::true_type{}) : by_size(dim, std::false_type{}); };
     d == 128 ? by_direction(std::integral_constant<int, 128>{}) : by_direction(std::integral_constant<int, 64>{});
   }
   if (g.out[0] || g.out[1]) {
-    if (d == 128) hipLaunchKernelGGL(ca_rotate_gain_kernel<128>, dim3(128 / 16, 2), dim3(1024), 0, st, g);
-    else hipLaunchKernelGGL(ca_rotate_gain_kernel<64>, dim3(64 / 16, 2), dim3(1024), 0, st, g);
+    if (d == 128) hipLaunchKernelGGL(ca_rotate_gain_kernel<128>, dim3(128 / 4, 2), dim3(256), 0, st, g);
+    else hipLaunchKernelGGL(ca_rotate_gain_kernel<64>, dim3(64 / 4, 2), dim3(256), 0, st, g);
   }
   if (const hipError_t e = hipGetLastError(); e != hipSuccess)
     return refuse(CA_ERR_HIP, std::string("rotation: ") + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")");

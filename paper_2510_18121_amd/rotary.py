@@ -77,7 +77,10 @@ class Rotation:
         self.device = self.turns.device
         self.desc = RotationDesc(head_dim, self.rot_dim, self.interleaved, self.factor, self.turns.data_ptr() if freq.size else None)
         self.desc_ref = ctypes.byref(self.desc)
+        # what the calls look up every time
         self.index = self.turns.get_device() if self.turns.is_cuda else None  # (None: no tensor is there)
+        self.i32, self.f32, self.bf16 = torch.int32, torch.float32, torch.bfloat16
+        self.current_device, self.raw_stream = torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
     def __call__(self, q, k=None, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, eps=1e-6):
         """q and k [rows, heads, head_dim] (bf16; k may be None), turned, as contiguous tensors; differentiable in q, k and the gains (fp32

@@ -126,4 +126,4 @@ def test_gains_without_a_rotation_are_refused():
 
 
 def test_workspace_does_not_depend_on_the_call():
-    assert B.lib().ca_rotate_backward_workspace_bytes() == 2 * 2048 * 128 * 4
+    assert B.lib().ca_rotate_backward_workspace_bytes() == 2 * 1024 * 128 * 4
