@@ -35,9 +35,16 @@ __device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
   w[2] = __builtin_amdgcn_perm(d, b, 0x05040100), w[3] = __builtin_amdgcn_perm(d, b, 0x07060302);
 }
 
-// One wave per (page with tokens that are asked for, KV head, K or V).  K: a lane has 16 columns of a token; V: 8 columns of 16 (head_dim 64: 8) tokens.
-template <int D>
+// One wave per (page with tokens that are asked for, KV head, K or V).  K: a lane has 8 columns of a token; V: 8 columns of 16 (head_dim 64: 8) tokens.
+// STREAM: rows that the last cache does not hold until somebody reads them are stored past it.
+// (8 sequences of about 16K tokens, 8 heads of 128, 1.08 GB: 223 us, 215 past the cache, 5.0 TB/s; with the codes' loads past it too 220.  16 columns of a token
+// to a lane of K, whose stores are then halves of lines: 233 and 287.  A copy of 512 MB: 5.3 to 5.6 TB/s.)
+template <int D, bool STREAM>
 __global__ __launch_bounds__(256) void ca_cache_read_kernel(const ReadArgs a) {
+  auto put = [](u32x4 *p, const u32x4 &v) __attribute__((always_inline)) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+  };
   extern __shared__ __attribute__((aligned(16))) char smem[];
   SeqTable tab;
   auto first_pos = [](const Seq &q) { return max(0, q.len - q.n); };
@@ -56,17 +63,16 @@ __global__ __launch_bounds__(256) void ca_cache_read_kernel(const ReadArgs a) {
   const size_t at = size_t(max(page, 0)) * a.hkv + h, row = size_t(a.hkv) * D;
   const float f = page < 0 ? 0.f : (is_k ? a.k_scale : a.v_scale)[at];
   if (is_k) {
-    constexpr int LPT = D / 16, TPI = 64 / LPT;  // lanes per token, tokens per load
-    const uint8_t *const src = a.k + at * (PAGE * D) + 16 * (lane % LPT);
-    bf16_t *const dst = a.out_k + row0 * int64_t(row) + size_t(h) * D + 16 * (lane % LPT);
+    constexpr int LPT = D / 8, TPI = 64 / LPT;  // lanes per token, tokens per load
+    const uint8_t *const src = a.k + at * (PAGE * D) + 8 * (lane % LPT);
+    bf16_t *const dst = a.out_k + row0 * int64_t(row) + size_t(h) * D + 8 * (lane % LPT);
 #pragma unroll
     for (int i = 0; i < PAGE / TPI; ++i) {
       const int t = TPI * i + lane / LPT;
       if (t < begin || t >= end) continue;
-      u32x4 w = {0, 0, 0, 0};
-      if (page >= 0) w = *reinterpret_cast<const u32x4 *>(src + t * D);
-      u32x4 *const y = reinterpret_cast<u32x4 *>(dst + t * int64_t(row));
-      y[0] = codes_times(w[0], w[1], f), y[1] = codes_times(w[2], w[3], f);
+      u32x2 w = {0, 0};
+      if (page >= 0) w = *reinterpret_cast<const u32x2 *>(src + t * D);
+      put(reinterpret_cast<u32x4 *>(dst + t * int64_t(row)), codes_times(w[0], w[1], f));
     }
     return;
   }
@@ -97,7 +103,7 @@ __global__ __launch_bounds__(256) void ca_cache_read_kernel(const ReadArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int t = t0 + 4 * i + e;
-      if (t >= begin && t < end) *reinterpret_cast<u32x4 *>(dst + t * int64_t(row)) = codes_times(lo[e], hi[e], f);
+      if (t >= begin && t < end) put(reinterpret_cast<u32x4 *>(dst + t * int64_t(row)), codes_times(lo[e], hi[e], f));
     }
   }
 }
@@ -117,11 +123,13 @@ extern "C" int ca_cache_read(const ca_cache *c, const ca_cache_batch *b, void *k
   const int64_t touches = std::min<int64_t>(b->total_rows, b->total_rows / PAGE + 2 * int64_t(b->n_seqs));
   const int64_t groups = (touches * 2 * c->n_kv_heads + 3) / 4;
   if (groups > MOST_GROUPS) return fail(CA_ERR_UNSUPPORTED, "batch: rows times KV heads too many");
-  auto kern = c->head_dim == 128 ? ca_cache_read_kernel<128> : ca_cache_read_kernel<64>;
+  const bool past = b->total_rows * c->n_kv_heads * c->head_dim * 6 > int64_t(384) << 20;
+  auto kern = c->head_dim == 128 ? (past ? ca_cache_read_kernel<128, true> : ca_cache_read_kernel<128, false>)
+                                 : (past ? ca_cache_read_kernel<64, true> : ca_cache_read_kernel<64, false>);
   int device = 0;
   hipError_t e = hipGetDevice(&device);
-  static std::atomic<bool> done[2][16];
-  if (e == hipSuccess) e = set_smem(kern, int(seq_table_bytes(MAX_SEQS)), device, done[c->head_dim == 128]);
+  static std::atomic<bool> done[4][16];
+  if (e == hipSuccess) e = set_smem(kern, int(seq_table_bytes(MAX_SEQS)), device, done[2 * past + (c->head_dim == 128)]);
   if (e != hipSuccess) return launched("cache read", e);
   hipLaunchKernelGGL(kern, dim3(unsigned(groups)), dim3(256), seq_table_bytes(b->n_seqs), static_cast<hipStream_t>(hip_stream), a);
   return launched("cache read", hipSuccess);
