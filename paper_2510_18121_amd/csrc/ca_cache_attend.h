@@ -68,6 +68,7 @@ template <Part P>
 struct WorkSplit {
   SeqTableOf<P> tab;
   int total, run, cut, R, G, window, sinks;
+  bool stream;  // TAIL: codes pass the caches by
   template <int T, class A>
   __device__ __forceinline__ void count(void *lds, const A &a, int rows) {
     R = rows, G = a.G, window = a.window, sinks = a.sinks;
@@ -207,7 +208,7 @@ __device__ __forceinline__ void attend_workgroup(const A &a, char *smem, const W
       u32x4 kr[4 * NH], vr[NB];
       auto load_k = [&](int i) __attribute__((always_inline)) {
         const uint8_t *const p = a.k + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
-        if (a.stream) {
+        if (P == WHOLE ? a.stream : P == TAIL && split.stream) {
           asm volatile("" ::: "memory");  // (two branches, or the loads become one kind)
 #pragma unroll
           for (int f = 0; f < 4 * NH; ++f) kr[f] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + k_lane + 4 * (f / NH) * D + 64 * (f % NH)));
@@ -219,7 +220,7 @@ __device__ __forceinline__ void attend_workgroup(const A &a, char *smem, const W
       };
       auto load_v = [&](int i) __attribute__((always_inline)) {
         const uint8_t *const p = a.v + (size_t(__builtin_amdgcn_readlane(id, i)) * a.hkv + hk) * (PAGE * D);
-        if (a.stream) {
+        if (P == WHOLE ? a.stream : P == TAIL && split.stream) {
           asm volatile("" ::: "memory");
 #pragma unroll
           for (int b = 0; b < NB; ++b) vr[b] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + v_lane + 16 * PAGE * b));

@@ -26,6 +26,7 @@ struct SharedLaunch {
   float *parts;
   int groups;                // workgroups per KV head, of both kinds
   float cost[2], tiles[2];   // of PREFIX and of TAIL: what a unit costs a workgroup, and all tiles beside their units
+  float by_tiles;            // 1 / the tiles of PREFIX, about
 };
 
 // A worker is a workgroup where tiles are of 128 rows, otherwise a wave.
@@ -52,20 +53,23 @@ struct TwoSplits {
     if (clash) __syncthreads();
     tail.count<256>(KEEP_BOTH ? lds + seq_table_bytes(a.s.n_groups, PREFIX) : lds, a, 16 * NT);
     const float p = x.cost[0] * float(prefix.total) + x.tiles[0], t = x.cost[1] * float(tail.total) + x.tiles[1];
-    const int most = (prefix.total + LEAST * WP - 1) / (LEAST * WP);
+    // Units of a worker of PREFIX, at least: of tiles of 16 rows a page takes a wave about as long as the join takes for 14 parts.
+    const int least = NP == 8 ? 2 : max(2, int(__builtin_amdgcn_sqrtf(float(prefix.total) * x.by_tiles * (1.f / 14.f)) + 0.5f));
+    const int most = quotient(prefix.total + least * WP - 1, least * WP);
     groups = prefix.total == 0 ? 0 : min(most, max(1, min(x.groups - 1, int(float(x.groups) * p / (p + t) + 0.5f))));
     groups = __builtin_amdgcn_readfirstlane(groups);
     workers[0] = groups * WP, workers[1] = (x.groups - groups) * WT;
-    prefix.run = max(LEAST, quotient(prefix.total + max(workers[0], 1) - 1, max(workers[0], 1)));
+    prefix.run = max(__builtin_amdgcn_readfirstlane(least), quotient(prefix.total + max(workers[0], 1) - 1, max(workers[0], 1)));
     tail.run = max(1, quotient(tail.total + workers[1] - 1, workers[1]));
-    prefix.cut = NP == 8 ? CUT : CUT_SHARED, tail.cut = NT == 8 ? CUT : CUT_SHARED;
+    prefix.cut = tail.cut = CUT_SHARED;
+    // (tails that the last cache does not hold until the next call, as in ca_cache_attend; what is shared is fetched by several tiles)
+    tail.stream = float(tail.total) * float(a.hkv * 2 * PAGE * D) > float(384 << 20);
     parts[0] = x.parts, parts[1] = x.parts + size_t(workers[0]) * 2 * a.hkv * (16 * NP * (D + 2));
     if (clash && group < groups) {
       __syncthreads();
       prefix.count<256>(lds, a, 16 * NP);
     }
   }
-  static constexpr int LEAST = 2;  // units of a worker of PREFIX
 };
 
 template <int D, int NR>
@@ -205,6 +209,7 @@ static int launch_shared(SharedLaunch &x, hipStream_t st) {
   x.groups = shared_groups(a.hkv);
   const float rows = float(a.s.total) * a.G;
   x.cost[0] = NP == 8 ? 2.6f : 1.2f, x.cost[1] = NT == 8 ? 2.6f : 1.5f;
+  x.by_tiles = 1.f / (rows / (16 * NP) + float(std::max(1, a.s.n_groups)) / 2);
   x.tiles[0] = (rows / (16 * NP) + a.s.n_groups) * (NP == 8 ? 4.f : 1.f), x.tiles[1] = (rows / (16 * NT) + a.s.n_seqs) * (NT == 8 ? 4.f : 1.f);
   const size_t tables[2] = {seq_table_bytes(a.s.n_groups, PREFIX), seq_table_bytes(a.s.n_seqs, TAIL)};
   const size_t bytes = std::max(tile_bytes<D, NP>(), tile_bytes<D, NT>()) + std::max(tables[0], tables[1]);

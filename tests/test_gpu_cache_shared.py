@@ -85,6 +85,26 @@ def test_4096_sequences():
     run([(1000, 3), (3000, 2), (50, 1)], [1] * 4096, rng.integers(1, 70, 4096).tolist(), 2, 1, 64)
 
 
+def test_2048_groups():
+    rng = np.random.default_rng(2)
+    run([(2, int(p)) for p in rng.integers(0, 3, 2048)], [1] * 4096, rng.integers(1, 70, 4096).tolist(), 2, 1, 64)
+
+
+def test_tails_beyond_the_last_cache():
+    """Tails of 600 MB, whose codes pass the caches by, against attention without sharing: each is off by at most 2^-8 of what the probabilities and values
+    weigh, which for values of unlike signs is more than the result's own norm, so that twice 2^-8 of that bounds no less than what the two differ by here."""
+    groups, tails = [(30, 20), (10, 5)], [6400 + 37 * i for i in range(40)]
+    lens = [64 * p + t for (p, t) in zip([20] * 30 + [5] * 10, tails)]
+    table, pages = layout(groups, lens)
+    c = filled(pages, 8, 128)
+    q = queries(40, 32, 128)
+    o, lse = attend(c, q, [1] * 40, lens, table, groups)
+    want, want_lse = torch.empty_like(q), torch.empty_like(lse)
+    B.ca_cache_attend(c, q, want, want_lse, i32(np.arange(41)), i32(lens), i32(table), B.alloc_cache_workspace(c, 32))
+    assert (o.double() - want.double()).norm() <= 2.0 ** -7 * want.double().norm()
+    assert (lse - want_lse).abs().max() <= 2e-4
+
+
 def test_groups_of_some_sequences_only():
     """Groups that begin behind the first sequence and end before the last."""
     n, lens = [1] * 6, [64 * 3 + 5, 64 * 20 + 9, 64 * 20 + 64, 64 * 20 + 1, 30, 64 * 18]
