@@ -27,10 +27,11 @@ struct AttendArgsOf {
   __device__ __forceinline__ int token_of(int row) const { return G == 1 ? row : int(__umulhi(uint32_t(row), by_g)); }
 };
 using AttendArgs = AttendArgsOf<SeqArgs>;
-// PREFIX and TAIL: sums of a row and head, {m, l} behind them, of tiles that one worker had from their first page to their last.
+// PREFIX and TAIL: of tiles that one worker had from their first page to their last, a row and head's sums with {m, l} behind them.
 struct SharedArgs : AttendArgsOf<GroupedSeqs> {
-  float *row_sums[2], *row_ml[2];  // [total_rows][n_q_heads][D], [..][2]
+  float *row_sums[2];  // [total_rows][n_q_heads][row_floats(D)]
 };
+constexpr int row_floats(int d) { return d + 4; }
 
 // Rows of a sequence and KV head, token by token and then by head of the group, make up tiles of R = 16 NR; a unit of work is a page
 // of a tile.  The units of all sequences, in order, are dealt to the workers in equal runs, whatever the sequences' lengths
@@ -351,9 +352,9 @@ __device__ __forceinline__ void attend_workgroup(const A &a, char *smem, const W
         const int token = a.token_of(at), h = hk * G + at - token * G;
         if constexpr (P != WHOLE) {
           if (P == PREFIX || q.more > 0) {
-            const size_t i = size_t(q.row0 + token) * a.hq + h;
-            *reinterpret_cast<f32x4 *>(a.row_sums[P == TAIL] + i * D + c0 + col) = y;
-            if (stats) a.row_ml[P == TAIL][2 * i] = top, a.row_ml[P == TAIL][2 * i + 1] = all;
+            float *const sums = a.row_sums[P == TAIL] + (size_t(q.row0 + token) * a.hq + h) * row_floats(D);
+            *reinterpret_cast<f32x4 *>(sums + c0 + col) = y;
+            if (stats) sums[D] = top, sums[D + 1] = all;
             continue;
           }
         }
@@ -617,10 +618,10 @@ __device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, const Wo
         for (int rg = 0; rg < 2; ++rg) {
           const int r = row_w + 16 * rg + li, i = a.token_of(r);
           if (r > last_row) continue;
-          const size_t at = size_t(q.row0 + i) * a.hq + hk * G + r - i * G;
+          float *const sums = a.row_sums[P == TAIL] + (size_t(q.row0 + i) * a.hq + hk * G + r - i * G) * row_floats(D);
 #pragma unroll
-          for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4 *>(a.row_sums[P == TAIL] + at * D + 16 * b + 4 * j4) = acc[b][rg];
-          if (j4 == 0) a.row_ml[P == TAIL][2 * at] = m[rg], a.row_ml[P == TAIL][2 * at + 1] = sum[rg];
+          for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4 *>(sums + 16 * b + 4 * j4) = acc[b][rg];
+          if (j4 == 0) sums[D] = m[rg], sums[D + 1] = sum[rg];
         }
       }
     }

@@ -96,36 +96,32 @@ __global__ __launch_bounds__(256, 2) void ca_cache_shared_kernel(const SharedLau
 }
 
 // What there is of a row's tile: the parts of the workers that had a run of its pages each, or one sum of the row.
-template <int D>
 struct RowParts {
-  const float *first, *others, *first_ml, *others_ml;
-  size_t stride;  // from a worker's part to the next one's
+  const float *first, *others;
+  uint32_t stride;  // from a worker's part to the next one's
+  int sums, ml;     // where they are in a part
   int n;
-  template <Part P, class A>
+  template <Part P, int D, class A>
   __device__ __forceinline__ void of(const A &a, const WorkSplit<P> &split, const float *parts, int n_workers, int entry, const Seq &q, int row, int h, int hk) {
     const int R = split.R, G = a.G, r = (row - q.row0) * G + h - hk * G, tile = r / R, in_tile = r - tile * R;
     const int per = tile_pages(q.len, R, G, a.window, a.sinks), u0 = split.tab.before(entry) + tile * per;
     // (sequences that overlap, against their description, may have more units than are counted)
     const int w0 = min(quotient(u0, split.run), n_workers - 1), w1 = min(quotient(u0 + per - 1, split.run), n_workers - 1);
     if (per <= split.cut || w0 == w1) {
-      const size_t i = size_t(row) * a.hq + h;
-      n = 1, first = a.row_sums[P == TAIL] + i * D, first_ml = a.row_ml[P == TAIL] + 2 * i;
+      n = 1, sums = 0, ml = D, first = others = a.row_sums[P == TAIL] + (size_t(row) * a.hq + h) * row_floats(D);
       return;
     }
-    const size_t size = size_t(R) * (D + 2);
-    n = w1 - w0 + 1, stride = 2 * a.hkv * size;
-    const float *const p = parts + (size_t(2 * w0 + 1) * a.hkv + hk) * size;  // (the part of a tile that begins in a worker's run is its second)
-    first = p + in_tile * D, first_ml = p + R * D + 2 * in_tile;
-    const float *const o = parts + (size_t(2 * w0 + 2) * a.hkv + hk) * size;
-    others = o + in_tile * D, others_ml = o + R * D + 2 * in_tile;
+    const uint32_t size = R * (D + 2);
+    n = w1 - w0 + 1, stride = 2 * a.hkv * size, sums = in_tile * D, ml = R * D + 2 * in_tile;
+    first = parts + (size_t(2 * w0 + 1) * a.hkv + hk) * size;  // (the part of a tile that begins in a worker's run is its second)
+    others = parts + (size_t(2 * w0 + 2) * a.hkv + hk) * size;
   }
-  __device__ __forceinline__ const float *sum(int i) const { return i == 0 ? first : others + (i - 1) * stride; }
-  __device__ __forceinline__ const float *ml(int i) const { return i == 0 ? first_ml : others_ml + (i - 1) * stride; }
+  __device__ __forceinline__ const float *part(int i) const { return i == 0 ? first : others + uint32_t(i - 1) * size_t(stride); }
 };
 
 // A wave takes a row and head at a time: D / 4 lanes to a part.
 template <int D, int NP, int NT>
-__global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x, int rows_of_wave) {
+__global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   constexpr int LANES = D / 4, AT_A_TIME = 64 / LANES, LOADS = 8;
   const SharedArgs &a = x.a;
@@ -133,60 +129,63 @@ __global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x
   split.make<D, NP, NT, true>(smem, x, 0);
   const WorkSplit<PREFIX> &prefix = split.prefix;
   const WorkSplit<TAIL> &tail = split.tail;
-  const int lane = threadIdx.x & 63, mine = lane / LANES, col = 4 * (lane % LANES);
-  const int64_t wave = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = int64_t(a.s.total) * a.hq;
-  for (int64_t at = wave * rows_of_wave; at < min(n, (wave + 1) * rows_of_wave); ++at) {
-    const int row = int(at / a.hq), h = int(at - int64_t(row) * a.hq), hk = h / a.G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = lane / LANES, col = 4 * (lane % LANES);
+  for (int row = blockIdx.x; row < a.s.total; row += gridDim.x) {
     const int s = tail.tab.find_row(row);
     if (s < 0) continue;
     const Seq q = tail.tab.at(s);
     if (row < q.row0 || row >= q.row0 + q.n) continue;
-    RowParts<D> t, p;
-    t.template of<TAIL>(a, tail, split.parts[1], split.workers[1], s, q, row, h, hk);
-    p.n = 0;
+    int g = -1;
+    Seq of_group = {};
     if (q.more > 0) {
-      const int g = prefix.tab.find_row(row);
-      const Seq of_group = prefix.tab.at(max(g, 0));
-      if (g >= 0 && row >= of_group.row0 && row < of_group.row0 + of_group.n)
-        p.template of<PREFIX>(a, prefix, split.parts[0], split.workers[0], g, of_group, row, h, hk);
-    } else if (t.n == 1) {
-      continue;  // it is done
+      g = prefix.tab.find_row(row);
+      of_group = prefix.tab.at(max(g, 0));
+      if (row < of_group.row0 || row >= of_group.row0 + of_group.n) g = -1;
     }
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    float top = NO_MAX, sum = 0.f;
-    auto add = [&](float m, float l, const f32x4 &z) __attribute__((always_inline)) {
-      const float grown = fmaxf(top, m), old = fast_exp2(top - grown), w = fast_exp2(m - grown);
-      top = grown, sum = sum * old + w * l;
+    for (int h = 4 * blockIdx.y + wave; h < a.hq; h += 4 * gridDim.y) {
+      const int hk = a.token_of(h);  // h / G
+      RowParts t, p;
+      t.of<TAIL, D>(a, tail, split.parts[1], split.workers[1], s, q, row, h, hk);
+      if (q.more == 0 && t.n == 1) continue;  // it is done
+      p = t, p.n = 0;
+      if (g >= 0) p.of<PREFIX, D>(a, prefix, split.parts[0], split.workers[0], g, of_group, row, h, hk);
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+      float top = NO_MAX, sum = 0.f;
+      auto add = [&](float m, float l, const f32x4 &z) __attribute__((always_inline)) {
+        const float grown = fmaxf(top, m), old = fast_exp2(top - grown), w = fast_exp2(m - grown);
+        top = grown, sum = sum * old + w * l;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = y[e] * old + w * z[e];
-    };
-    const int n_parts = p.n + t.n;
-    for (int base = 0; base < n_parts; base += LOADS * AT_A_TIME) {  // (all of a round's loads before the first sum)
-      f32x4 z[LOADS];
-      f32x2 ml[LOADS];
+        for (int e = 0; e < 4; ++e) y[e] = y[e] * old + w * z[e];
+      };
+      const int n_parts = p.n + t.n;
+      for (int base = 0; base < n_parts; base += LOADS * AT_A_TIME) {  // (all of a round's loads before the first sum)
+        f32x4 z[LOADS];
+        f32x2 ml[LOADS];
 #pragma unroll
-      for (int k = 0; k < LOADS; ++k) {
-        const int i = min(base + k * AT_A_TIME + mine, n_parts - 1);
-        const bool in_prefix = i < p.n;
-        z[k] = *reinterpret_cast<const f32x4 *>((in_prefix ? p.sum(i) : t.sum(i - p.n)) + col);
-        ml[k] = *reinterpret_cast<const f32x2 *>(in_prefix ? p.ml(i) : t.ml(i - p.n));
+        for (int k = 0; k < LOADS; ++k) {
+          const int i = min(base + k * AT_A_TIME + mine, n_parts - 1);
+          const bool in_prefix = i < p.n;
+          const float *const from = in_prefix ? p.part(i) : t.part(i - p.n);
+          z[k] = *reinterpret_cast<const f32x4 *>(from + (in_prefix ? p.sums : t.sums) + col);
+          ml[k] = *reinterpret_cast<const f32x2 *>(from + (in_prefix ? p.ml : t.ml));
+        }
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k)
+          if (base + k * AT_A_TIME + mine < n_parts) add(ml[k][0], ml[k][1], z[k]);
       }
 #pragma unroll
-      for (int k = 0; k < LOADS; ++k)
-        if (base + k * AT_A_TIME + mine < n_parts) add(ml[k][0], ml[k][1], z[k]);
-    }
+      for (int o = LANES; o < 64; o <<= 1) {
+        f32x4 z;
 #pragma unroll
-    for (int o = LANES; o < 64; o <<= 1) {
-      f32x4 z;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[e] = __shfl_xor(y[e], o);
-      add(__shfl_xor(top, o), __shfl_xor(sum, o), z);
+        for (int e = 0; e < 4; ++e) z[e] = __shfl_xor(y[e], o);
+        add(__shfl_xor(top, o), __shfl_xor(sum, o), z);
+      }
+      if (mine != 0) continue;
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      *reinterpret_cast<u32x2 *>(a.o + (size_t(row) * a.hq + h) * D + col) =
+          u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
+      if (col == 0 && a.lse) a.lse[size_t(h) * a.s.total + row] = 0.6931471805599453f * (top + fast_log2(sum));
     }
-    if (mine != 0) continue;
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    *reinterpret_cast<u32x2 *>(a.o + (size_t(row) * a.hq + h) * D + col) =
-        u32x2{pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv)};
-    if (col == 0 && a.lse) a.lse[size_t(h) * a.s.total + row] = 0.6931471805599453f * (top + fast_log2(sum));
   }
 }
 
@@ -195,12 +194,12 @@ __global__ __launch_bounds__(256) void ca_cache_join_kernel(const SharedLaunch x
 static int shared_groups(int hkv) { return std::max(2, N_CU * 2 / hkv); }
 static size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
 struct SharedBytes {
-  size_t parts, sums, ml;  // sums, ml: of each kind
-  size_t all() const { return parts + 2 * (sums + ml); }
+  size_t parts, sums;  // sums: of each kind
+  size_t all() const { return parts + 2 * sums; }
 };
 static SharedBytes shared_bytes(int d, int hkv, int hq, int64_t rows) {
   // (parts: two of 128 rows for each workgroup, which is also room for two of 16 rows for each of its waves)
-  return {round_up(size_t(shared_groups(hkv)) * 2 * hkv * (128 * (d + 2)) * 4), round_up(size_t(rows) * hq * d * 4), round_up(size_t(rows) * hq * 2 * 4)};
+  return {round_up(size_t(shared_groups(hkv)) * 2 * hkv * (128 * (d + 2)) * 4), round_up(size_t(rows) * hq * row_floats(d) * 4)};
 }
 
 template <int D, int NP, int NT>
@@ -222,9 +221,8 @@ static int launch_shared(SharedLaunch &x, hipStream_t st) {
   if (e == hipSuccess) e = set_smem(join, int(seq_table_bytes(MAX_SEQS, PREFIX) + seq_table_bytes(MAX_SEQS, TAIL)), device, done[1]);
   if (e != hipSuccess) return launched("cache attention of groups", e);
   hipLaunchKernelGGL(kern, dim3(unsigned(a.hkv), unsigned(x.groups)), dim3(256), bytes, st, x);
-  const int64_t n = int64_t(a.s.total) * a.hq;
-  const int per = int(std::max<int64_t>(1, n / (N_CU * 64)));
-  hipLaunchKernelGGL(join, dim3(unsigned((n + 4 * per - 1) / (4 * per))), dim3(256), tables[0] + tables[1], st, x, per);
+  const int heads = std::min((a.hq + 3) / 4, 1 << 10), rows_at_a_time = std::min(a.s.total, std::max(1, N_CU * 64 / heads));
+  hipLaunchKernelGGL(join, dim3(unsigned(rows_at_a_time), unsigned(heads)), dim3(256), tables[0] + tables[1], st, x);
   return launched("cache attention of groups", hipSuccess);
 }
 
@@ -287,7 +285,6 @@ int ca_cache_attend_shared(const ca_cache *c, const ca_cache_batch *b, const ca_
   x.parts = reinterpret_cast<float *>(at), at += need.parts;
   for (int i = 0; i < 2; ++i) {
     a.row_sums[i] = reinterpret_cast<float *>(at), at += need.sums;
-    a.row_ml[i] = reinterpret_cast<float *>(at), at += need.ml;
   }
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   return c->head_dim == 128 ? shared_by_rows<128>(x, st) : shared_by_rows<64>(x, st);

@@ -107,7 +107,7 @@ def test_workspace_grows_with_the_rows():
         n = ctypes.c_size_t()
         assert B.lib().ca_cache_attend_shared_workspace_bytes(ctypes.byref(c), 32, rows, ctypes.byref(n)) == B.CA_OK
         sizes.append(n.value)
-    assert sizes[0] < sizes[1] <= sizes[2] < sizes[3] and sizes[3] - sizes[0] >= 2 * 1000 * 32 * (128 + 2) * 4
+    assert sizes[0] < sizes[1] <= sizes[2] < sizes[3] and sizes[3] - sizes[0] >= 2 * 1000 * 32 * (128 + 4) * 4
     assert B.lib().ca_cache_attend_shared_workspace_bytes(ctypes.byref(c), 33, 1, ctypes.byref(n)) == NOT
     assert B.lib().ca_cache_attend_shared_workspace_bytes(ctypes.byref(c), 32, -1, ctypes.byref(n)) == BAD
     assert B.lib().ca_cache_attend_shared_workspace_bytes(ctypes.byref(c), 32, 1, None) == BAD
