@@ -7,6 +7,15 @@
 // Here the rows of the whole group make up tiles of 128 rows (or 16, 32 where there are few), to which a page is fetched once: the prefix is
 // bound by the matrix products, 4 D flops per (row, head, token), and the tails by reading them.  Both go on side by side, in one launch of
 // workgroups of either kind (ca_cache_attend.h); a second one joins the results and the parts of the tiles that were cut.
+// Measured, whole calls (of which 9 to 10 us are the second launch and the gap before it), 8 KV heads of 128 unless noted, and ca_cache_attend beside it:
+//   64 tokens behind 8192, tails of about 560 tokens, 32 heads      44 us (106)
+//   32 tokens behind 130K, 64 heads                                184 to 195 us (703): 0.74 PFLOP/s, MFMAs 36 % busy
+//   24 drafts of 3 to 5 rows behind two prefixes of about 5000       40 us (51)
+//   200 tokens behind nine prefixes of up to 4000, 16/16 heads of 64  67 us (145): the tails' 165 MB in 45 of them
+//   8 tokens behind 2048                                            18 us (17): fixed times, 6 us from the start to the end of one page, most of it cold code and trips to memory
+// It pays from about 16 sequences of 8192 shared tokens, or 64 of 512, on; 2 to 8 sequences behind less than 8192 tokens are 1 to 5 us faster without.
+// Not kept: every workgroup with a share of both kinds (47 to 51 us, 190, 52, 76 in the first four: a second start costs what the balance gains); runs by what a
+// workgroup has beside it on its CU (46 to 49, 184 to 218); tails with workgroups of four waves (200 behind nine: 88); P of the tails as one operand (level).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -44,6 +53,7 @@ struct TwoSplits {
   // KEEP_BOTH: tables of both (lds has room for them); otherwise of the kind that the workgroup is of.
   template <int D, int NP, int NT, bool KEEP_BOTH>
   __device__ __forceinline__ void make(char *lds, const SharedLaunch &x, int group) {
+#pragma clang fp contract(off)  // both launches have to come to the same numbers
     const SharedArgs &a = x.a;
     const bool clash = !KEEP_BOTH && a.s.n_groups > 64;  // both tables lie in LDS
     constexpr int WP = waves_apart(NP), WT = waves_apart(NT);
@@ -52,6 +62,7 @@ struct TwoSplits {
     prefix.count<256>(lds, a, 16 * NP);
     if (clash) __syncthreads();
     tail.count<256>(KEEP_BOTH ? lds + seq_table_bytes(a.s.n_groups, PREFIX) : lds, a, 16 * NT);
+    // (a unit of 128 rows to one of 16: 2.6 to 1.5.  With 1.8 and with 3.5 to 1.5 64 tokens behind 8192 take 50 and 46 us, not 44.5, 32 behind 130K 198 and 192, not 185.)
     const float p = x.cost[0] * float(prefix.total) + x.tiles[0], t = x.cost[1] * float(tail.total) + x.tiles[1];
     // Units of a worker of PREFIX, at least: of tiles of 16 rows a page takes a wave about as long as the join takes for 14 parts.
     const int least = NP == 8 ? 2 : max(2, int(__builtin_amdgcn_sqrtf(float(prefix.total) * x.by_tiles * (1.f / 14.f)) + 0.5f));
