@@ -158,7 +158,7 @@ class Sequences:
     def groups(self, seqs, rows, device=None):
         """group_start and prefix_pages (int32) of binding.ca_cache_attend_shared, for a call with the last rows[i] tokens of seqs[i]: neighbours in `seqs`
         that share their first pages make up groups, so that the most pages are read once instead of again.  (The arrays stay right
-        as long as the same sequences grow: they are made when sequences come and go.)"""
+        as long as the same sequences grow: they are made anew when sequences come or go, or let go of pages.)"""
         seqs, rows = list(seqs), [operator.index(n) for n in rows]
         if len(seqs) != len(rows):
             raise ValueError("groups: one count of rows for each of the sequences")

@@ -252,7 +252,4 @@ inline int launched(const char *what, hipError_t e) {
   if (e == hipSuccess) return CA_OK;
   return fail(CA_ERR_HIP, std::string(what) + ": " + hipGetErrorName(e) + " (" + hipGetErrorString(e) + ")");
 }
-
-// Workers of W waves per KV head: as many as are on the chip at a time (NR: 16-row groups of a tile; 8: chunks), eight waves to a CU.  Of tiles of
-
 }  // namespace ca

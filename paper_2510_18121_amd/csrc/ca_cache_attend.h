@@ -652,6 +652,8 @@ __device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, const Wo
 }
 
 // ------------------------------------------------------------------------------------------------ launches
+// Workers of W waves per KV head: as many as are on the chip at a time (NR: 16-row groups of a tile; 8: chunks), eight waves to a CU.  Of tiles of
+// 32 rows at head_dim 128 four (352 registers: in 256, 23 of them spill, and 64 sequences of about 4096 tokens with 8 rows each take 204 us, not 197;
 // at head_dim 64 eight waves take 110, four 176).  Of chunks at head_dim 64 twelve, where tiles are long (4 chunks of 500 rows behind 8192 tokens, 32/8 heads: 224 us
 // with eight, 200 with twelve).  Where they are short it goes by how the tiles fill the chip, which this rule does not know: one prompt of 1000, 32/32 heads, 26 us with
 // eight and 33 with twelve, sixteen with 8/8 55 and 65; but eight of 512 with 32/8 48 and 36, sixteen of 1000 with 16/16 98 and 74.

@@ -86,31 +86,33 @@ class Rotation:
         """q and k [rows, heads, head_dim] (bf16; k may be None), turned, as contiguous tensors; differentiable in q, k and the gains (fp32
         or bf16 [head_dim]).  Positions: q_pos and k_pos (int32 [rows]; k_pos None: those of q), or where = (q_start, kv_len, ..) of sequences
         (see binding.ca_rotate).  Rows of no sequence are undefined, and their gradients zero."""
-        gains = [None if g is None else g.float() for g in (q_gain, k_gain)]
-        out = _Rotate.apply(q, k, *gains, self, q_pos, k_pos, None if where is None else tuple(where[:2]), float(eps))
+        gains = [None if g is None else g.float().contiguous() for g in (q_gain, k_gain)]
+        q_start, kv_len = (None, None) if where is None else where[:2]
+        out = _Rotate.apply(q, k, *gains, self, q_pos, k_pos, q_start, kv_len, float(eps))
         return out if k is not None else out[0]
 
 
 class _Rotate(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, q_gain, k_gain, rotation, q_pos, k_pos, where, eps):
+    def forward(ctx, q, k, q_gain, k_gain, rotation, q_pos, k_pos, q_start, kv_len, eps):
         from . import binding as B
         yq, yk = (None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k))
-        B.ca_rotate(rotation, q, k, yq, yk, q_pos, k_pos, where, q_gain, k_gain, eps)
+        B.ca_rotate(rotation, q, k, yq, yk, q_pos, k_pos, None if q_start is None else (q_start, kv_len), q_gain, k_gain, eps)
         # (without a gain the gradient needs no input)
-        ctx.save_for_backward(*(x if g is not None else None for x, g in ((q, q_gain), (k, k_gain))), q_gain, k_gain)
-        ctx.rotation, ctx.pos, ctx.where, ctx.eps = rotation, (q_pos, k_pos), where, eps
+        ctx.save_for_backward(*(x if g is not None else None for x, g in ((q, q_gain), (k, k_gain))), q_gain, k_gain, q_pos, k_pos, q_start, kv_len)
+        ctx.rotation, ctx.eps = rotation, eps
         return yq, yk
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dyq, dyk):
         from . import binding as B
-        q, k, q_gain, k_gain = ctx.saved_tensors
+        q, k, q_gain, k_gain, q_pos, k_pos, q_start, kv_len = ctx.saved_tensors
+        where = None if q_start is None else (q_start, kv_len)
         dys = [None if d is None else B.rows_in_line(d) for d in (dyq, dyk)]
-        make = torch.empty if ctx.where is None else torch.zeros  # (rows of no sequence)
+        make = torch.empty if where is None else torch.zeros  # (rows of no sequence)
         dx = [None if d is None else make(d.shape, dtype=d.dtype, device=d.device) for d in dys]
         dg = [None if g is None else torch.empty_like(g) for g in (q_gain, k_gain)]
         ws = B.alloc_rotate_workspace(dys[0].device) if q_gain is not None or k_gain is not None else None
-        B.ca_rotate_backward(ctx.rotation, q, k, *dys, *dx, *ctx.pos, ctx.where, q_gain, k_gain, *dg, ctx.eps, ws)
-        return *dx, *dg, None, None, None, None, None
+        B.ca_rotate_backward(ctx.rotation, q, k, *dys, *dx, q_pos, k_pos, where, q_gain, k_gain, *dg, ctx.eps, ws)
+        return *dx, *dg, None, None, None, None, None, None

@@ -224,6 +224,29 @@ def test_second_gradients_are_refused():
         dq.sum().backward()
 
 
+def test_positions_that_change_before_the_backward_are_noticed():
+    r, q = R.Rotation(64, device=DEV), rand(3, 1, 64).requires_grad_()
+    pos, start, lens = i32([1, 2, 3]), i32([0, 3]), i32([9])
+    for y, changed in ((r(q, None, pos), pos), (r(q, None, where=(start, lens)), lens)):
+        changed += 1
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad(y, q, torch.ones_like(y))
+
+
+def test_gains_that_are_strided_and_frequencies_of_every_kind():
+    """A gain out of a larger tensor; slowed frequencies, negative ones, and far positions of them."""
+    freq = np.concatenate([R.by_parts(R.frequencies(40, 1e4), 8, 4096), [-0.3, 0.0, 6.5]])
+    r = R.Rotation(64, frequencies=freq, factor=0.7, device=DEV)
+    q, pos = rand(9, 2, 64), i32([0, 1, 2 ** 31 - 1, -(2 ** 31), 4096, 77777777, -1, 3, 2 ** 30])
+    both = torch.stack([gain_of(64, 1), gain_of(64, 2)], 1).requires_grad_()
+    y = r(q, None, pos, q_gain=both[:, 1])
+    U.close(y.detach(), *U.forward(q, pos, freq, False, 0.7, both[:, 1].detach()))
+    dg, = torch.autograd.grad(y, both, torch.ones_like(y))
+    _, want, _, far = U.backward(q, torch.ones_like(q), pos, freq, False, 0.7, both[:, 1].detach())
+    U.close_gain(dg[:, 1], want, far)
+    assert (dg[:, 0] == 0).all()
+
+
 def test_no_gradient_reaches_rows_of_no_sequence():
     r, q = R.Rotation(64, device=DEV), rand(5, 2, 64).requires_grad_()
     y = r(q, None, where=(i32([1, 4]), i32([9])))
