@@ -160,6 +160,24 @@ def test_graph_follows_the_lengths_and_streams():
             same(g.cpu(), w)
 
 
+@pytest.mark.parametrize("heads,d", [(8, 128), (16, 64)])
+def test_rows_beyond_the_last_cache(heads, d):
+    """More than 384 MiB, which is stored past the caches: the same bits as a sequence at a time."""
+    lens = [17001, 20000, 64 * 300, 13333]
+    table, pages = U.layout(lens, seed=7)
+    c = filled(pages, heads, d)
+    t = i32(table)
+    k, v = (torch.full((sum(lens) + 3, heads, d), 9.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    B.ca_cache_read(c, k, v, i32(np.concatenate([[0], np.cumsum(lens)])), i32(lens), t)
+    row = 0
+    for i, n in enumerate(lens):
+        ki, vi = (torch.empty(n, heads, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        B.ca_cache_read(c, ki, vi, i32([0, n]), i32([n]), t[i:i + 1])
+        assert torch.equal(k[row:row + n], ki) and torch.equal(v[row:row + n], vi)
+        row += n
+    assert (k[row:] == 9).all() and (v[row:] == 9).all()
+
+
 def test_pages_beyond_4_gib():
     c = KVCache.empty((1 << 32) // (8 * 64 * 128) + 9, 8, 128, DEV)
     table = np.array([[c.n_pages - 2, 1, c.n_pages - 1]], np.int32)

@@ -73,6 +73,30 @@ def test_many_rows_of_few_heads_and_of_many(interleaved, rot):
     U.close(dk, want, far, 2.0 ** -18)
 
 
+@pytest.mark.parametrize("d,rot,interleaved", [(128, 128, False), (128, 64, True), (128, 42, False), (64, 64, False), (64, 32, True), (64, 26, False)])
+def test_tensors_beyond_the_last_cache(d, rot, interleaved):
+    """More than 384 MiB read and written, which passes the caches by: the same bits as in pieces of less."""
+    r = R.Rotation(d, frequencies=R.frequencies(rot), interleaved=interleaved, device=DEV)
+    rows, heads = 41003, 20 * 128 // d
+    q, dy, pos, g = rand(rows, heads, d), rand(rows, heads, d, seed=1), positions(rows), gain_of(d, 2)
+    ws = B.alloc_rotate_workspace(DEV)
+
+    def both(a, e):
+        y, dx, dg = torch.empty_like(q[a:e]), torch.empty_like(q[a:e]), torch.empty(d, device=DEV)
+        B.ca_rotate(r, q[a:e], None, y, None, pos[a:e], q_gain=g)
+        B.ca_rotate_backward(r, q[a:e], None, dy[a:e], None, dx, None, pos[a:e], q_gain=g, dq_gain=dg, ws=ws)
+        return y, dx, dg
+
+    y, dx, dg = both(0, rows)
+    parts = [both(a, min(a + 14000, rows)) for a in range(0, rows, 14000)]
+    assert torch.equal(y, torch.cat([p[0] for p in parts])) and torch.equal(dx, torch.cat([p[1] for p in parts]))
+    tail = slice(rows - 500, rows)
+    U.close(y[tail], *U.forward(q[tail], pos[tail], r.frequencies, interleaved, 1.0, g))
+    # (sums of up to 512 terms one after the other here too; the magnitudes of all terms)
+    far = U.backward(q[tail], dy[tail], pos[tail], r.frequencies, interleaved, 1.0, g)[3] * (rows / 500) * 1.2
+    assert ((dg - sum(p[2] for p in parts)).abs() <= 2.0 ** -14 * far).all()
+
+
 def test_rows_of_a_joint_projection_and_in_place():
     r = R.Rotation(128, device=DEV)
     joint = rand(50, 6 * 128 + 8)
