@@ -85,7 +85,8 @@ class Rotation:
     def __call__(self, q, k=None, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, eps=1e-6):
         """q and k [rows, heads, head_dim] (bf16; k may be None), turned, as contiguous tensors; differentiable in q, k and the gains (fp32
         or bf16 [head_dim]).  Positions: q_pos and k_pos (int32 [rows]; k_pos None: those of q), or where = (q_start, kv_len, ..) of sequences
-        (see binding.ca_rotate).  Rows of no sequence are undefined, and their gradients zero."""
+        (see binding.ca_rotate).  Rows of no sequence are undefined, and their gradients zero.  A training pass is captured into a graph with
+        torch.autograd.grad, while no eager graph of the same leaves lives."""
         gains = [None if g is None else g.float().contiguous() for g in (q_gain, k_gain)]
         q_start, kv_len = (None, None) if where is None else where[:2]
         out = _Rotate.apply(q, k, *gains, self, q_pos, k_pos, q_start, kv_len, float(eps))

@@ -311,6 +311,37 @@ def test_graph_and_streams():
         U.close(got[0], *U.forward(q, pos, r.frequencies, False, 1.0, g))
 
 
+def test_captured_training_pass():
+    """Forward and gradients captured once, with gradients asked of autograd for the leaves directly, and replayed as inputs, positions and gains change."""
+    r = R.Rotation(64, device=DEV)
+    leaves = [rand(50, 4, 64).requires_grad_(), rand(50, 2, 64, seed=1).requires_grad_(), gain_of(64, 2).requires_grad_(), gain_of(64, 3).requires_grad_()]
+    pos, dys = positions(50), [rand(50, 4, 64, seed=4), rand(50, 2, 64, seed=5)]
+
+    def train(q, k, gq, gk):
+        ys = r(q, k, pos, q_gain=gq, k_gain=gk)
+        return *(y.detach() for y in ys), *torch.autograd.grad(ys, (q, k, gq, gk), dys)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        train(*leaves)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = train(*leaves)
+    for i in range(3):
+        with torch.no_grad():
+            leaves[0].copy_(rand(50, 4, 64, seed=20 + i)), leaves[2].mul_(1.1)
+        pos += 1000
+        for t in out:
+            t.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = train(*(t.detach().clone().requires_grad_() for t in leaves))
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
 @pytest.mark.parametrize("window", [None, 40])
 def test_attention_server_with_a_rotation(window):
     """The same bits as turning first; positions are those in the documents, for shards in any order."""
