@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import operator
 import os
+import struct
 
 import numpy as np
 
@@ -531,8 +532,8 @@ def rows_in_line(t):
 
 def _rows(rotation, t, shape, name):
     """Address and row stride of a bf16 tensor [rows, heads, head_dim] on the rotation's device, each of whose rows is one run of memory."""
-    rows, heads, d = shape
-    if t.shape == shape and t.dtype is rotation.bf16 and t.get_device() == rotation.index:
+    if t.dtype is rotation.bf16 and t.shape == shape and t.get_device() == rotation.index:
+        rows, heads, d = shape
         if t.is_contiguous():
             return t.data_ptr(), heads * d
         s = t.stride()
@@ -543,43 +544,45 @@ def _rows(rotation, t, shape, name):
 
 
 def _line(rotation, t, shape, dtype, name):
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != rotation.index or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != rotation.index or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous tensor {tuple(shape)} {dtype} on {rotation.device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
+# Descriptions as packed bytes, which take a third of the time of a ctypes.Structure (these calls run once per layer and token too).
+_ROTATE_TENSOR = struct.Struct("=6Q4qi4x")  # ca_rotate_tensor
+_ROTATE_WHERE = struct.Struct("=iiq3Q")     # ca_cache_batch
+
+
 def _rotate_tensor(rotation, x, dy, y, pos, where, gain, dgain, name):
-    """The fields of a ca_rotate_tensor; x None: of a gradient without a gain."""
+    """A ca_rotate_tensor; x None: of a gradient without a gain."""
     shape = y.shape
     if len(shape) != 3 or shape[2] != rotation.head_dim:
         raise ValueError(f"{name}: expected [rows, heads, {rotation.head_dim}], got {tuple(shape)}")
-    xp = xs = dp = ds = gp = dgp = pp = None
-    yp, ys = _rows(rotation, y, shape, name + " (out)")
+    xp = xs = dp = ds = gp = dgp = pp = 0
+    yp, ys = _rows(rotation, y, shape, name)
     if x is not None:
         xp, xs = _rows(rotation, x, shape, name)
     if dy is not None:
-        dp, ds = _rows(rotation, dy, shape, "gradient of " + name)
+        dp, ds = _rows(rotation, dy, shape, name)
     if gain is not None:
-        gp = _line(rotation, gain, shape[2:], rotation.f32, "gain of " + name)
+        gp = _line(rotation, gain, shape[2:], rotation.f32, name)
         if dy is not None:
-            dgp = _line(rotation, dgain, shape[2:], rotation.f32, "gradient of the gain of " + name)
+            dgp = _line(rotation, dgain, shape[2:], rotation.f32, name)
     if where is None:
         if pos is None:
             raise ValueError(f"{name}: neither positions nor sequences are given")
-        pp = _line(rotation, pos, shape[:1], rotation.i32, "positions of " + name)
-    return xp, dp, yp, gp, dgp, pp, shape[0], xs or 0, ds or 0, ys, shape[1]
-
-
-_RotateTensors = RotateTensor * 2
+        pp = _line(rotation, pos, shape[:1], rotation.i32, name)
+    return _ROTATE_TENSOR.pack(xp, dp, yp, gp, dgp, pp, shape[0], xs, ds, ys, shape[1])
 
 
 def _rotate_where(rotation, where, rows):
     """The sequences as a ca_cache_batch, or None."""
     if where is None:
         return None
-    n = where[1].shape[0]
-    return ctypes.byref(CacheBatch(n, 0, rows, _line(rotation, where[0], (n + 1,), rotation.i32, "q_start"),
-                                   _line(rotation, where[1], (n,), rotation.i32, "kv_len"), None))
+    start, lens = where[0], where[1]
+    n = lens.shape[0]
+    return _ROTATE_WHERE.pack(n, 0, rows, _line(rotation, start, (n + 1,), rotation.i32, "q_start"), _line(rotation, lens, (n,), rotation.i32, "kv_len"), 0)
 
 
 def _rotate_stream(rotation, stream):
@@ -595,31 +598,30 @@ def ca_rotate(rotation, q, k, q_out, k_out, q_pos=None, k_pos=None, where=None, 
     (rotation: rotary.Rotation).  q, k and the outputs: bf16 [rows, heads, head_dim], each row a run of memory, so that views of a joint projection
     will do; an output may be its input.  Positions: q_pos and k_pos (device int32 [rows]; k_pos None: those of q), or where = (q_start, kv_len, ..) of
     the sequences of a call on a cache: rows are their last ones, and rows of no sequence are left as they are.  Gains: fp32 [head_dim]."""
-    first = _rotate_tensor(rotation, q, None, q_out, q_pos, where, q_gain, None, "q")
-    if k is None:
-        n, tensors = 1, _RotateTensors(first)
-    else:
-        n, tensors = 2, _RotateTensors(first, _rotate_tensor(rotation, k, None, k_out, q_pos if k_pos is None else k_pos, where, k_gain, None, "k"))
-    _check(lib().ca_rotate(rotation.desc_ref, tensors, n, _rotate_where(rotation, where, first[6]), eps, _rotate_stream(rotation, stream)))
+    n, tensors = 1, _rotate_tensor(rotation, q, None, q_out, q_pos, where, q_gain, None, "q, its output, positions or gain")
+    if k is not None:
+        n, tensors = 2, tensors + _rotate_tensor(rotation, k, None, k_out, q_pos if k_pos is None else k_pos, where, k_gain, None,
+                                                 "k, its output, positions or gain")
+    _check(lib().ca_rotate(rotation.desc_ref, tensors, n, _rotate_where(rotation, where, q.shape[0]), eps, _rotate_stream(rotation, stream)))
 
 
 def ca_rotate_backward(rotation, q, k, dq_out, dk_out, dq, dk, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, dq_gain=None,
                        dk_gain=None, eps=1e-6, ws=None, stream=None):
     """Gradients of ca_rotate: dq and dk (may be dq_out and dk_out) and, with gains, dq_gain and dk_gain (fp32 [head_dim]), from dq_out and dk_out
     (dk_out None: of q alone).  q and k are needed where there is a gain, as is ws (alloc_rotate_workspace)."""
-    tensors = []
+    n, tensors, rows = 0, b"", 0
     for x, dy, dx, pos, gain, dgain, name in ((q, dq_out, dq, q_pos, q_gain, dq_gain, "q"),
                                               (k, dk_out, dk, q_pos if k_pos is None else k_pos, k_gain, dk_gain, "k")):
         if dy is None:
             continue
         if gain is not None and (x is None or dgain is None):
             raise ValueError(f"{name}: with a gain the gradient needs the input, and a tensor for that of the gain")
-        tensors.append(_rotate_tensor(rotation, x if gain is not None else None, dy, dx, pos, where, gain, dgain, name))
-    if not tensors:
+        tensors += _rotate_tensor(rotation, x if gain is not None else None, dy, dx, pos, where, gain, dgain, f"{name}, its gradients, positions or gain")
+        n, rows = n + 1, dy.shape[0]
+    if n == 0:
         raise ValueError("neither dq_out nor dk_out")
     wp, wn = (None, 0) if ws is None else (_line(rotation, ws, ws.shape, ws.dtype, "ws"), ws.numel() * ws.element_size())
-    _check(lib().ca_rotate_backward(rotation.desc_ref, _RotateTensors(*tensors), len(tensors), _rotate_where(rotation, where, tensors[0][6]), eps, wp, wn,
-                                    _rotate_stream(rotation, stream)))
+    _check(lib().ca_rotate_backward(rotation.desc_ref, tensors, n, _rotate_where(rotation, where, rows), eps, wp, wn, _rotate_stream(rotation, stream)))
 
 
 def alloc_rotate_workspace(device="cuda"):

@@ -49,16 +49,16 @@ __device__ __forceinline__ Seq seq_from(const SeqArgs &a, int start, int end, in
   return q;
 }
 __device__ __forceinline__ Seq seq_of(const SeqArgs &a, int s) { return seq_from(a, a.q_start[s], a.q_start[s + 1], a.kv_len[s]); }
-// What the groups' arrays say, and the first 64 entries of q_start, one per lane, so that what is looked up in them costs no further trips to memory.
+// What the arrays say of the first 64 groups and sequences, one per lane, all of it in one trip to memory.
 struct GroupLanes {
   int start, end, pages;  // of this lane's group
-  int row;                // q_start of this lane
+  int row, row_end, len;  // q_start of this lane and of the next, kv_len
   int n;                  // groups
   __device__ __forceinline__ void load(const GroupedSeqs &a) {
     const int lane = threadIdx.x & 63, g = min(lane, max(a.n_groups - 1, 0));
     n = a.n_groups, start = end = pages = 0;
     if (n > 0) start = a.group_start[g], end = a.group_start[g + 1], pages = a.prefix_pages[g];
-    row = a.q_start[min(lane, a.n_seqs)];
+    row = a.q_start[min(lane, a.n_seqs)], row_end = a.q_start[min(lane + 1, a.n_seqs)], len = a.kv_len[min(lane, a.n_seqs - 1)];
   }
   __device__ __forceinline__ int row_of(const GroupedSeqs &a, int i) const {  // q_start[i], of any lane's own i
     if (a.n_seqs < 64) return __shfl(row, i);
@@ -97,7 +97,7 @@ __device__ __forceinline__ Seq group_as_seq(const GroupedSeqs &a, const GroupLan
   return q;
 }
 __device__ __forceinline__ Seq tail_of(const GroupedSeqs &a, const GroupLanes &l, int s) {
-  Seq q = seq_of(a, s);
+  Seq q = a.n_seqs <= 64 ? seq_from(a, l.row, l.row_end, l.len) : seq_of(a, s);
   const int shared = l.shared_by(a, s);
   if (q.len - q.n >= shared * PAGE) q.more = shared, q.len -= shared * PAGE;
   return q;
@@ -149,7 +149,7 @@ struct SeqTableOf {
       group_start = a.group_start, last = a.n_seqs;
     }
     if (n_seqs <= 64) {
-      mine = entry(a, min(lane, n_seqs - 1));
+      mine = entry(a, min(lane, n_seqs - 1));  // (of lanes behind the last one nothing is used)
       upto = wave_prefix(lane < n_seqs ? units(mine) : 0);
       return __builtin_amdgcn_readlane(upto, 63);
     }

@@ -80,7 +80,9 @@ class Rotation:
         # what the calls look up every time
         self.index = self.turns.get_device() if self.turns.is_cuda else None  # (None: no tensor is there)
         self.i32, self.f32, self.bf16 = torch.int32, torch.float32, torch.bfloat16
-        self.current_device, self.raw_stream = torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        # (where there is a tensor on a device it is initialised, which is what torch.cuda.current_device looks at first)
+        self.current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
     def __call__(self, q, k=None, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, eps=1e-6):
         """q and k [rows, heads, head_dim] (bf16; k may be None), turned, as contiguous tensors; differentiable in q, k and the gains (fp32

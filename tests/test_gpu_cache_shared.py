@@ -90,6 +90,37 @@ def test_2048_groups():
     run([(2, int(p)) for p in rng.integers(0, 3, 2048)], [1] * 4096, rng.integers(1, 70, 4096).tolist(), 2, 1, 64)
 
 
+def test_more_kv_heads_than_workgroups_of_a_kind():
+    run([(3, 6)], [1, 2, 1], [5, 70, 64], 300, 300, 64)
+    run([(40, 5)], [1] * 40, [5 + i for i in range(40)], 260, 260, 64)
+
+
+def test_two_streams_with_a_workspace_each():
+    """Calls that overlap in time: each as it is alone."""
+    jobs = []
+    for i, (groups, seqs, hq, hkv, d) in enumerate((([(40, 40)], 40, 32, 8, 128), ([(5, 30), (6, 50)], 11, 16, 16, 64))):
+        lens = [64 * p + 100 + 7 * j for j, p in enumerate([p for m, p in groups for _ in range(m)])]
+        table, pages = layout(groups, lens, seed=i)
+        c, q = filled(pages, hkv, d, seed=i), queries(seqs, hq, d, seed=i)
+        where = [i32(x) for x in (np.arange(seqs + 1), lens, table, np.concatenate([[0], np.cumsum([m for m, _ in groups])]), [p for _, p in groups])]
+        jobs.append((c, q, where, B.alloc_shared_workspace(c, hq, seqs), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    alone = []
+    for c, q, where, ws, _ in jobs:
+        o = torch.empty_like(q)
+        B.ca_cache_attend_shared(c, q, o, None, *where, ws)
+        torch.cuda.synchronize()
+        alone.append(o)
+    outs = [[torch.empty_like(q) for _ in range(20)] for _, q, _, _, _ in jobs]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for (c, q, where, ws, stream), out in zip(jobs, outs):
+            B.ca_cache_attend_shared(c, q, out[i], None, *where, ws, stream=stream)
+    torch.cuda.synchronize()
+    for a, out in zip(alone, outs):
+        assert all(torch.equal(a, o) for o in out)
+
+
 def test_tails_beyond_the_last_cache():
     """Tails of 600 MB, whose codes pass the caches by, against attention without sharing: each is off by at most 2^-8 of what the probabilities and values
     weigh, which for values of unlike signs is more than the result's own norm, so that twice 2^-8 of that bounds no less than what the two differ by here."""
