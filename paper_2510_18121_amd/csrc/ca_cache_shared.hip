@@ -12,7 +12,7 @@
 //   32 tokens behind 130K, 64 heads                                184 to 195 us (703): 0.74 PFLOP/s, MFMAs 36 % busy
 //   24 drafts of 3 to 5 rows behind two prefixes of about 5000       40 us (51)
 //   200 tokens behind nine prefixes of up to 4000, 16/16 heads of 64  67 us (145): the tails' 165 MB in 45 of them
-//   8 tokens behind 2048                                            18 us (17): fixed times, 6 us from the start to the end of one page, most of it cold code and trips to memory
+//   8 tokens behind 2048                                            17 us (17): fixed times, 6 us from the start to the end of one page, most of it cold code and trips to memory
 // It pays from about 16 sequences of 8192 shared tokens, or 64 of 512, on; 2 to 8 sequences behind less than 8192 tokens are 1 to 5 us faster without.
 // Not kept: every workgroup with a share of both kinds (47 to 51 us, 190, 52, 76 in the first four: a second start costs what the balance gains); runs by what a
 // workgroup has beside it on its CU (46 to 49, 184 to 218); tails with workgroups of four waves (200 behind nine: 88); P of the tails as one operand (level).
