@@ -273,8 +273,8 @@ int ca_cache_attend_workspace_bytes(const ca_cache *cache, int32_t n_q_heads, si
  * for all rows of a group.  Group g: sequences group_start[g] .. group_start[g + 1] - 1, the first prefix_pages[g] entries of whose page_table
  * rows are the same (those of the group's first sequence are taken for all); sequences of no group, and groups of 0 pages, share nothing.  The arrays are DEVICE
  * memory, read when the kernels run.  What is shared are whole pages that every row of a sequence sees: a sequence of which kv_len - (its
- * rows) is less than 64 prefix_pages is attended by itself, from its own entries.  Results are those of ca_cache_attend but for the order of sums and the rounding of P, which goes
- * by the rows per group here and there by the rows per sequence: of the shared tokens bf16 where a group has more than 32 rows on average (queries times heads of a KV head).
+ * rows) is less than 64 prefix_pages is attended by itself, from its own entries.  Results are those of ca_cache_attend but for the order of sums: P is rounded as there, by the
+ * average rows per sequence, whatever the groups.
  * ws: device workspace of ca_cache_attend_shared_workspace_bytes (of this many rows or fewer), 256-byte aligned, written; calls that may overlap in time need one each.
  * Two launches on hip_stream; allocates nothing, never synchronises, bit-reproducible.
  */

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void ca_cache_chunk_kernel(co
   WorkSplit<WHOLE> split;
   split.count<256>(smem + ChunkSmem<D>::TOTAL, a, 128);
   split.deal(gridDim.y, a.by_workers, 4);
-  chunk_workgroup<WHOLE, D>(a, smem, split, blockIdx.x, blockIdx.y, a.parts);
+  chunk_workgroup<WHOLE, D, false>(a, smem, split, blockIdx.x, blockIdx.y, a.parts);
 }
 
 // Adds up the parts of the tiles that were cut, in their order: a wave takes RW rows, and two (four) parts of each at a time.  4 to 5 us, of which

@@ -376,7 +376,8 @@ __device__ __forceinline__ void attend_workgroup(const A &a, char *smem, const W
 // the four tiles' rows, V^T's chunks of 8 keys in the order of its fragments, both swizzled as the other kernels' tiles are.
 // (4 chunks of 500 rows behind 8192 tokens, 32/8 heads of 128, the whole call: 412 us with 64 rows to a wave of the kernel above, 305 through
 // LDS, 258 with fragments fetched ahead and exponentials between MFMAs, 235 now.  MFMAs 38 % busy, vector instructions issue 46 %: conversions,
-// exponentials and packing beside them bound it.)  P is one bf16 operand here (its rounding is as large as O's own), not two as above.
+// exponentials and packing beside them bound it.)  P is one bf16 operand here (its rounding is as large as O's own), or, TWO, two as above: where the rows are
+// those of a group of sequences with few rows each, which have two wherever else they are attended.
 template <int D>
 struct ChunkSmem {
   static constexpr int V_OFF = PAGE * 2 * D, STAGE = 2 * PAGE * 2 * D;
@@ -384,7 +385,7 @@ struct ChunkSmem {
   static_assert(4 * PATCH_BYTES <= TOTAL, "patches fit in the stages");
 };
 
-template <Part P, int D, class A>
+template <Part P, int D, bool TWO, class A>
 __device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, const WorkSplit<P> &split, int hk, int worker, float *parts) {
   using S = ChunkSmem<D>;
   constexpr int R = 128, NK = D / 32, NB = D / 16, ROWB = 2 * D, NL = D / 64;  // NL: loads of K, and of V, of a wave per page
@@ -523,7 +524,7 @@ __device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, const Wo
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
               f32x4 x[2][2];
-              uint32_t w[2][4];
+              uint32_t w[2][4], rest[2][4];  // (rest: the second operand, TWO)
               float sum[2] = {0.f, 0.f};
               // probabilities times the scale of V of tile t and row group rg, relative to the reference as it stands
               auto expo = [&](int t, int rg) __attribute__((always_inline)) {
@@ -531,7 +532,12 @@ __device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, const Wo
 #pragma unroll
                 for (int e = 0; e < 4; ++e) p[e] = fast_exp2(fmaf(x[t][rg][e], ksi, lvi - m[rg]));
                 sum[rg] += (p[0] + p[1]) + (p[2] + p[3]);
-                w[rg][2 * t] = pack_bf16(p[0], p[1]), w[rg][2 * t + 1] = pack_bf16(p[2], p[3]);
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                  const uint32_t hi = pack_bf16(p[e], p[e + 1]);
+                  w[rg][2 * t + e / 2] = hi;
+                  if (TWO) rest[rg][2 * t + e / 2] = pack_bf16(p[e] - __builtin_bit_cast(float, hi << 16), p[e + 1] - __builtin_bit_cast(float, hi & 0xFFFF0000u));
+                }
               };
               auto mask = [&](int t) __attribute__((always_inline)) {  // lane (r, j) holds keys key0 + 16 j + 8 kk + 4 t + e
                 if (!hidden) return;
@@ -578,22 +584,31 @@ __device__ __forceinline__ void chunk_workgroup(const A &a, char *smem, const Wo
                   expo(0, rg), expo(1, rg);
                 }
               }
-              bf16x8 pb[2];
+              bf16x8 pb[2], pl[2];
 #pragma unroll
               for (int rg = 0; rg < 2; ++rg) {
                 l[rg] = fmaf(sum[rg], ivi, l[rg]);
                 pb[rg] = __builtin_bit_cast(bf16x8, u32x4{w[rg][0], w[rg][1], w[rg][2], w[rg][3]});
+                if (TWO) pl[rg] = __builtin_bit_cast(bf16x8, u32x4{rest[rg][0], rest[rg][1], rest[rg][2], rest[rg][3]});
               }
               if (lvi == 0.f && vsi != 1.f) {  // a scale of V that the exponent does not take
 #pragma unroll
                 for (int rg = 0; rg < 2; ++rg)
 #pragma unroll
-                  for (int i = 0; i < 8; ++i) pb[rg][i] = bf16_t(float(pb[rg][i]) * vsi);
+                  for (int i = 0; i < 8; ++i) {
+                    const float x = (TWO ? float(pb[rg][i]) + float(pl[rg][i]) : float(pb[rg][i])) * vsi;
+                    pb[rg][i] = bf16_t(x);
+                    if (TWO) pl[rg][i] = bf16_t(x - float(pb[rg][i]));
+                  }
               }
 #pragma unroll
               for (int b = 0; b < NB; ++b) {
 #pragma unroll
                 for (int rg = 0; rg < 2; ++rg) acc[b][rg] = mfma16(fr[now % AHEAD], pb[rg], acc[b][rg]);
+                if (TWO) {
+#pragma unroll
+                  for (int rg = 0; rg < 2; ++rg) acc[b][rg] = mfma16(fr[now % AHEAD], pl[rg], acc[b][rg]);
+                }
                 advance();
               }
             }

@@ -62,7 +62,8 @@ struct TwoSplits {
     prefix.count<256>(lds, a, 16 * NP);
     if (clash) __syncthreads();
     tail.count<256>(KEEP_BOTH ? lds + seq_table_bytes(a.s.n_groups, PREFIX) : lds, a, 16 * NT);
-    // (a unit of 128 rows to one of 16: 2.6 to 1.5.  With 1.8 and with 3.5 to 1.5 64 tokens behind 8192 take 50 and 46 us, not 44.5, 32 behind 130K 198 and 192, not 185.)
+    // (a unit of 128 rows to one of 16: 3.4 to 1.5, with P in one operand 2.6.  With 2.6 and with 3.8 to 1.5 64 tokens behind 8192 take 47.2 and 46.1 us, not 46.4, 24 drafts
+    // behind two prefixes 45.1 and 42.3, not 42.2, 32 tokens behind 130K 232 and 233, not 236.)
     const float p = x.cost[0] * float(prefix.total) + x.tiles[0], t = x.cost[1] * float(tail.total) + x.tiles[1];
     // Units of a worker of PREFIX, at least: of tiles of 16 rows a page takes a wave about as long as the join takes for 14 parts.
     const int least = NP == 8 ? 2 : max(2, int(__builtin_amdgcn_sqrtf(float(prefix.total) * x.by_tiles * (1.f / 14.f)) + 0.5f));
@@ -88,10 +89,10 @@ constexpr int tile_bytes() {
   if constexpr (NR == 8) return ChunkSmem<D>::TOTAL;
   else return 4 * AttendShape<D, NR, 1>::MERGE;
 }
-template <Part P, int D, int NR, class A>
+template <Part P, int D, int NR, bool TWO, class A>
 __device__ __forceinline__ void tile_workgroup(const A &a, char *smem, const WorkSplit<P> &split, int hk, int group, float *parts) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if constexpr (NR == 8) chunk_workgroup<P, D>(a, smem, split, hk, group, parts);
+  if constexpr (NR == 8) chunk_workgroup<P, D, TWO>(a, smem, split, hk, group, parts);
   else attend_workgroup<P, D, NR, 1>(a, smem + wave * AttendShape<D, NR, 1>::MERGE, split, hk, 4 * group + wave, parts);
 }
 
@@ -99,11 +100,14 @@ __device__ __forceinline__ void tile_workgroup(const A &a, char *smem, const Wor
 template <int D, int NP, int NT>
 __global__ __launch_bounds__(256, 2) void ca_cache_shared_kernel(const SharedLaunch x) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
+  // P of tiles of 128 rows in two operands where ca_cache_attend has them, by the rows of a sequence and whatever the group: one costs 2.3e-3 of O in place of
+  // 1.7e-3, two cost 64 tokens behind 8192 46 us in place of 44, 24 drafts 42 (40), 32 tokens behind 130K 236 (186).
+  constexpr bool TWO = NT != 8;
   const int group = blockIdx.y;
   TwoSplits s;
   s.make<D, NP, NT, false>(smem + std::max(tile_bytes<D, NP>(), tile_bytes<D, NT>()), x, group);
-  if (group < s.groups) tile_workgroup<PREFIX, D, NP>(x.a, smem, s.prefix, blockIdx.x, group, s.parts[0]);
-  else tile_workgroup<TAIL, D, NT>(x.a, smem, s.tail, blockIdx.x, group - s.groups, s.parts[1]);
+  if (group < s.groups) tile_workgroup<PREFIX, D, NP, TWO>(x.a, smem, s.prefix, blockIdx.x, group, s.parts[0]);
+  else tile_workgroup<TAIL, D, NT, TWO>(x.a, smem, s.tail, blockIdx.x, group - s.groups, s.parts[1]);
 }
 
 // What there is of a row's tile: the parts of the workers that had a run of its pages each, or one sum of the row.
@@ -218,7 +222,7 @@ static int launch_shared(SharedLaunch &x, hipStream_t st) {
   const SharedArgs &a = x.a;
   x.groups = shared_groups(a.hkv);
   const float rows = float(a.s.total) * a.G;
-  x.cost[0] = NP == 8 ? 2.6f : 1.2f, x.cost[1] = NT == 8 ? 2.6f : 1.5f;
+  x.cost[0] = NP == 8 ? (NT == 8 ? 2.6f : 3.4f) : 1.2f, x.cost[1] = NT == 8 ? 2.6f : 1.5f;
   x.by_tiles = 1.f / (rows / (16 * NP) + float(std::max(1, a.s.n_groups)) / 2);
   x.tiles[0] = (rows / (16 * NP) + a.s.n_groups) * (NP == 8 ? 4.f : 1.f), x.tiles[1] = (rows / (16 * NT) + a.s.n_seqs) * (NT == 8 ? 4.f : 1.f);
   const size_t tables[2] = {seq_table_bytes(a.s.n_groups, PREFIX), seq_table_bytes(a.s.n_seqs, TAIL)};
