@@ -330,7 +330,9 @@ typedef struct {
   const int32_t *pos; /* DEVICE [rows]: the position of each row, of any sign; not read where the call has sequences */
   int64_t rows, x_stride, dy_stride, y_stride;
   int32_t heads;
+  int32_t gaps;       /* not 0: a row at position CA_ROTATE_GAP takes no part: its y (dx) is left as it is, and dgain has nothing of it */
 } ca_rotate_tensor;
+#define CA_ROTATE_GAP (-2147483647 - 1)
 
 /*
  * ca_rotate: y of one or two tensors (queries and keys, which may have different rows and positions) in one launch.

@@ -10,6 +10,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from .rotary import GAP
 
 
 class _CoreAttention(torch.autograd.Function):
@@ -47,6 +48,18 @@ def row_positions(batch):
     return q, kv
 
 
+def rows_in_use(batch, window=None, sinks=0):
+    """Which rows of the packed Q belong to a task, and which of the packed K some row of a task sees."""
+    q, kv = np.zeros(batch.total_q, bool), np.zeros(batch.total_kv, bool)
+    for doc, a, n, p, length in zip(*(np.asarray(x).tolist() for x in (batch.task_doc, batch.task_q_start, batch.task_q_len, batch.task_q_pos, batch.task_kv_len))):
+        if n > 0:
+            q[a:a + n] = True
+            first, end = int(batch.doc_kv_start[doc]), min(p + n, length)  # (the last row sees end tokens, the first row's window begins furthest back)
+            begin = 0 if window is None else min(max(0, p - window + 1), end)
+            kv[first + begin:first + end] = kv[first:first + min(sinks, end)] = True
+    return q, kv
+
+
 class AttentionServer:
     """One fused batch of CA-tasks planned once and run as a differentiable op:
 
@@ -58,7 +71,8 @@ class AttentionServer:
     have undefined output and zero gradient.  one_pass: see binding.alloc_workspace.  window, sinks: every row attends the last
     `window` keys of its context, itself among them, and the context's first `sinks` (None: all of it); see binding.ca_plan.
     rotation (rotary.Rotation): q and k are turned by the positions of their rows in their documents first, and, with gains, each head of
-    them is normed before: o = server(q, k, v, q_gain, k_gain)."""
+    them is normed before: o = server(q, k, v, q_gain, k_gain).  Rows that no task has, and keys that none sees, add nothing to the gradients
+    of the gains, whatever they hold."""
 
     def __init__(self, batch, device="cuda", one_pass=None, window=None, sinks=0, rotation=None, eps=1e-6):
         if rotation is not None and rotation.head_dim != batch.head_dim:
@@ -68,11 +82,14 @@ class AttentionServer:
         self.fwd_ws_bytes = self.plan.workspace_bytes_split()[0]
         self.rotation, self.eps = rotation, eps
         if rotation is not None:
-            self.q_pos, self.kv_pos = (torch.from_numpy(x).to(device) for x in row_positions(batch))
+            positions = row_positions(batch)
+            self.q_pos, self.kv_pos = (torch.from_numpy(x).to(device) for x in positions)
+            self.grad_pos = [None if used.all() else torch.from_numpy(np.where(used, x, GAP).astype(np.int32)).to(device)
+                             for x, used in zip(positions, rows_in_use(batch, window, sinks))]
 
     def __call__(self, q, k, v, q_gain=None, k_gain=None):
         if self.rotation is not None:
-            q, k = self.rotation(q, k, self.q_pos, self.kv_pos, q_gain=q_gain, k_gain=k_gain, eps=self.eps)
+            q, k = self.rotation(q, k, self.q_pos, self.kv_pos, q_gain=q_gain, k_gain=k_gain, eps=self.eps, grad_pos=self.grad_pos)
         elif q_gain is not None or k_gain is not None:
             raise ValueError("gains without a rotation (one of no frequencies turns nothing)")
         return _CoreAttention.apply(q, k, v, self)

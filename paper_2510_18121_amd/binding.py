@@ -61,7 +61,7 @@ class RotateTensor(ctypes.Structure):
 
     _fields_ = [("x", ctypes.c_void_p), ("dy", ctypes.c_void_p), ("y", ctypes.c_void_p), ("gain", ctypes.c_void_p), ("dgain", ctypes.c_void_p),
                 ("pos", ctypes.c_void_p), ("rows", ctypes.c_int64), ("x_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64),
-                ("y_stride", ctypes.c_int64), ("heads", ctypes.c_int32)]
+                ("y_stride", ctypes.c_int64), ("heads", ctypes.c_int32), ("gaps", ctypes.c_int32)]
 
 
 def lib() -> ctypes.CDLL:
@@ -550,11 +550,11 @@ def _line(rotation, t, shape, dtype, name):
 
 
 # Descriptions as packed bytes, which take a third of the time of a ctypes.Structure (these calls run once per layer and token too).
-_ROTATE_TENSOR = struct.Struct("=6Q4qi4x")  # ca_rotate_tensor
+_ROTATE_TENSOR = struct.Struct("=6Q4q2i")  # ca_rotate_tensor
 _ROTATE_WHERE = struct.Struct("=iiq3Q")     # ca_cache_batch
 
 
-def _rotate_tensor(rotation, x, dy, y, pos, where, gain, dgain, name):
+def _rotate_tensor(rotation, x, dy, y, pos, where, gain, dgain, name, gaps=0):
     """A ca_rotate_tensor; x None: of a gradient without a gain."""
     shape = y.shape
     if len(shape) != 3 or shape[2] != rotation.head_dim:
@@ -573,7 +573,7 @@ def _rotate_tensor(rotation, x, dy, y, pos, where, gain, dgain, name):
         if pos is None:
             raise ValueError(f"{name}: neither positions nor sequences are given")
         pp = _line(rotation, pos, shape[:1], rotation.i32, name)
-    return _ROTATE_TENSOR.pack(xp, dp, yp, gp, dgp, pp, shape[0], xs, ds, ys, shape[1])
+    return _ROTATE_TENSOR.pack(xp, dp, yp, gp, dgp, pp, shape[0], xs, ds, ys, shape[1], gaps)
 
 
 def _rotate_where(rotation, where, rows):
@@ -606,17 +606,18 @@ def ca_rotate(rotation, q, k, q_out, k_out, q_pos=None, k_pos=None, where=None, 
 
 
 def ca_rotate_backward(rotation, q, k, dq_out, dk_out, dq, dk, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, dq_gain=None,
-                       dk_gain=None, eps=1e-6, ws=None, stream=None):
+                       dk_gain=None, eps=1e-6, ws=None, stream=None, q_gaps=False, k_gaps=False):
     """Gradients of ca_rotate: dq and dk (may be dq_out and dk_out) and, with gains, dq_gain and dk_gain (fp32 [head_dim]), from dq_out and dk_out
-    (dk_out None: of q alone).  q and k are needed where there is a gain, as is ws (alloc_rotate_workspace)."""
+    (dk_out None: of q alone).  q and k are needed where there is a gain, as is ws (alloc_rotate_workspace).  q_gaps, k_gaps: rows at
+    position rotary.GAP take no part, whatever they hold: their dq (dk) is left as it is, and the gain's gradient has nothing of them."""
     n, tensors, rows = 0, b"", 0
-    for x, dy, dx, pos, gain, dgain, name in ((q, dq_out, dq, q_pos, q_gain, dq_gain, "q"),
-                                              (k, dk_out, dk, q_pos if k_pos is None else k_pos, k_gain, dk_gain, "k")):
+    for x, dy, dx, pos, gain, dgain, gaps, name in ((q, dq_out, dq, q_pos, q_gain, dq_gain, q_gaps, "q"),
+                                                    (k, dk_out, dk, q_pos if k_pos is None else k_pos, k_gain, dk_gain, k_gaps, "k")):
         if dy is None:
             continue
         if gain is not None and (x is None or dgain is None):
             raise ValueError(f"{name}: with a gain the gradient needs the input, and a tensor for that of the gain")
-        tensors += _rotate_tensor(rotation, x if gain is not None else None, dy, dx, pos, where, gain, dgain, f"{name}, its gradients, positions or gain")
+        tensors += _rotate_tensor(rotation, x if gain is not None else None, dy, dx, pos, where, gain, dgain, f"{name}, its gradients, positions or gain", gaps)
         n, rows = n + 1, dy.shape[0]
     if n == 0:
         raise ValueError("neither dq_out nor dk_out")

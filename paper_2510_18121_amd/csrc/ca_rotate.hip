@@ -41,6 +41,7 @@ struct RotateTensor {
   const int32_t *pos;  // or nullptr: by the sequences
   int64_t rows, x_stride, y_stride, dy_stride;
   int heads, segments, blocks;  // waves per row; workgroups
+  int gaps;                     // rows at position CA_ROTATE_GAP are of nobody
 };
 struct RotateArgs {
   RotateTensor t[2];
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(256) void ca_rotate_kernel(const RotateArgs a) {
     const int this_h0 = h0;
     const bool new_row = h0 == first;
     if (new_row) {
-      pos = next_pos, known = true;
+      pos = next_pos, known = !t.gaps || pos != CA_ROTATE_GAP;
       if (!t.pos) known = position_in_sequence(a, t.rows, row, lane, pos);
     }
     h0 += SLOTS;
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(256) void ca_rotate_kernel(const RotateArgs a) {
       next = load(row, h0);
       if (t.pos && h0 == first) next_pos = t.pos[row];
     }
-    if (!known) continue;  // a row of no sequence
+    if (!known) continue;  // a row of no sequence, a gap
     if (new_row) {
       if (lane < D / 2) mine.cs[lane] = cos_sin(pos, turns) * a.factor;
       wave_sync();
@@ -406,6 +407,7 @@ static int rotate(const ca_rotation *r, const ca_rotate_tensor *tensors, int n, 
     t.x = static_cast<const bf16_t *>(s.x), t.dy = static_cast<const bf16_t *>(s.dy), t.y = static_cast<bf16_t *>(s.y);
     t.gain = s.gain, t.pos = where ? nullptr : s.pos, t.rows = where && where->n_seqs == 0 ? 0 : s.rows;
     t.x_stride = s.x_stride, t.y_stride = s.y_stride, t.dy_stride = s.dy_stride, t.heads = s.heads;
+    t.gaps = !where && s.gaps;
     shape(t, d);
     bytes += t.rows * t.heads * d * (backward && t.gain ? 6 : 4);
     if (backward && s.gain) {

@@ -19,6 +19,7 @@ from fractions import Fraction
 import numpy as np
 import torch
 
+GAP = -2 ** 31  # the position of a row that takes no part in a gradient (see Rotation.__call__)
 TWO_PI = 2 * Fraction(314159265358979323846264338327950288419716939937510, 10 ** 50)
 
 
@@ -84,23 +85,27 @@ class Rotation:
         self.current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
-    def __call__(self, q, k=None, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, eps=1e-6):
+    def __call__(self, q, k=None, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, eps=1e-6, grad_pos=(None, None)):
         """q and k [rows, heads, head_dim] (bf16; k may be None), turned, as contiguous tensors; differentiable in q, k and the gains (fp32
         or bf16 [head_dim]).  Positions: q_pos and k_pos (int32 [rows]; k_pos None: those of q), or where = (q_start, kv_len, ..) of sequences
-        (see binding.ca_rotate).  Rows of no sequence are undefined, and their gradients zero.  A training pass is captured into a graph with
+        (see binding.ca_rotate).  Rows of no sequence are undefined, and their gradients zero.  grad_pos: of q and of k, None or the same positions (int32
+        [rows]) but GAP at rows that have no gradient, whatever they hold: theirs are zero, and they add nothing to the gains'.  A training pass is captured into a graph with
         torch.autograd.grad, while no eager graph of the same leaves lives."""
         gains = [None if g is None else g.float().contiguous() for g in (q_gain, k_gain)]
         q_start, kv_len = (None, None) if where is None else where[:2]
-        out = _Rotate.apply(q, k, *gains, self, q_pos, k_pos, q_start, kv_len, float(eps))
+        out = _Rotate.apply(q, k, *gains, self, q_pos, k_pos, q_start, kv_len, float(eps), *grad_pos)
         return out if k is not None else out[0]
 
 
 class _Rotate(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, q_gain, k_gain, rotation, q_pos, k_pos, q_start, kv_len, eps):
+    def forward(ctx, q, k, q_gain, k_gain, rotation, q_pos, k_pos, q_start, kv_len, eps, q_grad_pos, k_grad_pos):
         from . import binding as B
         yq, yk = (None if x is None else torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k))
         B.ca_rotate(rotation, q, k, yq, yk, q_pos, k_pos, None if q_start is None else (q_start, kv_len), q_gain, k_gain, eps)
+        ctx.gaps = q_grad_pos is not None, k_grad_pos is not None
+        k_pos = k_grad_pos if k_grad_pos is not None else q_pos if k_pos is None else k_pos
+        q_pos = q_pos if q_grad_pos is None else q_grad_pos
         # (without a gain the gradient needs no input)
         ctx.save_for_backward(*(x if g is not None else None for x, g in ((q, q_gain), (k, k_gain))), q_gain, k_gain, q_pos, k_pos, q_start, kv_len)
         ctx.rotation, ctx.eps = rotation, eps
@@ -113,9 +118,10 @@ class _Rotate(torch.autograd.Function):
         q, k, q_gain, k_gain, q_pos, k_pos, q_start, kv_len = ctx.saved_tensors
         where = None if q_start is None else (q_start, kv_len)
         dys = [None if d is None else B.rows_in_line(d) for d in (dyq, dyk)]
-        make = torch.empty if where is None else torch.zeros  # (rows of no sequence)
-        dx = [None if d is None else make(d.shape, dtype=d.dtype, device=d.device) for d in dys]
+        # (zeros: rows of no sequence, and gaps)
+        dx = [None if d is None else (torch.empty if where is None and not gaps else torch.zeros)(d.shape, dtype=d.dtype, device=d.device)
+              for d, gaps in zip(dys, ctx.gaps)]
         dg = [None if g is None else torch.empty_like(g) for g in (q_gain, k_gain)]
         ws = B.alloc_rotate_workspace(dys[0].device) if q_gain is not None or k_gain is not None else None
-        B.ca_rotate_backward(ctx.rotation, q, k, *dys, *dx, q_pos, k_pos, where, q_gain, k_gain, *dg, ctx.eps, ws)
-        return *dx, *dg, None, None, None, None, None, None
+        B.ca_rotate_backward(ctx.rotation, q, k, *dys, *dx, q_pos, k_pos, where, q_gain, k_gain, *dg, ctx.eps, ws, None, *ctx.gaps)
+        return *dx, *dg, *[None] * 8
