@@ -556,6 +556,8 @@ _ROTATE_WHERE = struct.Struct("=iiq3Q")     # ca_cache_batch
 
 def _rotate_tensor(rotation, x, dy, y, pos, where, gain, dgain, name, gaps=0):
     """A ca_rotate_tensor; x None: of a gradient without a gain."""
+    if y is None:
+        raise ValueError(f"{name}: the result is None")
     shape = y.shape
     if len(shape) != 3 or shape[2] != rotation.head_dim:
         raise ValueError(f"{name}: expected [rows, heads, {rotation.head_dim}], got {tuple(shape)}")
@@ -599,7 +601,10 @@ def ca_rotate(rotation, q, k, q_out, k_out, q_pos=None, k_pos=None, where=None, 
     will do; an output may be its input.  Positions: q_pos and k_pos (device int32 [rows]; k_pos None: those of q), or where = (q_start, kv_len, ..) of
     the sequences of a call on a cache: rows are their last ones, and rows of no sequence are left as they are.  Gains: fp32 [head_dim]."""
     n, tensors = 1, _rotate_tensor(rotation, q, None, q_out, q_pos, where, q_gain, None, "q, its output, positions or gain")
-    if k is not None:
+    if k is None:
+        if k_out is not None or k_gain is not None:
+            raise ValueError("an output or a gain of k without k")
+    else:
         n, tensors = 2, tensors + _rotate_tensor(rotation, k, None, k_out, q_pos if k_pos is None else k_pos, where, k_gain, None,
                                                  "k, its output, positions or gain")
     _check(lib().ca_rotate(rotation.desc_ref, tensors, n, _rotate_where(rotation, where, q.shape[0]), eps, _rotate_stream(rotation, stream)))
@@ -614,6 +619,8 @@ def ca_rotate_backward(rotation, q, k, dq_out, dk_out, dq, dk, q_pos=None, k_pos
     for x, dy, dx, pos, gain, dgain, gaps, name in ((q, dq_out, dq, q_pos, q_gain, dq_gain, q_gaps, "q"),
                                                     (k, dk_out, dk, q_pos if k_pos is None else k_pos, k_gain, dk_gain, k_gaps, "k")):
         if dy is None:
+            if dx is not None or dgain is not None:
+                raise ValueError(f"{name}: a gradient without that of the output")
             continue
         if gain is not None and (x is None or dgain is None):
             raise ValueError(f"{name}: with a gain the gradient needs the input, and a tensor for that of the gain")
