@@ -290,8 +290,8 @@ int ca_cache_attend_shared_workspace_bytes(const ca_cache *cache, int32_t n_q_he
 /*
  * ca_cache_read: the rows of the batch back out of the pages of their sequences: k and v (device bf16 [total_rows][n_kv_heads][head_dim], 16-byte aligned; one of them may be
  * NULL) receive code * scale, rounded once (NaN where the code is; exact, but for values below bf16's normal range, where scales are powers of two, as ca_cache_append makes them).
- * A token whose page_table entry is no page reads as zeros.  Rows of no sequence, of tokens before a sequence's first and of those beyond the table are left as
- * they are.  One launch on hip_stream; allocates nothing, never synchronises.
+ * A token whose page_table entry is no page reads as zeros.  Rows of no sequence and of tokens before a sequence's first are left as they are; a length beyond the
+ * table counts as far as that goes (see ca_cache_batch), so that the rows are then the last tokens the table has.  One launch on hip_stream; allocates nothing, never synchronises.
  */
 int ca_cache_read(const ca_cache *cache, const ca_cache_batch *batch, void *k, void *v, void *hip_stream);
 
@@ -337,7 +337,8 @@ typedef struct {
 /*
  * ca_rotate: y of one or two tensors (queries and keys, which may have different rows and positions) in one launch.
  * where: NULL, or the sequences of the rows (n_seqs, q_start and kv_len of a ca_cache_batch are read, on the device): row r of sequence s is
- * at position kv_len[s] - (q_start[s + 1] - r), and rows of no sequence are left as they are.
+ * at position kv_len[s] - (q_start[s + 1] - r), a q_start beyond the tensor's rows counting as far as they go, and rows of no sequence are left as they are.  The
+ * table is not looked at: a kv_len beyond it, which the calls on the cache take for what the table holds, is taken as it is.
  * ca_rotate_backward: dx, and dgain (the sum over all rows and heads, in a fixed order), of the same y: all but y and dy as in the forward call.  ws: device
  * workspace of ca_rotate_backward_workspace_bytes, 16-byte aligned, needed where there is a gain; calls that may overlap in time need one
  * each.  One launch, or two with gains.  dx rows of no sequence are left as they are.
