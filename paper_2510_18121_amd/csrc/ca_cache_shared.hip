@@ -36,6 +36,7 @@ struct SharedLaunch {
   int groups;                // workgroups per KV head, of both kinds
   float cost[2], tiles[2];   // of PREFIX and of TAIL: what a unit costs a workgroup, and all tiles beside their units
   float by_tiles;            // 1 / the tiles of PREFIX, about
+  int one_tile;              // the average sequence's rows are one tile of TAIL: a page of it is read once
 };
 
 // A worker is a workgroup where tiles are of 128 rows, otherwise a wave.
@@ -74,8 +75,9 @@ struct TwoSplits {
     prefix.run = max(__builtin_amdgcn_readfirstlane(least), quotient(prefix.total + max(workers[0], 1) - 1, max(workers[0], 1)));
     tail.run = max(1, quotient(tail.total + workers[1] - 1, workers[1]));
     prefix.cut = tail.cut = CUT_SHARED;
-    // (tails that the last cache does not hold until the next call, as in ca_cache_attend; what is shared is fetched by several tiles)
-    tail.stream = float(tail.total) * float(a.hkv * 2 * PAGE * D) > float(384 << 20);
+    // Tails that the last cache does not hold until the next call, as in ca_cache_attend.  Not what is fetched by several tiles: the prefix, and tails of more rows (24 sequences
+    // of 20 or 32 rows behind a prefix of 6000, 8 heads of 128: tails of 329 MiB 145 us past the cache, 128 through it, 446 MiB 197 and 173, 835 MiB 296 and 286, 890 MiB 336 and 342).
+    tail.stream = x.one_tile && float(tail.total) * float(a.hkv * 2 * PAGE * D) > float(384 << 20);
     parts[0] = x.parts, parts[1] = x.parts + size_t(workers[0]) * 2 * a.hkv * (16 * NP * (D + 2));
     if (clash && group < groups) {
       __syncthreads();
@@ -223,6 +225,7 @@ static int launch_shared(SharedLaunch &x, hipStream_t st) {
   x.groups = shared_groups(a.hkv);
   const float rows = float(a.s.total) * a.G;
   x.cost[0] = NP == 8 ? (NT == 8 ? 2.6f : 3.4f) : 1.2f, x.cost[1] = NT == 8 ? 2.6f : 1.5f;
+  x.one_tile = int64_t(a.s.total) * a.G <= int64_t(16 * NT) * a.s.n_seqs;
   x.by_tiles = 1.f / (rows / (16 * NP) + float(std::max(1, a.s.n_groups)) / 2);
   x.tiles[0] = (rows / (16 * NP) + a.s.n_groups) * (NP == 8 ? 4.f : 1.f), x.tiles[1] = (rows / (16 * NT) + a.s.n_seqs) * (NT == 8 ? 4.f : 1.f);
   const size_t tables[2] = {seq_table_bytes(a.s.n_groups, PREFIX), seq_table_bytes(a.s.n_seqs, TAIL)};
@@ -242,7 +245,9 @@ static int launch_shared(SharedLaunch &x, hipStream_t st) {
 }
 
 // Rows per tile, as in ca_cache_attend, from the average group and the average sequence.  (Tiles of 32 rows, as there, are none here: at head_dim 128 they leave
-// room for four waves to a CU, 8 answers to a prompt of 2048 tokens 20.6 us with them and 17.8 without; at 64 200 answers to nine of 4000 72 and 68.)
+// room for four waves to a CU, 8 answers to a prompt of 2048 tokens 20.6 us with them and 17.8 without; at 64 200 answers to nine of 4000 72 and 68.  Without them sequences of
+// 17 to 32 rows read their tails twice: 24 of 20 rows behind 6000 tokens of one prefix, 8 heads of 128, tails of about 500 tokens 46 us and ca_cache_attend 55, of 2000 63 and 68, of 5000 128 and
+// 105, of 16000 286 and 200.  Sequences of more rows, whose prefix is bound by its products, gain nothing: 4 of 500 behind 8192, 32 heads, 366 and 313, at 64 281 and 195.)
 template <int D>
 static int shared_by_rows(SharedLaunch &x, hipStream_t st) {
   const SharedArgs &a = x.a;
