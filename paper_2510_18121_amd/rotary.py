@@ -75,8 +75,12 @@ class Rotation:
         self.head_dim, self.rot_dim, self.interleaved, self.factor = head_dim, 2 * freq.size, bool(interleaved), float(factor)
         self.frequencies = freq
         self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self._describe()
+
+    def _describe(self):
+        """What belongs to this process and to where `turns` lies."""
         self.device = self.turns.device
-        self.desc = RotationDesc(head_dim, self.rot_dim, self.interleaved, self.factor, self.turns.data_ptr() if freq.size else None)
+        self.desc = RotationDesc(self.head_dim, self.rot_dim, self.interleaved, self.factor, self.turns.data_ptr() if self.rot_dim else None)
         self.desc_ref = ctypes.byref(self.desc)
         # what the calls look up every time
         self.index = self.turns.get_device() if self.turns.is_cuda else None  # (None: no tensor is there)
@@ -84,6 +88,13 @@ class Rotation:
         # (where there is a tensor on a device it is initialised, which is what torch.cuda.current_device looks at first)
         self.current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+    def __getstate__(self):  # (copied and saved with the module that holds it)
+        return {x: getattr(self, x) for x in ("head_dim", "rot_dim", "interleaved", "factor", "frequencies", "turns")}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self._describe()
 
     def __call__(self, q, k=None, q_pos=None, k_pos=None, where=None, q_gain=None, k_gain=None, eps=1e-6, grad_pos=(None, None)):
         """q and k [rows, heads, head_dim] (bf16; k may be None), turned, as contiguous tensors; differentiable in q, k and the gains (fp32
