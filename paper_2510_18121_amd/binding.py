@@ -471,7 +471,7 @@ def ca_cache_attend(cache, q, o, lse, q_start, kv_len, page_table, ws, window=No
 
 def ca_cache_attend_shared(cache, q, o, lse, q_start, kv_len, page_table, group_start, prefix_pages, ws, softmax_scale=0.0, stream=None):
     """ca_cache_attend where groups of sequences share their first pages, which are attended once for all rows of a group: group g has the sequences
-    group_start[g] .. group_start[g + 1] - 1, and their first prefix_pages[g] pages are the same (device int32; cache.Sequences.groups).
+    group_start[g] .. group_start[g + 1] - 1, and their first prefix_pages[g] pages are the same (device int32; cache.Sequences.groups, which says when it pays).
     ws: alloc_shared_workspace."""
     rows, hq, _ = shape = q.shape
     qp = _on_cache(cache, q, (rows, hq, cache.head_dim), cache.bf16, "q")

@@ -158,7 +158,11 @@ class Sequences:
     def groups(self, seqs, rows, device=None):
         """group_start and prefix_pages (int32) of binding.ca_cache_attend_shared, for a call with the last rows[i] tokens of seqs[i]: neighbours in `seqs`
         that share their first pages make up groups, so that the most pages are read once instead of again.  (The arrays stay right
-        as long as the same sequences grow: they are made anew when sequences come or go, or let go of pages.)"""
+        as long as the same sequences grow: they are made anew when sequences come or go, or let go of pages.)
+        Whether sharing pays is for the caller to decide: with 32/8 heads of 128 from about 16 sequences of one new token behind 8192 shared ones, or 64 behind
+        512, on; fewer, or sequences of more than 16 rows per KV head (queries times heads of a group) with long tails, are faster in ca_cache_attend.  Sequences that
+        share nothing are groups of no pages here; where those that share come first in `seqs`, the groups behind theirs are better left off
+        (group_start[:g + 1], prefix_pages[:g])."""
         seqs, rows = list(seqs), [operator.index(n) for n in rows]
         if len(seqs) != len(rows):
             raise ValueError("groups: one count of rows for each of the sequences")

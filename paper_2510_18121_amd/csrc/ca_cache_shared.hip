@@ -8,13 +8,15 @@
 // bound by the matrix products, 4 D flops per (row, head, token), and the tails by reading them.  Both go on side by side, in one launch of
 // workgroups of either kind (ca_cache_attend.h); a second one joins the results and the parts of the tiles that were cut.
 // Measured, whole calls (of which 9 to 10 us are the second launch and the gap before it), 8 KV heads of 128 unless noted, and ca_cache_attend beside it:
-//   64 tokens behind 8192, tails of about 560 tokens, 32 heads      44 us (106)
-//   32 tokens behind 130K, 64 heads                                184 to 195 us (703): 0.74 PFLOP/s, MFMAs 36 % busy
-//   24 drafts of 3 to 5 rows behind two prefixes of about 5000       40 us (51)
+//   64 tokens behind 8192, tails of about 560 tokens, 32 heads      46 to 47 us (104)
+//   32 tokens behind 130K, 64 heads                                234 to 242 us (703): 0.58 PFLOP/s, MFMAs 43 % busy (a third of them for P's second operand)
+//   24 drafts of 3 to 5 rows behind two prefixes of about 5000       42 us (51)
 //   200 tokens behind nine prefixes of up to 4000, 16/16 heads of 64  67 us (145): the tails' 165 MB in 45 of them
 //   8 tokens behind 2048                                            17 us (17): fixed times, 6 us from the start to the end of one page, most of it cold code and trips to memory
 // It pays from about 16 sequences of 8192 shared tokens, or 64 of 512, on; 2 to 8 sequences behind less than 8192 tokens are 1 to 5 us faster without.
-// Not kept: every workgroup with a share of both kinds (47 to 51 us, 190, 52, 76 in the first four: a second start costs what the balance gains); runs by what a
+// Sequences that share nothing cost less in no group than as groups of no pages, which count in the average that tiles go by: 64 behind 8192 beside 100 of about 1000
+// tokens 86 and 99 us (151 without sharing), 16 behind 32768 beside 100 79 and 96 (163), 2 behind 8192 beside 198 109 and 108 (97).
+// Not kept (measured with P of the prefix in one operand): every workgroup with a share of both kinds (47 to 51 us, 190, 52, 76 in the first four: a second start costs what the balance gains); runs by what a
 // workgroup has beside it on its CU (46 to 49, 184 to 218); tails with workgroups of four waves (200 behind nine: 88); P of the tails as one operand (level).
 #include <hip/hip_runtime.h>
 

@@ -13,6 +13,9 @@
 // lane, and handed out through the wave's LDS.  Measured (32/8 heads of 128 unless noted; a copy of 512 MB in turn: 5.3 to 5.6 TB/s):
 //   forward    65536 rows with gains 228 to 238 us, 5.6 to 5.9 TB/s; 40001 out of a joint projection 140 to 148
 //   backward   65536 rows with gains 357 to 367 us, 5.5 TB/s; 16411 rows of 16/16 heads of 64: 27 forward, 38 to 48 backward
+//   half of each head of 128 turned in halves 298 and 420, whose lanes read runs that are further apart; a number of pairs that is no multiple of 8, through LDS:
+//   120 or 38 columns of 128 250 to 257 forward, 407 to 419 backward; 58 or 26 of 64 of the 16411 rows 32 and 61 to 64
+//   without gains 65536 rows 232 and 235, 16411 rows 24 and 24
 //   one row 3.1 us, 250 rows of 64/8 heads 5.1 (a launch, and the trips to memory for the position and the row)
 #include <hip/hip_runtime.h>
 
